@@ -355,6 +355,144 @@ int lutgemm_plan_group(const int64_t* m, const int64_t* n, int count, int q, int
    sink_bytes < 32768 is LUTGEMM_EWORKSPACE.                                              */
 int lutgemm_stream_read(const void* src, size_t bytes, void* sink, size_t sink_bytes, void* hip_stream);
 
+/* =======================================================================================
+ * The attention half of a decode step: what stands between a layer's query/key/value product
+ * and its output product.  Rotary positions, a key/value cache of 16, 8 or 4 bits a value, and
+ * attention of a few new tokens of each sequence over it.  Everything is fp16 unless it says
+ * otherwise; strides are in elements.
+ * ======================================================================================= */
+
+/* `flags` of lutgemm_rope (beside LUTGEMM_Y_F16 / LUTGEMM_Y_F32, which name the type of x and y). */
+enum {
+  LUTGEMM_ROPE_NEIGHBOURS = 8,  /* pair i is channels (2i, 2i + 1); else (i, i + rot_dim / 2) */
+  LUTGEMM_ROPE_TRANSPOSE = 16   /* turn back: the gradient, and for amplitude 1 the inverse   */
+};
+
+/* `scaling` of lutgemm_rope_frequencies: how positions beyond the trained length are met. */
+enum {
+  LUTGEMM_ROPE_PLAIN = 0,   /* f_i = base^(-2 i / rot_dim) radians a position                       */
+  LUTGEMM_ROPE_LINEAR = 1,  /* f_i / factor                                                         */
+  LUTGEMM_ROPE_BASE = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) in place of base: the slowest
+                               pair is slowed by factor, the fastest is not (rot_dim = 2: PLAIN)    */
+  LUTGEMM_ROPE_PARTS = 3    /* by how often a pair turns within the trained length, n_i = f_i *
+                               trained / (2 pi): kept where n_i >= high, divided by factor where
+                               n_i <= low, between them weighted linearly                           */
+};
+
+/* HOST.  The rot_dim / 2 frequencies as 64-bit fractions of a turn a position:
+   turns[i] = round(2^64 f_i / (2 pi)), computed in double.  In this form position * frequency modulo one turn is an exact
+   integer product at any position.  rot_dim even, 2..65536; base > 1; factor >= 1; low < high and
+   trained > 0 for PARTS (ignored otherwise).                                             */
+int lutgemm_rope_frequencies(int rot_dim, double base, int scaling, double factor, double low, double high,
+                             double trained, uint64_t* turns);
+
+/* DEVICE.  Rotary positions: for every token t, head h and pair i (channels a, b of the head)
+     y_a = amplitude * (x_a cos - x_b sin),   y_b = amplitude * (x_a sin + x_b cos)
+   at the angle positions[t] * f_i; with LUTGEMM_ROPE_TRANSPOSE at minus that angle.  The first rot_dim
+   channels of a head are turned, the others copied.  fp32 arithmetic, one rounding.
+     x          [tokens] rows of x_stride elements, a row's heads one after the other, head_dim each
+     y          the same with y_stride; may be x (with the same stride), else must not overlap it
+     positions  int32 [tokens], negative ones included       turns  uint64 [rot_dim / 2], 8-byte aligned
+   head_dim even, up to 512; rot_dim even, 2..head_dim; strides >= heads * head_dim.  Query and key heads of
+   one product's rows are neighbours there: one call turns both.  Any alignment of x and y
+   that their type has; 16-byte aligned rows, heads and halves are faster.
+   tokens = 0 does nothing.                                                               */
+int lutgemm_rope(const void* x, void* y, const int32_t* positions, const uint64_t* turns, int tokens, int heads,
+                 int head_dim, int rot_dim, int64_t x_stride, int64_t y_stride, float amplitude, unsigned flags,
+                 void* hip_stream);
+
+/* A cache: a pool of pages of page_tokens positions (a multiple of 32) of all key/value heads.
+     head_dim  64, 96, 128, 192 or 256
+     bits      16: values as they are (fp16).  8: signed integers and a scale for every `group`
+               channels of a position's head.  4: unsigned integers, a scale and an offset
+     group     a multiple of 32 that divides head_dim; 0: the whole head
+   Quantisation of a group's values x (fp16), all in fp32:
+     8 bits    s = max|x| / 127 rounded TOWARDS ZERO to fp16, u = rint(x / s) in -127..127, kept as u + 128
+     4 bits    z = min x, s = (max x - z) / 15 rounded towards zero to fp16, u = rint((x - z) / s) in 0..15
+   (rint to even; s = 0 gives u = 0; rounding s down keeps every value within the group's range, so none
+   overflows.)  A code stands for fp16(s * u) or fp16(s * u + z), rounded once: this is what lutgemm_kv_read
+   returns and what lutgemm_attention multiplies with.  A group that holds an infinity or a NaN reads
+   as NaN throughout.
+
+   Layout of the pool.  Position p of a sequence is in its page p / page_tokens, block
+   (p % page_tokens) / 32, place n = p % 32.  A block of one head is contiguous, blocks of a head in a page
+   follow each other, heads follow each other, then pages:
+     block offset = ((page * heads + head) * (page_tokens / 32) + block) * block bytes
+     block = key codes | key scales | value codes | value scales
+   Codes are kept in units of 32 channels (channel d: unit c = d / 32), a unit as the lanes of a
+   wavefront hold it: 64 lanes with two runs (j = 0, 1) of eight values (e = 0..7) each.
+     keys     place n = 8 a + 4 j + b (a, b = 0..3), channel 32 c + 8 g + e   in lane 16 g + 4 a + b
+     values   place n = 8 g + e,            channel 32 c + 16 j + r  in lane 16 g + r
+     8 bits   byte       ((c * 64 + lane) * 2 + j) * 8 + e
+     16 bits  half word  ((c * 2 + j) * 64 + lane) * 8 + e
+     4 bits   keys: nibble e / 2 + 4 (e % 2) (0 = lowest) of the word at byte ((c * 64 + lane) * 2 + j) * 4;
+              values: nibble j of the byte (c * 64 + lane) * 8 + 4 (e / 4) + {0, 2, 1, 3}[e % 4]
+   Scales (fp16), group G of a head:
+     keys     8 bits: half word G * 32 + (4 a + b) * 2 + j;  4 bits: s at G * 64 + (4 a + b) * 4 + 2 j, z after it
+     values   8 bits: half word G * 32 + n;  4 bits: s at G * 64 + n, z at G * 64 + 32 + n
+   A position's bytes are its own: writing one position leaves all others as they are.    */
+typedef struct lutgemm_kv_cache {
+  void* pool;          /* DEVICE, 16-byte aligned, lutgemm_kv_pool_bytes; need not be initialised */
+  int64_t pages;
+  int page_tokens, heads, head_dim, bits, group;
+} lutgemm_kv_cache;
+
+/* The new tokens of a step.  Rows first[s] .. first[s + 1] - 1 of the step's tokens belong to
+   sequence s and stand at its positions past[s], past[s] + 1, ...; its position p is in page
+   table[s * table_pages + p / page_tokens].  Arrays are DEVICE memory, so that a captured graph can be
+   replayed with other lengths.  What the host says besides must bound them: every first[s + 1] - first[s]
+   <= most_tokens.  The kernels check what they read: rows outside 0..tokens, positions beyond the table and page
+   numbers outside the pool are left out (not written, read as zeros, not seen by attention). */
+typedef struct lutgemm_kv_step {
+  const int32_t* first;  /* [seqs + 1] */
+  const int32_t* past;   /* [seqs]     */
+  const int32_t* table;  /* [seqs][table_pages] */
+  int seqs, table_pages, tokens, most_tokens;
+} lutgemm_kv_step;
+
+/* Bytes of a pool; 0 for a shape that is not offered. */
+size_t lutgemm_kv_pool_bytes(int64_t pages, int page_tokens, int heads, int head_dim, int bits, int group);
+
+/* DEVICE.  Quantise the step's keys and values into the cache.  Row r of k (v) is at k + r * k_stride, heads one after the
+   other: the key and value parts of a product's rows serve as they are.  rows: NULL, or int32 [tokens]:
+   the token at place i of the step takes row rows[i] of k and v (>= 0; a negative one is left out); with it the accepted
+   tokens of a drafted tree are written again, next to each other.  k or v may be NULL: only
+   the other is written.  k, v 16-byte aligned, strides multiples of 8.                   */
+int lutgemm_kv_write(const void* k, const void* v, const int32_t* rows, const lutgemm_kv_cache* cache,
+                     const lutgemm_kv_step* step, int64_t k_stride, int64_t v_stride, void* hip_stream);
+
+/* DEVICE.  The reverse: positions past[s] .. of every sequence as fp16 rows of k and v (either may be NULL).  Any
+   range of positions is a step: past = where it begins.                                 */
+int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, void* k, void* v, int64_t k_stride,
+                    int64_t v_stride, void* hip_stream);
+
+/* DEVICE.  Attention of the step's tokens over the cache, which holds their own keys and values already:
+     y[t][h] = sum_p w_p V_p,   w = softmax over the positions p that token t sees of scale * q[t][h] . K_p
+   with the keys and values of head h / (q_heads / heads).  Token t of sequence s sees every position before past[s], and
+   of the new ones position past[s] + j where bit j of mask[t] is set (a token that sees itself has its
+   own bit set; bits beyond the sequence's tokens count for nothing).  mask NULL: each new token sees itself and those before it.  A
+   row that sees nothing is zero.  Up to 64 new tokens a sequence; a longer prompt is taken in chunks.
+     q, y            fp16 rows of q_stride / y_stride, heads one after the other; 16-byte aligned, strides
+                     multiples of 8.  y must not overlap q
+     mask            uint64 [tokens] or NULL
+     most_positions  of the longest sequence after this step; 0: as many as the table holds.  Only
+                     how the work is split depends on it: the result is right for longer ones too
+     workspace       lutgemm_attention_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any
+                     other and shared with products on the same stream if large enough
+   Products and sums are fp32, the weights w are rounded to fp16 before they meet V.  Infinities and NaNs in positions that a row does
+   not see do not reach it.  Bitwise reproducible.                                        */
+int lutgemm_attention(const void* q, const uint64_t* mask, const lutgemm_kv_cache* cache, const lutgemm_kv_step* step,
+                      void* y, int q_heads, int64_t q_stride, int64_t y_stride, float scale, int64_t most_positions,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,
+                                         int64_t most_positions);
+
+/* HOST.  How lutgemm_attention splits such a call: out[0] tiles of 16 rows (token, query head) that a wavefront holds, out[1]
+   workgroups along the rows of a key head, out[2] along the positions, out[3] positions of each
+   of these, out[4] wavefronts of a workgroup.                                            */
+int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,
+                           int64_t most_positions, int* out);
+
 /* Human-readable name of an error code (static storage).                                */
 const char* lutgemm_strerror(int code);
 

@@ -1,6 +1,6 @@
 """Build liblutgemm.so (gfx950) in-tree with hipcc.  `python -m paper_2206_09557_amd.build`.
 
-The device source is compiled once per kernel family (-DLUT_PART=k) in parallel, then linked with the host source."""
+The device sources are compiled once per kernel family (-DLUT_PART=k) in parallel, then linked with the host sources."""
 from __future__ import annotations
 
 import os
@@ -14,11 +14,11 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "liblutgemm.so")
-HOST_SOURCE = os.path.join(PKG, "csrc", "lutgemm_host.cpp")
-DEVICE_SOURCE = os.path.join(PKG, "csrc", "lutgemm_device.hip")
+HOST_SOURCES = ("lutgemm_host.cpp", "lutgemm_kv_host.cpp")
+# device sources and the kernel families of each (LUT_PART = 0, 1, ...)
+DEVICE_SOURCES = {"lutgemm_device.hip": 20, "lutgemm_kv.hip": 1, "lutgemm_attention.hip": 15}
 BINDING = os.path.join(PKG, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))   # of this Python alone
 BINDING_SOURCE = os.path.join(PKG, "csrc", "lutgemm_binding.cpp")
-PARTS = 20   # kernel families of lutgemm_device.hip (LUT_PART = 0 .. 19)
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-pthread",
@@ -52,16 +52,17 @@ def build_library(verbose: bool = True, jobs: int | None = None, report: bool = 
     them use scratch memory (none should: a spill in a lookup loop costs more than any
     prefetch hides) and the largest LDS allocation."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    jobs = jobs or min(PARTS + 1, os.cpu_count() or 1, 16)
+    jobs = jobs or min(os.cpu_count() or 1, 16)
     inc = ["-I", os.path.join(ROOT, "include")]
     with tempfile.TemporaryDirectory(prefix="lutgemm_build_") as tmp:
-        units = [(HOST_SOURCE, os.path.join(tmp, "host.o"), [])]
-        units += [(DEVICE_SOURCE, os.path.join(tmp, f"device_{k}.o"), [f"-DLUT_PART={k}"]) for k in range(PARTS)]
+        units = [(os.path.join(PKG, "csrc", name), os.path.join(tmp, name + ".o"), []) for name in HOST_SOURCES]
+        units += [(os.path.join(PKG, "csrc", name), os.path.join(tmp, f"{name}_{k}.o"), [f"-DLUT_PART={k}"])
+                  for name, parts in DEVICE_SOURCES.items() for k in range(parts)]
 
         def compile_unit(unit):
             src, obj, extra = unit
             cmd = [hipcc, *HIPCC_FLAGS, *extra, *inc, "-c", "-o", obj, src]
-            if report and src == DEVICE_SOURCE:
+            if report and src.endswith(".hip"):
                 cmd.append("-Rpass-analysis=kernel-resource-usage")
             if verbose:
                 print(" ".join(cmd), flush=True)

@@ -1,0 +1,66 @@
+// The key/value cache's layout as the kernels and the host helpers number it (the contract is in lutgemm.h), and the
+// checks that every entry point on a cache shares.
+#ifndef LUTGEMM_KV_H
+#define LUTGEMM_KV_H
+
+#include <cstddef>
+#include <cstdint>
+
+#include "lutgemm.h"
+
+namespace lutgemm_kv_detail {
+
+constexpr int kBlock = 32;        // positions of a block, channels of a unit
+constexpr int kMostTokens = 64;   // new tokens of a sequence that attention takes: one bit each in a mask word
+
+// Bytes of one block's keys (or values): codes, then scales.
+inline int code_bytes(int head_dim, int bits) { return kBlock * head_dim * bits / 8; }
+inline int scale_bytes(int head_dim, int bits, int group) {
+  return bits == 16 ? 0 : head_dim / group * kBlock * (bits == 8 ? 2 : 4);
+}
+inline int block_bytes(int head_dim, int bits, int group) {
+  return 2 * (code_bytes(head_dim, bits) + scale_bytes(head_dim, bits, group));
+}
+
+inline int group_of(int head_dim, int bits, int group) { return group == 0 || bits == 16 ? head_dim : group; }
+
+// LUTGEMM_OK if a cache can have this shape.
+inline int check_shape(int64_t pages, int page_tokens, int heads, int head_dim, int bits, int group) {
+  if (pages < 1 || page_tokens < kBlock || page_tokens % kBlock != 0 || heads < 1 || head_dim < 1 || group < 0) return LUTGEMM_EINVAL;
+  if (bits != 4 && bits != 8 && bits != 16) return LUTGEMM_EUNSUPPORTED;
+  if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 192 && head_dim != 256) return LUTGEMM_EUNSUPPORTED;
+  const int g = group_of(head_dim, bits, group);
+  if (head_dim % g != 0) return LUTGEMM_EINVAL;
+  if (g % kBlock != 0) return LUTGEMM_EUNSUPPORTED;
+  if (pages > INT32_MAX || page_tokens > 1 << 20 || heads > 1 << 12) return LUTGEMM_EUNSUPPORTED;
+  return LUTGEMM_OK;
+}
+
+inline int check_cache(const lutgemm_kv_cache* c) {
+  if (!c || !c->pool || ((uintptr_t)c->pool & 15) != 0) return LUTGEMM_EINVAL;
+  return check_shape(c->pages, c->page_tokens, c->heads, c->head_dim, c->bits, c->group);
+}
+
+inline int check_step(const lutgemm_kv_step* s) {
+  if (!s || !s->first || !s->past || !s->table) return LUTGEMM_EINVAL;
+  if ((((uintptr_t)s->first | (uintptr_t)s->past | (uintptr_t)s->table) & 3) != 0) return LUTGEMM_EINVAL;
+  if (s->seqs < 1 || s->table_pages < 1 || s->tokens < 0 || s->most_tokens < 0) return LUTGEMM_EINVAL;
+  if (s->seqs > 65535) return LUTGEMM_EUNSUPPORTED;
+  return LUTGEMM_OK;
+}
+
+// How lutgemm_attention splits its work; see plan_attention in lutgemm_kv_host.cpp.
+struct AttentionPlan {
+  int row_tiles;    // tiles of 16 rows (token, query head) that a wavefront holds
+  int row_blocks;   // workgroups along the rows of a key head
+  int splits;       // workgroups along the positions, at most
+  int chunk;        // positions of a split: a multiple of 32
+  int waves;        // wavefronts of a workgroup
+};
+AttentionPlan plan_attention(int heads, int head_dim, int bits, int q_heads, int seqs, int most_tokens, int64_t most_positions);
+// Floats of the partial results behind the workspace's counters (0: nothing is split).
+int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens);
+
+}  // namespace lutgemm_kv_detail
+
+#endif

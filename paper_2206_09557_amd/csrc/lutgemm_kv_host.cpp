@@ -1,0 +1,105 @@
+// Host side of the attention half: sizes of caches and workspaces, how attention splits its work, rotary frequencies.
+// Nothing here touches the GPU.
+#include "lutgemm_kv.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace lutgemm_kv_detail {
+
+namespace {
+constexpr int64_t kCounters = 8192;      // arrival counters of a workspace (32 KB)
+constexpr int64_t kWorkgroups = 1024;    // that fill 256 compute units, four wavefronts each
+}  // namespace
+
+AttentionPlan plan_attention(int heads, int head_dim, int bits, int q_heads, int seqs, int most_tokens, int64_t most_positions) {
+  (void)bits;
+  AttentionPlan p;
+  const int64_t rows = (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads);
+  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 || head_dim > 128 ? 2 : 4);
+  p.row_blocks = (int)std::max<int64_t>(1, (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+  p.waves = 4;
+  const int64_t units = (int64_t)seqs * heads * p.row_blocks;
+  const int64_t blocks = std::max<int64_t>(1, (most_positions + kBlock - 1) / kBlock);
+  // Splits until the device is full, of no fewer than four blocks a wavefront (the partial results of a split cost
+  // its rows once more, and the last workgroup reads them all), where there are counters for them.
+  int64_t splits = units > kCounters ? 1 : std::min((kWorkgroups + units - 1) / units, (blocks + 4 * p.waves - 1) / (4 * p.waves));
+  splits = std::max<int64_t>(1, std::min<int64_t>(splits, 256));
+  const int64_t per = (blocks + splits - 1) / splits;
+  p.chunk = (int)std::min<int64_t>(per, 1 << 24) * kBlock;
+  p.splits = (int)((blocks + per - 1) / per);
+  return p;
+}
+
+int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens) {
+  if (p.splits == 1) return 0;
+  const int64_t rows = std::min<int64_t>(16 * p.row_tiles, (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads));
+  return (int64_t)seqs * heads * p.row_blocks * p.splits * rows * (head_dim + 2);
+}
+
+}  // namespace lutgemm_kv_detail
+
+using namespace lutgemm_kv_detail;
+
+namespace {
+
+// LUTGEMM_OK and the plan of a call's shape.
+int plan_of(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, AttentionPlan* plan) {
+  if (!cache || !step || step->seqs < 1 || step->table_pages < 1 || step->most_tokens < 0 || q_heads < 1 || most_positions < 0) return LUTGEMM_EINVAL;
+  const int rc = check_shape(cache->pages, cache->page_tokens, cache->heads, cache->head_dim, cache->bits, cache->group);
+  if (rc != LUTGEMM_OK) return rc;
+  if (q_heads % cache->heads != 0) return LUTGEMM_EINVAL;
+  if (step->seqs > 65535 || step->most_tokens > kMostTokens || q_heads > 1 << 14) return LUTGEMM_EUNSUPPORTED;
+  const int64_t held = (int64_t)step->table_pages * cache->page_tokens;
+  if (most_positions == 0 || most_positions > held) most_positions = held;
+  *plan = plan_attention(cache->heads, cache->head_dim, cache->bits, q_heads, step->seqs, step->most_tokens, most_positions);
+  return LUTGEMM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lutgemm_kv_pool_bytes(int64_t pages, int page_tokens, int heads, int head_dim, int bits, int group) {
+  if (check_shape(pages, page_tokens, heads, head_dim, bits, group) != LUTGEMM_OK) return 0;
+  return (size_t)pages * heads * (page_tokens / kBlock) * block_bytes(head_dim, bits, group_of(head_dim, bits, group));
+}
+
+size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions) {
+  AttentionPlan p;
+  if (plan_of(cache, step, q_heads, most_positions, &p) != LUTGEMM_OK) return 0;
+  return 32768 + 4 * (size_t)attention_partial_floats(p, cache->heads, cache->head_dim, q_heads, step->seqs, step->most_tokens);
+}
+
+int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, int* out) {
+  AttentionPlan p;
+  if (!out) return LUTGEMM_EINVAL;
+  const int rc = plan_of(cache, step, q_heads, most_positions, &p);
+  if (rc != LUTGEMM_OK) return rc;
+  const int v[5] = {p.row_tiles, p.row_blocks, p.splits, p.chunk, p.waves};
+  std::copy(v, v + 5, out);
+  return LUTGEMM_OK;
+}
+
+int lutgemm_rope_frequencies(int rot_dim, double base, int scaling, double factor, double low, double high, double trained, uint64_t* turns) {
+  if (!turns || rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > 65536 || !(base > 1.0) || !std::isfinite(base)) return LUTGEMM_EINVAL;
+  if (scaling < LUTGEMM_ROPE_PLAIN || scaling > LUTGEMM_ROPE_PARTS) return LUTGEMM_EUNSUPPORTED;
+  if (scaling != LUTGEMM_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return LUTGEMM_EINVAL;
+  if (scaling == LUTGEMM_ROPE_PARTS && (!(low < high) || !(trained > 0.0) || !std::isfinite(low) || !std::isfinite(high) || !std::isfinite(trained)))
+    return LUTGEMM_EINVAL;
+  constexpr double kTwoPi = 6.283185307179586476925286766559;
+  if (scaling == LUTGEMM_ROPE_BASE && rot_dim > 2) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  if (!std::isfinite(base)) return LUTGEMM_EINVAL;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot_dim);
+    if (scaling == LUTGEMM_ROPE_LINEAR) f /= factor;
+    if (scaling == LUTGEMM_ROPE_PARTS) {
+      const double kept = std::min(1.0, std::max(0.0, (f * trained / kTwoPi - low) / (high - low)));
+      f = f * kept + f / factor * (1.0 - kept);
+    }
+    turns[i] = (uint64_t)std::nearbyint(std::ldexp(f / kTwoPi, 64));   // f <= 1: below 2^62
+  }
+  return LUTGEMM_OK;
+}
+
+}  // extern "C"

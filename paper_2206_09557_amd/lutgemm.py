@@ -20,6 +20,8 @@ LIB_PATH = os.environ.get("LUTGEMM_LIB") or os.path.join(_PKG, "liblutgemm.so")
 LUTGEMM_OK, LUTGEMM_EINVAL, LUTGEMM_EUNSUPPORTED, LUTGEMM_EWORKSPACE, LUTGEMM_EHIP = 0, -1, -2, -3, -4
 LUTGEMM_Q_GREEDY, LUTGEMM_Q_GREEDY_MEAN_OFFSET, LUTGEMM_Q_UNIFORM_RTN, LUTGEMM_Q_ALTERNATING = 0, 1, 2, 3
 LUTGEMM_Y_F16, LUTGEMM_Y_F32, LUTGEMM_ALPHA_SHARED, LUTGEMM_PATH_AUTO = 0, 1, 2, 4
+LUTGEMM_ROPE_NEIGHBOURS, LUTGEMM_ROPE_TRANSPOSE = 8, 16
+LUTGEMM_ROPE_PLAIN, LUTGEMM_ROPE_LINEAR, LUTGEMM_ROPE_BASE, LUTGEMM_ROPE_PARTS = 0, 1, 2, 3
 LUTGEMM_KERNEL_GEMV, LUTGEMM_KERNEL_PAIR, LUTGEMM_KERNEL_QUAD, LUTGEMM_KERNEL_FP4, LUTGEMM_KERNEL_FP16 = 1, 2, 4, 16, 32
 
 _c = ctypes
@@ -61,6 +63,18 @@ _SIGNATURES = {
                                      _c.c_void_p, _c.c_int]),
     "lutgemm_plan_group": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int, _c.c_int, _c.c_int, _c.c_void_p]),
     "lutgemm_stream_read": (_c.c_int, [_c.c_void_p, _c.c_size_t, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "lutgemm_rope_frequencies": (_c.c_int, [_c.c_int, _c.c_double, _c.c_int, _c.c_double, _c.c_double, _c.c_double,
+                                            _c.c_double, _c.c_void_p]),
+    "lutgemm_rope": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int, _c.c_int, _c.c_int,
+                                _c.c_int64, _c.c_int64, _c.c_float, _c.c_uint, _c.c_void_p]),
+    "lutgemm_kv_pool_bytes": (_c.c_size_t, [_c.c_int64, _c.c_int, _c.c_int, _c.c_int, _c.c_int, _c.c_int]),
+    "lutgemm_kv_write": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64,
+                                    _c.c_void_p]),
+    "lutgemm_kv_read": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64, _c.c_int64, _c.c_void_p]),
+    "lutgemm_attention": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int64,
+                                     _c.c_int64, _c.c_float, _c.c_int64, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "lutgemm_attention_workspace_bytes": (_c.c_size_t, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int64]),
+    "lutgemm_plan_attention": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int64, _c.c_void_p]),
     "lutgemm_strerror": (_c.c_char_p, [_c.c_int]),
 }
 EXPORTS = tuple(_SIGNATURES)
@@ -291,6 +305,81 @@ def lutgemm_gemm_dequant_mfma(x, bits, alpha, z, y, q, g, mu, m, n, batch, flags
     _check(lib().lutgemm_gemm_dequant_mfma(_addr(x), _addr(bits), _addr(alpha), _addr(z), _addr(y), q, g, mu, m, n,
                                            batch, flags, _addr(workspace), workspace_bytes, stream or None),
            "lutgemm_gemm_dequant_mfma")
+
+
+# ---- the attention half of a decode step ----------------------------------------------
+class lutgemm_kv_cache(ctypes.Structure):
+    """A cache's pool and shape, for the calls below; holds on to what it was given."""
+    _fields_ = [("pool", _c.c_void_p), ("pages", _c.c_int64), ("page_tokens", _c.c_int), ("heads", _c.c_int),
+                ("head_dim", _c.c_int), ("bits", _c.c_int), ("group", _c.c_int)]
+
+    def __init__(self, pool, pages, page_tokens, heads, head_dim, bits, group=0):
+        super().__init__(_addr(pool), pages, page_tokens, heads, head_dim, bits, group)
+        self._held = pool
+        self._address = ctypes.addressof(self)
+
+    def data_ptr(self):
+        return self._address
+
+
+class lutgemm_kv_step(ctypes.Structure):
+    """The new tokens of a step: see the header.  Holds on to what it was given."""
+    _fields_ = [("first", _c.c_void_p), ("past", _c.c_void_p), ("table", _c.c_void_p), ("seqs", _c.c_int),
+                ("table_pages", _c.c_int), ("tokens", _c.c_int), ("most_tokens", _c.c_int)]
+
+    def __init__(self, first, past, table, seqs, table_pages, tokens, most_tokens):
+        super().__init__(_addr(first), _addr(past), _addr(table), seqs, table_pages, tokens, most_tokens)
+        self._held = (first, past, table)
+        self._address = ctypes.addressof(self)
+
+    def data_ptr(self):
+        return self._address
+
+
+def lutgemm_rope_frequencies(rot_dim, base=10000.0, scaling=LUTGEMM_ROPE_PLAIN, factor=1.0, low=1.0, high=32.0, trained=0.0):
+    """numpy uint64 [rot_dim / 2]: fractions of a turn a position."""
+    turns = np.empty(max(int(rot_dim) // 2, 1), dtype=np.uint64)
+    _check(lib().lutgemm_rope_frequencies(rot_dim, base, scaling, factor, low, high, trained, turns.ctypes.data),
+           "lutgemm_rope_frequencies")
+    return turns
+
+
+def lutgemm_rope(x, y, positions, turns, tokens, heads, head_dim, rot_dim, x_stride, y_stride, amplitude, flags, stream=0):
+    _check(lib().lutgemm_rope(_addr(x), _addr(y), _addr(positions), _addr(turns), tokens, heads, head_dim, rot_dim, x_stride,
+                              y_stride, amplitude, flags, stream or None), "lutgemm_rope")
+
+
+def lutgemm_kv_pool_bytes(pages, page_tokens, heads, head_dim, bits, group=0):
+    return lib().lutgemm_kv_pool_bytes(pages, page_tokens, heads, head_dim, bits, group)
+
+
+def lutgemm_kv_write(k, v, rows, cache, step, k_stride, v_stride, stream=0):
+    _check(lib().lutgemm_kv_write(_addr(k), _addr(v), _addr(rows), _addr(cache), _addr(step), k_stride, v_stride,
+                                  stream or None), "lutgemm_kv_write")
+
+
+def lutgemm_kv_read(cache, step, k, v, k_stride, v_stride, stream=0):
+    _check(lib().lutgemm_kv_read(_addr(cache), _addr(step), _addr(k), _addr(v), k_stride, v_stride, stream or None),
+           "lutgemm_kv_read")
+
+
+def lutgemm_attention_workspace_bytes(cache, step, q_heads, most_positions=0):
+    return lib().lutgemm_attention_workspace_bytes(_addr(cache), _addr(step), q_heads, most_positions)
+
+
+def lutgemm_attention(q, mask, cache, step, y, q_heads, q_stride, y_stride, scale, most_positions, workspace, workspace_bytes,
+                      stream=0):
+    _check(lib().lutgemm_attention(_addr(q), _addr(mask), _addr(cache), _addr(step), _addr(y), q_heads, q_stride, y_stride,
+                                   scale, most_positions, _addr(workspace), workspace_bytes, stream or None),
+           "lutgemm_attention")
+
+
+def lutgemm_plan_attention(cache, step, q_heads, most_positions=0):
+    """(tiles of 16 rows a wavefront, row blocks, splits of the positions, positions a split, wavefronts a workgroup)"""
+    out = (ctypes.c_int * 5)()
+    _check(lib().lutgemm_plan_attention(_addr(cache), _addr(step), q_heads, most_positions, ctypes.addressof(out)),
+           "lutgemm_plan_attention")
+    return tuple(out)
 
 
 # The calls of a serving loop are bound by this marshalling where the layer is small: csrc/lutgemm_binding.cpp does it
