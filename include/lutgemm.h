@@ -487,7 +487,7 @@ int lutgemm_attention(const void* q, const uint64_t* mask, const lutgemm_kv_cach
 size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,
                                          int64_t most_positions);
 
-/* HOST.  How lutgemm_attention splits such a call: out[0] tiles of 16 rows (token, query head) that a wavefront holds, out[1]
+/* HOST.  How lutgemm_attention splits such a call: out[0] tiles of 16 rows (token, query head) of a workgroup, out[1]
    workgroups along the rows of a key head, out[2] along the positions, out[3] positions of each
    of these, out[4] wavefronts of a workgroup.                                            */
 int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,

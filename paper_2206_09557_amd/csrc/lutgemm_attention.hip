@@ -40,11 +40,12 @@ struct Params {
   int64_t q_stride, y_stride, pages;
   int tokens, most_tokens, table_pages, page_blocks, heads, shared;   // shared: query heads of a key head
   int block_bytes, splits, chunk, row_blocks, partial_rows;
-  float scale;                                           // of the scores, times log2 e
+  float scale;                                           // of the scores, times log2 e; not negative ...
+  uint32_t flip;                                         // ... the queries' signs are
 };
 
-typedef const void* (*Family)(int group_units, int row_tiles);
-#define DECLARE(k) const void* family##k(int group_units, int row_tiles);
+typedef const void* (*Family)(int group_units, int row_tiles, int waves);
+#define DECLARE(k) const void* family##k(int group_units, int row_tiles, int waves);
 DECLARE(0) DECLARE(1) DECLARE(2) DECLARE(3) DECLARE(4) DECLARE(5) DECLARE(6) DECLARE(7)
 DECLARE(8) DECLARE(9) DECLARE(10) DECLARE(11) DECLARE(12) DECLARE(13) DECLARE(14)
 #undef DECLARE
@@ -63,11 +64,27 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4;
 constexpr float kSlack = 8.0f;    // how far, in powers of two, a score may pass the kept maximum: weights up to 2^8 in fp16
 
-__device__ __forceinline__ void store_coherent(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float load_coherent(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Partial results cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
+// that are served from it (what a relaxed atomic of device scope is, but of 16 or 8 bytes).
+constexpr int kDeviceScope = 16;     // sc1
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(float* p, int64_t floats) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, 0, (int)(floats * 4), 0x00027000);
+}
+__device__ __forceinline__ void store4(Buffer b, int at, float4v v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), b, at * 4, 0, kDeviceScope);
+}
+__device__ __forceinline__ void store2(Buffer b, int at, float2v v) {
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), b, at * 4, 0, kDeviceScope);
+}
+__device__ __forceinline__ float4v load4(Buffer b, int at) {
+  return __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(b, at * 4, 0, kDeviceScope));
+}
+__device__ __forceinline__ float2v load2(Buffer b, int at) {
+  return __builtin_bit_cast(float2v, __builtin_amdgcn_raw_buffer_load_b64(b, at * 4, 0, kDeviceScope));
+}
 
 // The larger of a lane's value and those of the lanes 16, 32 and 48 away.
 __device__ __forceinline__ float max_of_column(float v) {
@@ -89,11 +106,16 @@ __device__ __forceinline__ half2v bytes_to_half(uint32_t w, uint32_t selector) {
   return __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, w, selector)) - both((_Float16)1152.0f);
 }
 // 4 bits: nibbles 0 and 4 (low), or 1 and 5 of a word, likewise; the latter count 16ths of 1024 + 16 u.
-__device__ __forceinline__ half2v low_nibbles(uint32_t w) {
-  return __builtin_bit_cast(half2v, (w & 0x000f000fu) | 0x64006400u) - both((_Float16)1024.0f);
+// (One and_or each: the instruction takes no literal, so the constants are made to live in registers.)
+__device__ __forceinline__ uint32_t nibbles(uint32_t w, uint32_t mask) {
+  uint32_t exponent = 0x64006400u;
+  asm("" : "+s"(mask));
+  asm("" : "+v"(exponent));
+  return (w & mask) | exponent;
 }
+__device__ __forceinline__ half2v low_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, nibbles(w, 0x000f000fu)) - both((_Float16)1024.0f); }
 __device__ __forceinline__ half2v high_nibbles(uint32_t w) {
-  return __builtin_elementwise_fma(__builtin_bit_cast(half2v, (w & 0x00f000f0u) | 0x64006400u), both((_Float16)0.0625f), both((_Float16)-64.0f));
+  return __builtin_elementwise_fma(__builtin_bit_cast(half2v, nibbles(w, 0x00f000f0u)), both((_Float16)0.0625f), both((_Float16)-64.0f));
 }
 
 // The raw words of a unit (32 places x 32 channels) as a lane holds them: two runs of eight values.
@@ -226,8 +248,9 @@ __device__ __forceinline__ half8v value_operand(const ValueWords<BITS, DC, GU>& 
 
 __device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// A walk over every kWaves-th block of a split: which page a block is in, without a division a block.  The table's entries are
+// A walk over every WAVES-th block of a split: which page a block is in, without a division a block.  The table's entries are
 // fetched 64 at a time, one a lane.
+template <int WAVES>
 struct Walk {
   const int32_t* table;        // of the sequence
   int64_t pages;
@@ -237,18 +260,21 @@ struct Walk {
   int base;                    // first table entry held
   int held;                    // this lane's
 };
-__device__ __forceinline__ void walk_fetch(Walk& w, int lane) {
+template <int WAVES>
+__device__ __forceinline__ void walk_fetch(Walk<WAVES>& w, int lane) {
   w.base = w.col;
   w.held = w.col + lane < w.table_pages ? w.table[w.col + lane] : -1;
 }
-__device__ __forceinline__ void walk_begin(Walk& w, int block, int lane) {
+template <int WAVES>
+__device__ __forceinline__ void walk_begin(Walk<WAVES>& w, int block, int lane) {
   w.col = block / w.page_blocks;
   w.in_page = block - w.col * w.page_blocks;
-  w.col_step = kWaves / w.page_blocks;
-  w.block_step = kWaves - w.col_step * w.page_blocks;
+  w.col_step = WAVES / w.page_blocks;
+  w.block_step = WAVES - w.col_step * w.page_blocks;
   walk_fetch(w, lane);
 }
-__device__ __forceinline__ void walk_on(Walk& w, int lane) {
+template <int WAVES>
+__device__ __forceinline__ void walk_on(Walk<WAVES>& w, int lane) {
   w.col += w.col_step;
   w.in_page += w.block_step;
   if (w.in_page >= w.page_blocks) {
@@ -258,84 +284,365 @@ __device__ __forceinline__ void walk_on(Walk& w, int lane) {
   if (w.col - w.base >= 64) walk_fetch(w, lane);
 }
 // Number of the page (-1: none).
-__device__ __forceinline__ int walk_page(const Walk& w) {
+template <int WAVES>
+__device__ __forceinline__ int walk_page(const Walk<WAVES>& w) {
   const int page = __builtin_amdgcn_readlane(w.held, w.col - w.base);
   return page >= 0 && page < w.pages ? page : -1;
 }
 
-// One workgroup: a split (blockIdx.x), a key head and row block (blockIdx.y), a sequence (blockIdx.z).
-// BITS of a code, DC units of 32 channels to a head, GU of them to a scale, RT tiles of 16 rows.
+// Factor of a part's sums where parts meet: its top is at most `raised`.  A part that saw nothing has none; a NaN stays one.
+__device__ __forceinline__ float part_factor(float top, float raised, float total) {
+  if (top == -__builtin_inff()) return total == total ? 0.0f : total;
+  return __builtin_amdgcn_exp2f(top - raised);
+}
+// Top and total of a row over the wavefronts.
+template <int WAVES, int ROWS>
+__device__ __forceinline__ float2v row_ends(const float* tops, const float* totals, int row) {
+  float raised = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) raised = fmaxf(raised, tops[w * ROWS + row]);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const float t = totals[w * ROWS + row];
+    sum += part_factor(tops[w * ROWS + row], raised, t) * t;
+  }
+  return (float2v){raised, sum};
+}
+// Four channels of a row's result (a row that saw nothing has a total of zero).
+__device__ __forceinline__ void store_row(const Params& p, int row_first, int head, int row, int dim, int d, float4v a, float total) {
+  const int token = row / p.shared;
+  const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+  *reinterpret_cast<half4v*>(p.y + (int64_t)(row_first + token) * p.y_stride + ((int64_t)head * p.shared + row - token * p.shared) * dim + d) =
+      __builtin_convertvector(a * inverse, half4v);
+}
+
+// What a wavefront carries from block to block.
+template <int DC, int RT>
+struct Sums {
+  half8v query[RT][DC];                // row `column` of a tile, channels 32 c + 8 quarter + (0..7)
+  float4v out[RT][2 * DC], total[RT];  // row `column`, channels 16 u + 4 quarter + (0..3)
+  float top[RT];                       // what the weights are relative to, in powers of two
+};
+
+// The scores' turn: S^T of a block's 32 positions.
 template <int BITS, int DC, int GU, int RT>
-__global__ __launch_bounds__(kWaves * 64) void lutgemm_attention_kernel(Params p) {
-  constexpr int kTiles = 2 * DC;            // of 16 channels
-  constexpr int kRows = 16 * RT;
-  // The wavefronts' sums meet kMeet units of channels at a time.
-  constexpr int kMeet = RT == 1 ? DC : (RT == 2 ? (DC % 2 == 0 ? 2 : 1) : 1);
-  __shared__ float sums[kWaves][kRows][kMeet * 32 + 4];
-  __shared__ float tops[kWaves][kRows], totals[kWaves][kRows];
-  __shared__ uint32_t last;
+__device__ __forceinline__ void block_scores(float4v (&score)[RT][2], const KeyWords<BITS, DC, GU>& keys, const Sums<DC, RT>& s) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int c = 0; c < DC; ++c) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const half8v k = key_operand<BITS, DC, GU>(keys, c, j);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) score[t][j] = mfma(k, s.query[t][c], score[t][j]);
+    }
+  }
+}
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int column = lane & 15, quarter = lane >> 4;
-  const int seq = blockIdx.z, head = blockIdx.y / p.row_blocks, row_block = blockIdx.y - head * p.row_blocks;
+// The weights' turn: of one tile's eight positions a lane, as the next product's operand.  MASKED: visible has a bit for each.
+template <int DC, int RT, bool MASKED>
+__device__ __forceinline__ half8v block_weights(const float4v (&score)[2], Sums<DC, RT>& s, int t, float scale, uint32_t visible, half8v ones) {
+  float most = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = score[i >> 2][i & 3];
+    most = fmaxf(most, !MASKED || (visible >> i & 1u) ? v : -__builtin_inff());
+  }
+  most *= scale;
+  if (__any(most > s.top[t] + kSlack)) {
+    most = max_of_column(most);
+    const float raised = most > s.top[t] + kSlack ? most : s.top[t];     // (a row's own need: others do not change its result)
+    const float shrink = raised == s.top[t] ? 1.0f : __builtin_amdgcn_exp2f(s.top[t] - raised);
+    s.top[t] = raised;
+    s.total[t] *= shrink;
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= shrink;
+  }
+  half2v w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float2v e;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], scale, -s.top[t]));
+      if (MASKED) e[k] = visible >> (2 * i + k) & 1u ? e[k] : 0.0f;
+    }
+    w[i] = __builtin_convertvector(e, half2v);
+  }
+  const half8v weight = join(w[0], w[1], w[2], w[3]);
+  s.total[t] = mfma(ones, weight, s.total[t]);
+  return weight;
+}
 
-  // What the step says of the sequence, within what the host said.
-  const int row_first = max(p.first[seq], 0);
-  const int count = min(min(p.first[seq + 1], p.tokens) - row_first, p.most_tokens);   // (at most kMostTokens)
-  const int rows = count * p.shared;         // of the key head
-  const int row0 = row_block * kRows;
-  if (count <= 0 || row0 >= rows) return;
-  const int past = max(p.past[seq], 0);
-  const int64_t capacity = (int64_t)p.table_pages * p.page_blocks * kBlock;
-  const int64_t length = min((int64_t)past + count, capacity);
+// What a workgroup has to do: a split (blockIdx.x) of the positions, a row block of a key head (blockIdx.y), a sequence (blockIdx.z).
+struct Place {
+  int seq, head, row_block;
+  int row_first;               // the sequence's first row of q and y
+  int rows, row0;              // (token, query head) pairs of the key head; the row block's first
+  int past;
+  int64_t length;              // positions that exist
+  int active;                  // splits that have any
+  int first_block, end_block;  // of this one
+};
+// From what the step says, within what the host said.  False: nothing to do.
+__device__ __forceinline__ bool find_place(const Params& p, int block_rows, Place* w) {
+  w->seq = blockIdx.z;
+  w->head = blockIdx.y / p.row_blocks;
+  w->row_block = blockIdx.y - w->head * p.row_blocks;
+  w->row_first = max(p.first[w->seq], 0);
+  const int count = min(min(p.first[w->seq + 1], p.tokens) - w->row_first, p.most_tokens);   // (at most kMostTokens)
+  w->past = max(p.past[w->seq], 0);
+  w->rows = count * p.shared;
+  w->row0 = w->row_block * block_rows;
+  if (count <= 0 || w->row0 >= w->rows) return false;
+  w->length = min((int64_t)w->past + count, (int64_t)p.table_pages * p.page_blocks * kBlock);
   int64_t chunk = p.chunk;
-  if (chunk * p.splits < length) chunk = ((length + p.splits - 1) / p.splits + kBlock - 1) / kBlock * kBlock;
-  const int active = max(1, (int)((length + chunk - 1) / chunk));
-  if ((int)blockIdx.x >= active) return;
-  const int first_block = (int)(blockIdx.x * chunk / kBlock);
-  const int end_block = (int)((min((blockIdx.x + 1) * chunk, length) + kBlock - 1) / kBlock);
+  if (chunk * p.splits < w->length) chunk = ((w->length + p.splits - 1) / p.splits + kBlock - 1) / kBlock * kBlock;
+  w->active = max(1, (int)((w->length + chunk - 1) / chunk));
+  if ((int)blockIdx.x >= w->active) return false;
+  w->first_block = (int)(blockIdx.x * chunk / kBlock);
+  w->end_block = (int)((min((blockIdx.x + 1) * chunk, w->length) + kBlock - 1) / kBlock);
+  return true;
+}
 
-  // Queries: lane holds row `column` of a tile, channels 32 c + 8 quarter + (0..7).
-  half8v query[RT][DC];
-  uint32_t mask_low[RT], mask_high[RT];
+template <int DC, int RT>
+__device__ __forceinline__ void clear_sums(Sums<DC, RT>& s) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int row = row0 + 16 * t + column;
-    const bool live = row < rows;
-    const int token = live ? row / p.shared : 0;
-    const _Float16* q = p.q + (int64_t)(row_first + token) * p.q_stride + ((int64_t)head * p.shared + (live ? row - token * p.shared : 0)) * (DC * 32);
+    s.top[t] = -__builtin_inff();
+    s.total[t] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) s.out[t][u] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+}
+// Queries of the rows from `row` on, and which new positions their tokens see.
+template <int DC, int RT>
+__device__ __forceinline__ void load_queries(const Params& p, const Place& w, int row, int lane, Sums<DC, RT>& s, uint64_t (&sees)[RT]) {
+  const int column = lane & 15, quarter = lane >> 4;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int r = row + 16 * t + column;
+    const bool live = r < w.rows;
+    const int token = live ? r / p.shared : 0;
+    const _Float16* q = p.q + (int64_t)(w.row_first + token) * p.q_stride + ((int64_t)w.head * p.shared + (live ? r - token * p.shared : 0)) * (DC * 32);
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
-      const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
-      query[t][c] = live ? *reinterpret_cast<const half8v*>(q + 32 * c + 8 * quarter) : none;
+      u32x4 v = {0u, 0u, 0u, 0u};
+      if (live) v = *reinterpret_cast<const u32x4*>(q + 32 * c + 8 * quarter) ^ p.flip;     // (a negative scale's sign)
+      s.query[t][c] = __builtin_bit_cast(half8v, v);
     }
-    const uint64_t sees = !live ? 0 : (p.mask ? p.mask[row_first + token] : ~0ull >> (63 - token));
-    mask_low[t] = (uint32_t)sees;
-    mask_high[t] = (uint32_t)(sees >> 32);
+    sees[t] = !live ? 0 : (p.mask ? p.mask[w.row_first + token] : ~0ull >> (63 - token));
   }
+}
+// Which of a lane's eight positions of a block a tile's row sees: bit 4 j + i for position 8 quarter + 4 j + i.
+__device__ __forceinline__ uint32_t visible_places(int place, int limit, uint64_t sees) {
+  uint32_t visible = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int n = place + i;
+    visible |= n < limit && (n < 0 || (sees >> (n & 63) & 1u) != 0) ? 1u << i : 0u;
+  }
+  return visible;
+}
+// Adds a tile of 16 channels of a block that not every row sees all of.  A weight of zero must not meet an infinity or a NaN: what
+// is not finite is taken out of the operand, and counted for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there
+// are at most 32 of each).
+template <int DC, int RT>
+__device__ __forceinline__ void add_masked(half8v v, int place, int limit, const half8v (&weight)[RT], const uint32_t (&visible)[RT], Sums<DC, RT>& s, int u) {
+  half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t bits = bits_of(v[i]);
+    const bool exists = place + i < limit, infinite = (bits & 0x7c00u) == 0x7c00u;
+    if (infinite && exists) odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
+    any |= infinite && exists;
+    if (infinite || !exists) v[i] = (_Float16)0;
+  }
+  if (__any(any)) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      half8v seen;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) seen[i] = visible[t] >> i & 1u ? (_Float16)1.0f : (_Float16)0;
+      const float4v n = mfma(odd, seen, (float4v){0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int found = (int)n[i];
+        const bool plus = (found & 63) != 0, minus = (found >> 6 & 63) != 0, nan = found >= 4096 || (plus && minus);
+        s.out[t][u][i] += nan ? __builtin_nanf("") : (plus ? __builtin_inff() : (minus ? -__builtin_inff() : 0.0f));
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
+}
 
-  float4v out[RT][kTiles], total[RT];
-  float top[RT];
+// The end of a workgroup, of GROUPS_R x PARTS wavefronts: PARTS that took different positions for the same RT tiles of rows, GROUPS_R
+// that took different rows.  The parts' sums meet in LDS in their order, then the splits' through memory.
+template <int DC, int RT, int GROUPS_R, int PARTS>
+struct Ending {
+  static constexpr int kRows = 16 * RT * GROUPS_R, kThreads = 64 * GROUPS_R * PARTS, kDim = DC * 32;
+  // Units of channels that meet at a time: what 40 KB hold, or 72 KB where a workgroup has the compute unit to itself.
+  static constexpr int kFit = (PARTS * kRows <= 64 ? 40960 : 73728) / (PARTS * kRows * 128 + PARTS * kRows * 24);
+  static constexpr int kMeet = kFit >= DC ? DC : (kFit >= 4 && DC % 4 == 0 ? 4 : (kFit >= 3 && DC % 3 == 0 ? 3 : (kFit >= 2 && DC % 2 == 0 ? 2 : 1)));
+  static constexpr int kPitch = kMeet * 32 + 4;
+  static constexpr int kMeetFloats = PARTS * kRows * (kPitch + 2);
+  static constexpr int kJoinFloats = 2 * kMostSplitRows + kRows + kThreads * 4;
+  static constexpr int kFloats = kMeetFloats > kJoinFloats ? kMeetFloats : kJoinFloats;
+};
+template <int DC, int RT, int GROUPS_R, int PARTS>
+__device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, float* lds, uint32_t* last, Sums<DC, RT>& s, int group, int part, int lane) {
+  using E = Ending<DC, RT, GROUPS_R, PARTS>;
+  constexpr int kRows = E::kRows, kThreads = E::kThreads, kDim = E::kDim, kMeet = E::kMeet, kPitch = E::kPitch;
+  const int column = lane & 15, quarter = lane >> 4;
+  float* sums = lds;                            // [PARTS][kRows][kPitch]
+  float* tops = lds + PARTS * kRows * kPitch;   // [PARTS][kRows]
+  float* totals = tops + PARTS * kRows;
+  const int live_rows = min(w.rows - w.row0, kRows), mine0 = 16 * RT * group + column;   // (the lane's first row)
+  if (quarter == 0) {
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    top[t] = -__builtin_inff();
-    total[t] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int u = 0; u < kTiles; ++u) out[t][u] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < RT; ++t) {
+      tops[part * kRows + mine0 + 16 * t] = s.top[t];
+      totals[part * kRows + mine0 + 16 * t] = s.total[t][0];
+    }
   }
+  __syncthreads();
+  if constexpr (PARTS > 1) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      float raised = -__builtin_inff();
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) raised = fmaxf(raised, tops[k * kRows + mine0 + 16 * t]);
+      const float factor = part_factor(s.top[t], raised, s.total[t][0]);
+#pragma unroll
+      for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= factor;
+    }
+  }
+  const int unit = (w.seq * p.heads + w.head) * p.row_blocks + w.row_block;
+  const int64_t split_floats = (int64_t)p.partial_rows * (kDim + 2);     // a split's sums, then a top and a total for each row
+  float* unit_partial = p.partial + unit * p.splits * split_floats;
+  const Buffer mine = buffer_of(unit_partial + blockIdx.x * split_floats, split_floats);
+#pragma unroll
+  for (int m = 0; m < DC / kMeet; ++m) {
+    if (m > 0) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+      if (mine0 + 16 * t < live_rows) {
+#pragma unroll
+        for (int u = 0; u < 2 * kMeet; ++u)
+          *reinterpret_cast<float4v*>(&sums[(part * kRows + mine0 + 16 * t) * kPitch + 16 * u + 4 * quarter]) = s.out[t][2 * kMeet * m + u];
+      }
+    __syncthreads();
+    constexpr int kFours = kMeet * 8;           // a thread takes four channels
+    for (int i = threadIdx.x; i < live_rows * kFours; i += kThreads) {
+      const int row = i / kFours, d = i % kFours * 4;
+      float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) a += *reinterpret_cast<const float4v*>(&sums[(k * kRows + row) * kPitch + d]);
+      if (w.active > 1)
+        store4(mine, row * kDim + m * kMeet * 32 + d, a);
+      else
+        store_row(p, w.row_first, w.head, w.row0 + row, kDim, m * kMeet * 32 + d, a, row_ends<PARTS, kRows>(tops, totals, row)[1]);
+    }
+  }
+  if (w.active == 1) return;
+  for (int row = threadIdx.x; row < live_rows; row += kThreads) store2(mine, p.partial_rows * kDim + 2 * row, row_ends<PARTS, kRows>(tops, totals, row));
+
+  // The last workgroup to arrive adds the splits.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    *last = __hip_atomic_fetch_add(p.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w.active - 1) ? 1u : 0u;
+  __syncthreads();
+  if (*last == 0u) return;
+  const Buffer all = buffer_of(unit_partial, p.splits * split_floats);
+  float* split_top = lds;                       // [live_rows][active], then the splits' factors
+  float* split_total = lds + kMostSplitRows;
+  float* row_total = lds + 2 * kMostSplitRows;  // [kRows]
+  float* shares = row_total + kRows;            // [kThreads][4]
+  for (int i = threadIdx.x; i < live_rows * w.active; i += kThreads) {
+    const int split = i / live_rows, row = i - split * live_rows;
+    const float2v end = load2(all, (int)(split * split_floats) + p.partial_rows * kDim + 2 * row);
+    split_top[row * w.active + split] = end[0];
+    split_total[row * w.active + split] = end[1];
+  }
+  __syncthreads();
+  for (int row = threadIdx.x >> 4; row < live_rows; row += kThreads / 16) {      // sixteen lanes a row
+    float raised = -__builtin_inff(), sum = 0.0f;
+    for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, split_top[row * w.active + i]);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, 16));
+    for (int i = column; i < w.active; i += 16) {
+      const float total = split_total[row * w.active + i], factor = part_factor(split_top[row * w.active + i], raised, total);
+      split_top[row * w.active + i] = factor;
+      sum += factor * total;
+    }
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 16);
+    if (column == 0) row_total[row] = sum;
+  }
+  __syncthreads();
+  // An item is four channels of a row; where there are fewer items than threads, several threads share one's splits.
+  constexpr int kFours = kDim / 4;
+  const int items = live_rows * kFours;
+  int sharers = 1;
+  while (sharers < 16 && 2 * sharers * items <= kThreads && 2 * sharers <= w.active) sharers *= 2;
+  const int side = kThreads / sharers, share = threadIdx.x / side;
+  for (int base = 0; base < items; base += side) {
+    const int i = base + threadIdx.x - share * side;
+    const int row = i / kFours, d = i % kFours * 4;
+    const bool item = i < items && share < sharers;
+    float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (item) {
+      const int at = row * kDim + d;
+      int split = share;
+      for (; split + 7 * sharers < w.active; split += 8 * sharers) {
+        float4v v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = load4(all, (int)((split + k * sharers) * split_floats) + at);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) a += v[k] * split_top[row * w.active + split + k * sharers];
+      }
+      for (; split < w.active; split += sharers) a += load4(all, (int)(split * split_floats) + at) * split_top[row * w.active + split];
+    }
+    if (sharers > 1) {
+      __syncthreads();
+      *reinterpret_cast<float4v*>(&shares[threadIdx.x * 4]) = a;
+      __syncthreads();
+      if (item && share == 0)
+        for (int k = 1; k < sharers; ++k) a += *reinterpret_cast<const float4v*>(&shares[(threadIdx.x + k * side) * 4]);
+    }
+    if (item && share == 0) store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_total[row]);
+  }
+  if (threadIdx.x == 0) __hip_atomic_store(p.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Few rows: every wavefront takes all of them, and blocks of its own, from memory straight into registers.
+// BITS of a code, DC units of 32 channels to a head, GU of them to a scale, RT tiles of 16 rows.
+template <int BITS, int DC, int GU, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, RT)) void lutgemm_attention_kernel(Params p) {
+  __shared__ __attribute__((aligned(16))) float lds[Ending<DC, RT, 1, WAVES>::kFloats];
+  __shared__ uint32_t last;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+  Place w;
+  if (!find_place(p, 16 * RT, &w)) return;
+
+  Sums<DC, RT> s;
+  clear_sums(s);
   const half2v one = both((_Float16)1.0f);
   const half8v ones = join(one, one, one, one);
-
-  int block = first_block + wave;
-  if (block < end_block) {
-    Walk walk;
-    walk.table = p.table + (int64_t)seq * p.table_pages;
+  int block = w.first_block + wave;
+  if (block < w.end_block) {
+    Walk<WAVES> walk;
+    walk.table = p.table + (int64_t)w.seq * p.table_pages;
     walk.pages = p.pages;
     walk.table_pages = p.table_pages;
     walk.page_blocks = p.page_blocks;
     walk_begin(walk, block, lane);
     const int64_t page_bytes = (int64_t)p.heads * p.page_blocks * p.block_bytes;
-    const char* head_base = p.pool + (int64_t)head * p.page_blocks * p.block_bytes;
+    const char* head_base = p.pool + (int64_t)w.head * p.page_blocks * p.block_bytes;
     const int value_offset = p.block_bytes / 2;
 
     int page = walk_page(walk);
@@ -344,9 +651,186 @@ __global__ __launch_bounds__(kWaves * 64) void lutgemm_attention_kernel(Params p
     ValueWords<BITS, DC, GU> values;
     load_keys<BITS, DC, GU>(keys, at, lane);
     load_values<BITS, DC, GU>(values, at + value_offset, lane);
+    uint64_t sees[RT];
+    load_queries<DC, RT>(p, w, w.row0, lane, s, sees);
 
-    while (true) {
-      // ---- scores
+    // Blocks that every row sees all of: the past but for its last few positions.  A block's keys are asked for when the one before
+    // has met the queries, its values when that one's have been added.
+    const int whole_end = w.past / kBlock;
+    while (block < whole_end) {
+      float4v score[RT][2];
+      block_scores<BITS, DC, GU, RT>(score, keys, s);
+      const int next = block + WAVES;
+      const bool dead = page < 0;
+      if (next < w.end_block) {
+        walk_on(walk, lane);
+        page = walk_page(walk);
+        at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
+        load_keys<BITS, DC, GU>(keys, at, lane);
+      }
+      if (!dead) {
+        half8v weight[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) weight[t] = block_weights<DC, RT, false>(score[t], s, t, p.scale, 0u, ones);
+#pragma unroll
+        for (int c = 0; c < DC; ++c) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const half8v v = value_operand<BITS, DC, GU>(values, c, j);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) s.out[t][2 * c + j] = mfma(v, weight[t], s.out[t][2 * c + j]);
+          }
+        }
+      }
+      block = next;
+      if (block >= w.end_block) break;
+      load_values<BITS, DC, GU>(values, at + value_offset, lane);
+    }
+
+    // The others: the last positions of the past, the new ones, and what is behind them in the last block.
+    while (block < w.end_block) {
+      float4v score[RT][2];
+      block_scores<BITS, DC, GU, RT>(score, keys, s);
+      const int next = block + WAVES;
+      const int place = block * kBlock + 8 * quarter - w.past;              // of the lane's first position, counted from the new ones
+      const int limit = page < 0 ? -(1 << 30) : (int)(w.length - w.past);   // positions from here on do not exist
+      if (next < w.end_block) {
+        walk_on(walk, lane);
+        page = walk_page(walk);
+        at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
+        load_keys<BITS, DC, GU>(keys, at, lane);
+      }
+      half8v weight[RT];
+      uint32_t visible[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        visible[t] = visible_places(place, limit, sees[t]);
+        weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
+      }
+#pragma unroll
+      for (int c = 0; c < DC; ++c) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) add_masked<DC, RT>(value_operand<BITS, DC, GU>(values, c, j), place, limit, weight, visible, s, 2 * c + j);
+      }
+      block = next;
+      if (block >= w.end_block) break;
+      load_values<BITS, DC, GU>(values, at + value_offset, lane);
+    }
+  }
+  end_workgroup<DC, RT, 1, WAVES>(p, w, lds, &last, s, 0, wave, lane);
+}
+
+// Many rows: GROUPS_R wavefronts share a block, RT tiles of rows each, so that its codes are fetched and made fp16 once for all of them:
+// each does its share of the block's 2 DC units (keys, values) and puts the operands into LDS, in the order
+// in which the lanes want them back (16 bytes each, no bank conflicts).  The next block's codes are in registers meanwhile, its
+// operands go to the other half of the LDS; one barrier a block.  Where there are fewer rows than
+// eight wavefronts hold, PARTS sets of GROUPS_R take blocks in turn.
+template <int BITS, int DC, int GU, int RT, int GROUPS_R, int PARTS>
+__global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_shared_kernel(Params p) {
+  constexpr int kEach = (2 * DC + GROUPS_R - 1) / GROUPS_R;        // units of a wavefront
+  constexpr int kOperands = 2 * DC * 2 * 1024;                     // bytes of a block's: units x runs
+  using E = Ending<DC, RT, GROUPS_R, PARTS>;
+  constexpr int kBytes = 2 * PARTS * kOperands > E::kFloats * 4 ? 2 * PARTS * kOperands : E::kFloats * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kBytes];
+  __shared__ uint32_t last;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+  const int group = wave % GROUPS_R, part = wave / GROUPS_R;
+  Place w;
+  if (!find_place(p, 16 * RT * GROUPS_R, &w)) return;
+
+  Sums<DC, RT> s;
+  clear_sums(s);
+  const half2v one = both((_Float16)1.0f);
+  const half8v ones = join(one, one, one, one);
+  Walk<PARTS> walk;
+  walk.table = p.table + (int64_t)w.seq * p.table_pages;
+  walk.pages = p.pages;
+  walk.table_pages = p.table_pages;
+  walk.page_blocks = p.page_blocks;
+  walk_begin(walk, w.first_block + part, lane);
+  const int64_t page_bytes = (int64_t)p.heads * p.page_blocks * p.block_bytes;
+  const char* head_base = p.pool + (int64_t)w.head * p.page_blocks * p.block_bytes;
+
+  constexpr int kCode = kBlock * DC * 32 * BITS / 8;
+  Unit<BITS> unit[kEach];
+  half8v scale[kEach], offset[BITS == 4 ? kEach : 1];              // of a value unit; of a key unit in the first words
+  int page;
+  auto fetch = [&]() {                                             // this wavefront's units of the block that `walk` is at
+    page = walk_page(walk);
+    const char* at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int u = group + i * GROUPS_R;
+      if (u >= 2 * DC) continue;
+      const int c = u < DC ? u : u - DC, g = c / GU;
+      const char* half_block = at + (u < DC ? 0 : p.block_bytes / 2);
+      load_unit<BITS>(unit[i], half_block, c, lane);
+      if constexpr (BITS == 8) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (u < DC)
+          v[0] = reinterpret_cast<const uint32_t*>(half_block + kCode + g * 64)[lane & 15];
+        else
+          v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 64)[lane >> 4];
+        scale[i] = __builtin_bit_cast(half8v, v);
+      }
+      if constexpr (BITS == 4) {
+        u32x4 v = {0u, 0u, 0u, 0u}, z = v;
+        if (u < DC) {
+          const u32x2 k = reinterpret_cast<const u32x2*>(half_block + kCode + g * 128)[lane & 15];
+          v[0] = k[0];
+          v[1] = k[1];
+        } else {
+          v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128)[lane >> 4];
+          z = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128 + 64)[lane >> 4];
+        }
+        scale[i] = __builtin_bit_cast(half8v, v);
+        offset[i] = __builtin_bit_cast(half8v, z);
+      }
+    }
+  };
+  auto operands = [&](int half) { return lds + (half * PARTS + part) * kOperands; };
+  auto put = [&](int half) {                                       // the fetched units, as operands
+    u32x4* to = reinterpret_cast<u32x4*>(operands(half)) + lane;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int u = group + i * GROUPS_R;
+      if (u >= 2 * DC) continue;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        half8v v;
+        if (BITS == 16 || u >= DC)
+          v = value_values<BITS>(unit[i], j, scale[i], offset[BITS == 4 ? i : 0]);
+        else if (BITS == 8)
+          v = key_values<BITS>(unit[i], j, scale[i][j], (_Float16)0);
+        else
+          v = key_values<BITS>(unit[i], j, scale[i][2 * j], scale[i][2 * j + 1]);
+        to[(u * 2 + j) * 64] = __builtin_bit_cast(u32x4, v);
+      }
+    }
+  };
+
+  int block = w.first_block + part;                                // this part's
+  const int stages = (w.end_block - w.first_block + PARTS - 1) / PARTS;
+  if (block < w.end_block) fetch();
+  uint64_t sees[RT];
+  load_queries<DC, RT>(p, w, w.row0 + 16 * RT * group, lane, s, sees);
+  bool dead = false, next_dead = false;
+  if (block < w.end_block) {
+    put(0);
+    dead = page < 0;
+  }
+  const int whole_end = w.past / kBlock;
+  const bool idle = w.row0 + 16 * RT * group >= w.rows;            // no row of this wavefront's lives: it only helps with the operands
+  for (int stage = 0; stage < stages; ++stage) {
+    const int next = block + PARTS;
+    if (next < w.end_block) {
+      walk_on(walk, lane);
+      fetch();
+      next_dead = page < 0;
+    }
+    __syncthreads();
+    if (block < w.end_block && !idle) {
+      const half8v* from = reinterpret_cast<const half8v*>(operands(stage & 1)) + lane;
       float4v score[RT][2];
 #pragma unroll
       for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
@@ -354,239 +838,73 @@ __global__ __launch_bounds__(kWaves * 64) void lutgemm_attention_kernel(Params p
       for (int c = 0; c < DC; ++c) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const half8v k = key_operand<BITS, DC, GU>(keys, c, j);
+          const half8v k = from[(c * 2 + j) * 64];
 #pragma unroll
-          for (int t = 0; t < RT; ++t) score[t][j] = mfma(k, query[t][c], score[t][j]);
+          for (int t = 0; t < RT; ++t) score[t][j] = mfma(k, s.query[t][c], score[t][j]);
         }
       }
-      const int next = block + kWaves;
-      const bool more = next < end_block;
-      const bool dead = page < 0;
-      const char* following = at;
-      if (more) {
-        walk_on(walk, lane);
-        page = walk_page(walk);
-        following = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
-        load_keys<BITS, DC, GU>(keys, following, lane);
-      }
-
-      // ---- weights.  A lane has positions 32 block + 8 quarter + 4 j + i of its rows.
-      const bool whole = (int64_t)(block + 1) * kBlock <= past && !dead;       // every row sees all of the block
       half8v weight[RT];
-      uint32_t visible[RT];                    // bit 4 j + i
-      const int place = block * kBlock + 8 * quarter - past;     // of the lane's first position, counted from the new ones
-      const int limit = dead ? -(1 << 30) : (int)(length - past);   // positions from here on do not exist
+      if (block < whole_end) {
+        if (!dead) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        float s[8];
+          for (int t = 0; t < RT; ++t) weight[t] = block_weights<DC, RT, false>(score[t], s, t, p.scale, 0u, ones);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = score[t][i >> 2][i & 3] * p.scale;
-        visible[t] = 0xffu;
-        if (!whole) {
-          visible[t] = 0u;
-          const uint64_t sees = (uint64_t)mask_high[t] << 32 | mask_low[t];
+          for (int u = 0; u < 2 * DC; ++u) {
+            const half8v v = from[(2 * DC + u) * 64];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int n = place + i;
-            const bool v = n < limit && (n < 0 || ((sees >> (n & 63)) & 1u) != 0);
-            visible[t] |= v ? 1u << i : 0u;
+            for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
           }
         }
-        float most = -__builtin_inff();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, whole || (visible[t] >> i & 1u) ? s[i] : -__builtin_inff());
-        if (__any(most > top[t] + kSlack)) {
-          most = max_of_column(most);
-          const float raised = most > top[t] + kSlack ? most : top[t];     // (a row's own need: others do not change its result)
-          const float shrink = raised == top[t] ? 1.0f : __builtin_amdgcn_exp2f(top[t] - raised);
-          top[t] = raised;
-          total[t] *= shrink;
-#pragma unroll
-          for (int u = 0; u < kTiles; ++u) out[t][u] *= shrink;
-        }
-        half2v w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float2v e = {__builtin_amdgcn_exp2f(s[2 * i] - top[t]), __builtin_amdgcn_exp2f(s[2 * i + 1] - top[t])};
-          if (!whole) {
-            e[0] = visible[t] >> (2 * i) & 1u ? e[0] : 0.0f;
-            e[1] = visible[t] >> (2 * i + 1) & 1u ? e[1] : 0.0f;
-          }
-          w[i] = __builtin_convertvector(e, half2v);
-        }
-        weight[t] = join(w[0], w[1], w[2], w[3]);
-        total[t] = mfma(ones, weight[t], total[t]);
-      }
-
-      // ---- weighted values
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          half8v v = value_operand<BITS, DC, GU>(values, c, j);
-          if (!whole) {
-            // A weight of zero must not meet an infinity or a NaN: what is not finite is taken out of the operand, and
-            // counted for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there are at most 32 of each).
-            half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
-            bool any = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t bits = bits_of(v[i]);
-              const bool exists = place + i < limit, infinite = (bits & 0x7c00u) == 0x7c00u;
-              if (infinite && exists) odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
-              any |= infinite && exists;
-              if (infinite || !exists) v[i] = (_Float16)0;
-            }
-            if (__any(any)) {
-#pragma unroll
-              for (int t = 0; t < RT; ++t) {
-                half8v seen;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) seen[i] = visible[t] >> i & 1u ? (_Float16)1.0f : (_Float16)0;
-                const float4v n = mfma(odd, seen, (float4v){0.0f, 0.0f, 0.0f, 0.0f});
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const int found = (int)n[i];
-                  const bool plus = (found & 63) != 0, minus = (found >> 6 & 63) != 0, nan = found >= 4096 || (plus && minus);
-                  out[t][2 * c + j][i] += nan ? __builtin_nanf("") : (plus ? __builtin_inff() : (minus ? -__builtin_inff() : 0.0f));
-                }
-              }
-            }
-          }
-#pragma unroll
-          for (int t = 0; t < RT; ++t) out[t][2 * c + j] = mfma(v, weight[t], out[t][2 * c + j]);
-        }
-      }
-      if (!more) break;
-      block = next;
-      at = following;
-      load_values<BITS, DC, GU>(values, at + value_offset, lane);
-    }
-  }
-
-  // ---- the wavefronts' sums meet.  out[t][u][i]: row 16 t + column, channel 16 u + 4 quarter + i.
-  if (quarter == 0) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      tops[wave][16 * t + column] = top[t];
-      totals[wave][16 * t + column] = total[t][0];
-    }
-  }
-  __syncthreads();
-  const int live_rows = min(rows - row0, kRows);
-  float factor[RT];                            // of this wavefront's sums
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    float raised = -__builtin_inff();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) raised = fmaxf(raised, tops[w][16 * t + column]);
-    factor[t] = top[t] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top[t] - raised);
-    if (factor[t] == 0.0f && !(total[t][0] == total[t][0])) factor[t] = total[t][0];     // a NaN stays one
-  }
-  const int unit = (seq * p.heads + head) * p.row_blocks + row_block;
-  float* partial = p.partial + ((int64_t)unit * p.splits + blockIdx.x) * p.partial_rows * (DC * 32 + 2);
-#pragma unroll
-  for (int m = 0; m < DC / kMeet; ++m) {
-    if (m > 0) __syncthreads();
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int u = 0; u < 2 * kMeet; ++u) {
-        const float4v o = out[t][2 * kMeet * m + u] * factor[t];
-        *reinterpret_cast<float4v*>(&sums[wave][16 * t + column][16 * u + 4 * quarter]) = o;
-      }
-    __syncthreads();
-    // a thread takes two channels
-    constexpr int kPairs = kMeet * 16;
-    for (int i = threadIdx.x; i < live_rows * kPairs; i += kWaves * 64) {
-      const int row = i / kPairs, d = i % kPairs * 2;
-      float a = 0.0f, b = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        a += sums[w][row][d];
-        b += sums[w][row][d + 1];
-      }
-      if (active > 1) {
-        store_coherent(partial + row * (DC * 32) + m * kMeet * 32 + d, a);
-        store_coherent(partial + row * (DC * 32) + m * kMeet * 32 + d + 1, b);
       } else {
-        float raised = -__builtin_inff(), sum = 0.0f;
+        const int place = block * kBlock + 8 * quarter - w.past, limit = dead ? -(1 << 30) : (int)(w.length - w.past);
+        uint32_t visible[RT];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) raised = fmaxf(raised, tops[w][row]);
+        for (int t = 0; t < RT; ++t) {
+          visible[t] = visible_places(place, limit, sees[t]);
+          weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
+        }
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) sum += tops[w][row] == -__builtin_inff() ? totals[w][row] : __builtin_amdgcn_exp2f(tops[w][row] - raised) * totals[w][row];
-        const int r = row0 + row, token = r / p.shared;
-        const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const half2v y = __builtin_convertvector((float2v){a * inverse, b * inverse}, half2v);
-        *reinterpret_cast<half2v*>(p.y + (int64_t)(row_first + token) * p.y_stride + ((int64_t)head * p.shared + r - token * p.shared) * (DC * 32) +
-                                   m * kMeet * 32 + d) = y;
+        for (int u = 0; u < 2 * DC; ++u) add_masked<DC, RT>(from[(2 * DC + u) * 64], place, limit, weight, visible, s, u);
       }
     }
+    if (next < w.end_block) put((stage + 1) & 1);
+    block = next;
+    dead = next_dead;
   }
-  if (active == 1) return;
-
-  // ---- the splits' sums meet: the last workgroup to arrive adds them in order
-  float* ends = partial + p.partial_rows * (DC * 32);
-  for (int row = threadIdx.x; row < live_rows; row += kWaves * 64) {
-    float raised = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) raised = fmaxf(raised, tops[w][row]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += tops[w][row] == -__builtin_inff() ? totals[w][row] : __builtin_amdgcn_exp2f(tops[w][row] - raised) * totals[w][row];
-    store_coherent(ends + 2 * row, raised);
-    store_coherent(ends + 2 * row + 1, sum);
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(p.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(active - 1) ? 1u : 0u;
-  __syncthreads();
-  if (last == 0u) return;
-  const float* all = p.partial + (int64_t)unit * p.splits * p.partial_rows * (DC * 32 + 2);
-  const int64_t stride = (int64_t)p.partial_rows * (DC * 32 + 2);
-  for (int i = threadIdx.x; i < live_rows * DC * 16; i += kWaves * 64) {
-    const int row = i / (DC * 16), d = i % (DC * 16) * 2;
-    float raised = -__builtin_inff();
-    for (int s = 0; s < active; ++s) raised = fmaxf(raised, load_coherent(all + s * stride + p.partial_rows * (DC * 32) + 2 * row));
-    float a = 0.0f, b = 0.0f, sum = 0.0f;
-    for (int s = 0; s < active; ++s) {
-      const float* one_split = all + s * stride;
-      const float t = load_coherent(one_split + p.partial_rows * (DC * 32) + 2 * row);
-      const float n = load_coherent(one_split + p.partial_rows * (DC * 32) + 2 * row + 1);
-      const float f = t == -__builtin_inff() ? (n == n ? 0.0f : n) : __builtin_amdgcn_exp2f(t - raised);
-      a += f * load_coherent(one_split + row * (DC * 32) + d);
-      b += f * load_coherent(one_split + row * (DC * 32) + d + 1);
-      sum += f * n;
-    }
-    const int r = row0 + row, token = r / p.shared;
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const half2v y = __builtin_convertvector((float2v){a * inverse, b * inverse}, half2v);
-    *reinterpret_cast<half2v*>(p.y + (int64_t)(row_first + token) * p.y_stride + ((int64_t)head * p.shared + r - token * p.shared) * (DC * 32) + d) = y;
-  }
-  if (threadIdx.x == 0) __hip_atomic_store(p.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  end_workgroup<DC, RT, GROUPS_R, PARTS>(p, w, reinterpret_cast<float*>(lds), &last, s, group, part, lane);
 }
 
 template <int BITS, int DC, int GU>
-const void* pick_tiles(int row_tiles) {
-  if (row_tiles == 1) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 1>);
-  if (row_tiles == 2) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 2>);
+const void* pick_tiles(int row_tiles, int waves) {
+  constexpr int kAll = 4 * attention_waves_per_simd(DC * 32, 1);
+  if (row_tiles == 1 && waves == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 1, 4>);
+  if (row_tiles == 1 && waves == kAll) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 1, kAll>);
+  if (row_tiles == 2 && waves == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 2, 4>);
+  if (waves != 8) return nullptr;
   if constexpr (DC <= 4) {
-    if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 4>);
+    if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 2, 4>);
+    if (row_tiles == 8) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 4, 2>);
+    if (row_tiles == 16) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 8, 1>);
+  } else {
+    if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 1, 4, 2>);
+    if (row_tiles == 8) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 1, 8, 1>);
   }
   return nullptr;
 }
 template <int BITS, int DC>
-const void* pick_group(int units, int row_tiles) {
-  if (BITS == 16 || units == DC) return pick_tiles<BITS, DC, DC>(row_tiles);
+const void* pick_group(int units, int row_tiles, int waves) {
+  if (BITS == 16 || units == DC) return pick_tiles<BITS, DC, DC>(row_tiles, waves);
   if constexpr (BITS != 16) {
-    if (units == 1) return pick_tiles<BITS, DC, 1>(row_tiles);
+    if (units == 1) return pick_tiles<BITS, DC, 1>(row_tiles, waves);
     if constexpr (DC % 2 == 0 && DC > 2) {
-      if (units == 2) return pick_tiles<BITS, DC, 2>(row_tiles);
+      if (units == 2) return pick_tiles<BITS, DC, 2>(row_tiles, waves);
     }
     if constexpr (DC == 6) {
-      if (units == 3) return pick_tiles<BITS, DC, 3>(row_tiles);
+      if (units == 3) return pick_tiles<BITS, DC, 3>(row_tiles, waves);
     }
     if constexpr (DC == 8) {
-      if (units == 4) return pick_tiles<BITS, DC, 4>(row_tiles);
+      if (units == 4) return pick_tiles<BITS, DC, 4>(row_tiles, waves);
     }
   }
   return nullptr;
@@ -597,10 +915,10 @@ const void* pick_group(int units, int row_tiles) {
 namespace lutgemm_attention_parts {
 #define NAME2(k) family##k
 #define NAME(k) NAME2(k)
-const void* NAME(LUT_PART)(int group_units, int row_tiles) {
+const void* NAME(LUT_PART)(int group_units, int row_tiles, int waves) {
   constexpr int kBits = LUT_PART / 5 == 0 ? 16 : (LUT_PART / 5 == 1 ? 8 : 4);
   constexpr int kUnits = LUT_PART % 5 == 0 ? 2 : (LUT_PART % 5 == 1 ? 3 : (LUT_PART % 5 == 2 ? 4 : (LUT_PART % 5 == 3 ? 6 : 8)));
-  return pick_group<kBits, kUnits>(group_units, row_tiles);
+  return pick_group<kBits, kUnits>(group_units, row_tiles, waves);
 }
 }  // namespace lutgemm_attention_parts
 
@@ -651,15 +969,16 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
   p.row_blocks = plan.row_blocks;
   const int most_rows = step->most_tokens * p.shared;
   p.partial_rows = most_rows < 16 * plan.row_tiles ? most_rows : 16 * plan.row_tiles;
-  p.scale = scale * 1.44269504088896340736f;
+  p.scale = (scale < 0.0f ? -scale : scale) * 1.44269504088896340736f;
+  p.flip = scale < 0.0f ? 0x80008000u : 0u;
   static const Family families[15] = {family0, family1, family2, family3, family4, family5, family6, family7,
                                       family8, family9, family10, family11, family12, family13, family14};
   const int bits = cache->bits == 16 ? 0 : (cache->bits == 8 ? 1 : 2), d = cache->head_dim;
   const int size = d == 64 ? 0 : (d == 96 ? 1 : (d == 128 ? 2 : (d == 192 ? 3 : 4)));
-  const void* kern = families[bits * 5 + size](group / 32, plan.row_tiles);
+  const void* kern = families[bits * 5 + size](group / 32, plan.row_tiles, plan.waves);
   if (!kern) return LUTGEMM_EUNSUPPORTED;
   void* args[] = {&p};
-  if (hipLaunchKernel(kern, dim3(plan.splits, cache->heads * plan.row_blocks, step->seqs), dim3(kWaves * 64), args, 0,
+  if (hipLaunchKernel(kern, dim3(plan.splits, cache->heads * plan.row_blocks, step->seqs), dim3(plan.waves * 64), args, 0,
                       static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return LUTGEMM_EHIP;
   return LUTGEMM_OK;

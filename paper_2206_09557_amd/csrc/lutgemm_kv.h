@@ -11,6 +11,7 @@
 namespace lutgemm_kv_detail {
 
 constexpr int kBlock = 32;        // positions of a block, channels of a unit
+constexpr int kMostSplitRows = 2048;   // splits of the positions times rows of a partial result
 constexpr int kMostTokens = 64;   // new tokens of a sequence that attention takes: one bit each in a mask word
 
 // Bytes of one block's keys (or values): codes, then scales.
@@ -49,9 +50,15 @@ inline int check_step(const lutgemm_kv_step* s) {
   return LUTGEMM_OK;
 }
 
+// Wavefronts a SIMD of the kernel that holds `row_tiles` tiles of 16 rows, by what its registers take (without scratch memory):
+// queries and results 12 registers a unit and tile, keys and values in flight up to 16 a unit.
+constexpr int attention_waves_per_simd(int head_dim, int row_tiles) {
+  return row_tiles == 1 ? (head_dim <= 64 ? 4 : (head_dim <= 128 ? 3 : 2)) : (row_tiles == 2 && head_dim <= 128 ? 2 : 1);
+}
+
 // How lutgemm_attention splits its work; see plan_attention in lutgemm_kv_host.cpp.
 struct AttentionPlan {
-  int row_tiles;    // tiles of 16 rows (token, query head) that a wavefront holds
+  int row_tiles;    // tiles of 16 rows (token, query head) of a workgroup: 1 or 2, which every wavefront holds, or 4 and more, shared out
   int row_blocks;   // workgroups along the rows of a key head
   int splits;       // workgroups along the positions, at most
   int chunk;        // positions of a split: a multiple of 32

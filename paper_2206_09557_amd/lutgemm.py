@@ -375,7 +375,7 @@ def lutgemm_attention(q, mask, cache, step, y, q_heads, q_stride, y_stride, scal
 
 
 def lutgemm_plan_attention(cache, step, q_heads, most_positions=0):
-    """(tiles of 16 rows a wavefront, row blocks, splits of the positions, positions a split, wavefronts a workgroup)"""
+    """(tiles of 16 rows a workgroup, row blocks, splits of the positions, positions a split, wavefronts a workgroup)"""
     out = (ctypes.c_int * 5)()
     _check(lib().lutgemm_plan_attention(_addr(cache), _addr(step), q_heads, most_positions, ctypes.addressof(out)),
            "lutgemm_plan_attention")
