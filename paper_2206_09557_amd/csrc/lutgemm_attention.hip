@@ -11,11 +11,14 @@
 // The maximum that the weights are relative to is only raised where a score passes it by 2^8, which is seldom;
 // the sum of the weights is one more product, of a tile of ones, so it adds what the other products add.
 //
-// At the end the wavefronts' sums meet in LDS, and where the positions are split the last workgroup to
-// arrive adds the splits in order (the hand-off is the one of finish_row_range in lutgemm_device.hip: write-through stores,
-// a wait for them, a barrier, a relaxed counter).  Results do not depend on who is last.
+// At the end the wavefronts' sums meet in LDS, and where the positions are split the splits' sums meet in memory: of up to 16 rows the
+// last workgroup to arrive adds them (the hand-off is the one of finish_row_range in lutgemm_device.hip: write-through
+// stores, a wait for them, a barrier, a relaxed counter), of more rows a second small kernel.  Both add in the order of
+// the splits.  JOIN_FIGURES
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "lutgemm_kv.h"
 
@@ -64,9 +67,10 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kJoinThreads = 256;
 constexpr float kSlack = 8.0f;    // how far, in powers of two, a score may pass the kept maximum: weights up to 2^8 in fp16
 
-// Partial results cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
+// Partial results that cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
 // that are served from it (what a relaxed atomic of device scope is, but of 16 or 8 bytes).
 constexpr int kDeviceScope = 16;     // sc1
 typedef __amdgpu_buffer_rsrc_t Buffer;
@@ -188,6 +192,8 @@ __device__ __forceinline__ half8v value_values(const Unit<BITS>& u, int j, const
   }
 }
 
+__device__ __forceinline__ _Float16 half_of(uint32_t word, int which) { return __builtin_bit_cast(_Float16, (uint16_t)(which ? word >> 16 : word)); }
+
 // Codes and scales of a block's keys or values on their way: DC units, and DC / GU groups' scales.
 template <int BITS, int DC, int GU>
 struct KeyWords {
@@ -235,11 +241,8 @@ __device__ __forceinline__ void load_values(ValueWords<BITS, DC, GU>& v, const c
 template <int BITS, int DC, int GU>
 __device__ __forceinline__ half8v key_operand(const KeyWords<BITS, DC, GU>& k, int c, int j) {
   if constexpr (BITS == 16) return key_values<16>(k.unit[c], j, (_Float16)0, (_Float16)0);
-  if constexpr (BITS == 8) return key_values<8>(k.unit[c], j, __builtin_bit_cast(half2v, k.scale[c / GU])[j], (_Float16)0);
-  if constexpr (BITS == 4) {
-    const half2v sz = __builtin_bit_cast(half2v, k.scale[2 * (c / GU) + j]);
-    return key_values<4>(k.unit[c], j, sz[0], sz[1]);
-  }
+  if constexpr (BITS == 8) return key_values<8>(k.unit[c], j, half_of(k.scale[c / GU], j), (_Float16)0);
+  if constexpr (BITS == 4) return key_values<4>(k.unit[c], j, half_of(k.scale[2 * (c / GU) + j], 0), half_of(k.scale[2 * (c / GU) + j], 1));
 }
 template <int BITS, int DC, int GU>
 __device__ __forceinline__ half8v value_operand(const ValueWords<BITS, DC, GU>& v, int c, int j) {
@@ -375,7 +378,7 @@ __device__ __forceinline__ half8v block_weights(const float4v (&score)[2], Sums<
   return weight;
 }
 
-// What a workgroup has to do: a split (blockIdx.x) of the positions, a row block of a key head (blockIdx.y), a sequence (blockIdx.z).
+// What a workgroup has to do: a split of the positions, a row block of a key head (blockIdx.y), a sequence (blockIdx.z).
 struct Place {
   int seq, head, row_block;
   int row_first;               // the sequence's first row of q and y
@@ -386,7 +389,7 @@ struct Place {
   int first_block, end_block;  // of this one
 };
 // From what the step says, within what the host said.  False: nothing to do.
-__device__ __forceinline__ bool find_place(const Params& p, int block_rows, Place* w) {
+__device__ __forceinline__ bool find_place(const Params& p, int block_rows, int split, Place* w) {
   w->seq = blockIdx.z;
   w->head = blockIdx.y / p.row_blocks;
   w->row_block = blockIdx.y - w->head * p.row_blocks;
@@ -400,10 +403,9 @@ __device__ __forceinline__ bool find_place(const Params& p, int block_rows, Plac
   int64_t chunk = p.chunk;
   if (chunk * p.splits < w->length) chunk = ((w->length + p.splits - 1) / p.splits + kBlock - 1) / kBlock * kBlock;
   w->active = max(1, (int)((w->length + chunk - 1) / chunk));
-  if ((int)blockIdx.x >= w->active) return false;
-  w->first_block = (int)(blockIdx.x * chunk / kBlock);
-  w->end_block = (int)((min((blockIdx.x + 1) * chunk, w->length) + kBlock - 1) / kBlock);
-  return true;
+  w->first_block = (int)(split * chunk / kBlock);
+  w->end_block = (int)((min((split + 1) * chunk, w->length) + kBlock - 1) / kBlock);
+  return split < w->active;
 }
 
 template <int DC, int RT>
@@ -445,38 +447,68 @@ __device__ __forceinline__ uint32_t visible_places(int place, int limit, uint64_
   }
   return visible;
 }
-// Adds a tile of 16 channels of a block that not every row sees all of.  A weight of zero must not meet an infinity or a NaN: what
-// is not finite is taken out of the operand, and counted for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there
-// are at most 32 of each).
+// For blocks that not every row sees all of.  Which of a lane's eight positions exist, as a mask of half words.
+__device__ __forceinline__ u32x4 existing_places(int place, int limit) {
+  u32x4 m;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = (place + 2 * i < limit ? 0x0000ffffu : 0u) | (place + 2 * i + 1 < limit ? 0xffff0000u : 0u);
+  return m;
+}
+__device__ __forceinline__ half8v masked(half8v v, u32x4 mask) { return __builtin_bit_cast(half8v, __builtin_bit_cast(u32x4, v) & mask); }
+// Zero, or a NaN where some of v is not finite.
+__device__ __forceinline__ half8v oddness(half8v v, half8v sum) {
+  const half8v zero = {0, 0, 0, 0, 0, 0, 0, 0};
+  return __builtin_elementwise_fma(v, zero, sum);
+}
+__device__ __forceinline__ bool any_odd(half8v sum) {
+  half8v t = sum;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) odd |= t[i] != t[i];
+  return __any(odd);
+}
+// A weight of zero must not meet an infinity or a NaN: where a block that some rows do not see has any, what is not finite is taken
+// out of the operand (returned) and counted for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there are at most 32 of
+// each); they get it added.
 template <int DC, int RT>
-__device__ __forceinline__ void add_masked(half8v v, int place, int limit, const half8v (&weight)[RT], const uint32_t (&visible)[RT], Sums<DC, RT>& s, int u) {
+__device__ __forceinline__ half8v take_odd(half8v v, const uint32_t (&visible)[RT], Sums<DC, RT>& s, int u) {
   half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
-  bool any = false;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t bits = bits_of(v[i]);
-    const bool exists = place + i < limit, infinite = (bits & 0x7c00u) == 0x7c00u;
-    if (infinite && exists) odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
-    any |= infinite && exists;
-    if (infinite || !exists) v[i] = (_Float16)0;
-  }
-  if (__any(any)) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      half8v seen;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) seen[i] = visible[t] >> i & 1u ? (_Float16)1.0f : (_Float16)0;
-      const float4v n = mfma(odd, seen, (float4v){0.0f, 0.0f, 0.0f, 0.0f});
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int found = (int)n[i];
-        const bool plus = (found & 63) != 0, minus = (found >> 6 & 63) != 0, nan = found >= 4096 || (plus && minus);
-        s.out[t][u][i] += nan ? __builtin_nanf("") : (plus ? __builtin_inff() : (minus ? -__builtin_inff() : 0.0f));
-      }
+    if ((bits & 0x7c00u) == 0x7c00u) {
+      odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
+      v[i] = (_Float16)0;
     }
   }
 #pragma unroll
-  for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
+  for (int t = 0; t < RT; ++t) {
+    half8v seen;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) seen[i] = visible[t] >> i & 1u ? (_Float16)1.0f : (_Float16)0;
+    const float4v n = mfma(odd, seen, (float4v){0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int found = (int)n[i];
+      const bool plus = (found & 63) != 0, minus = (found >> 6 & 63) != 0, nan = found >= 4096 || (plus && minus);
+      s.out[t][u][i] += nan ? __builtin_nanf("") : (plus ? __builtin_inff() : (minus ? -__builtin_inff() : 0.0f));
+    }
+  }
+  return v;
+}
+
+// A split's partial results: sums [partial_rows][dim], then a top and a total for each row.
+__device__ __forceinline__ float* partial_of(const Params& p, const Place& w, int split, int dim) {
+  const int64_t unit = ((int64_t)w.seq * p.heads + w.head) * p.row_blocks + w.row_block;
+  return p.partial + (unit * p.splits + split) * p.partial_rows * (dim + 2);
+}
+
+// The kernel's arguments once more, from memory: what only its end needs would else take up scalar registers through its loops.
+__device__ __forceinline__ Params arguments_again() {
+  typedef const __attribute__((address_space(4))) Params* Kernarg;
+  Kernarg args = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+  asm("" : "+s"(args));
+  return *(const Params*)args;
 }
 
 // The end of a workgroup, of GROUPS_R x PARTS wavefronts: PARTS that took different positions for the same RT tiles of rows, GROUPS_R
@@ -488,12 +520,13 @@ struct Ending {
   static constexpr int kFit = (PARTS * kRows <= 64 ? 40960 : 73728) / (PARTS * kRows * 128 + PARTS * kRows * 24);
   static constexpr int kMeet = kFit >= DC ? DC : (kFit >= 4 && DC % 4 == 0 ? 4 : (kFit >= 3 && DC % 3 == 0 ? 3 : (kFit >= 2 && DC % 2 == 0 ? 2 : 1)));
   static constexpr int kPitch = kMeet * 32 + 4;
+  static constexpr bool kLastAdds = kRows == 16;
   static constexpr int kMeetFloats = PARTS * kRows * (kPitch + 2);
-  static constexpr int kJoinFloats = 2 * kMostSplitRows + kRows + kThreads * 4;
+  static constexpr int kJoinFloats = kLastAdds ? 2 * kRows * kMostSplits + kRows + kThreads * 4 : 0;
   static constexpr int kFloats = kMeetFloats > kJoinFloats ? kMeetFloats : kJoinFloats;
 };
 template <int DC, int RT, int GROUPS_R, int PARTS>
-__device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, float* lds, uint32_t* last, Sums<DC, RT>& s, int group, int part, int lane) {
+__device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, float* lds, Sums<DC, RT>& s, int group, int part, int lane) {
   using E = Ending<DC, RT, GROUPS_R, PARTS>;
   constexpr int kRows = E::kRows, kThreads = E::kThreads, kDim = E::kDim, kMeet = E::kMeet, kPitch = E::kPitch;
   const int column = lane & 15, quarter = lane >> 4;
@@ -520,10 +553,9 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
       for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= factor;
     }
   }
-  const int unit = (w.seq * p.heads + w.head) * p.row_blocks + w.row_block;
-  const int64_t split_floats = (int64_t)p.partial_rows * (kDim + 2);     // a split's sums, then a top and a total for each row
-  float* unit_partial = p.partial + unit * p.splits * split_floats;
-  const Buffer mine = buffer_of(unit_partial + blockIdx.x * split_floats, split_floats);
+  float* mine = partial_of(p, w, blockIdx.x, kDim);
+  const int64_t split_floats = (int64_t)p.partial_rows * (kDim + 2);
+  const Buffer through = buffer_of(mine, split_floats);
 #pragma unroll
   for (int m = 0; m < DC / kMeet; ++m) {
     if (m > 0) __syncthreads();
@@ -541,134 +573,298 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
       float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int k = 0; k < PARTS; ++k) a += *reinterpret_cast<const float4v*>(&sums[(k * kRows + row) * kPitch + d]);
-      if (w.active > 1)
-        store4(mine, row * kDim + m * kMeet * 32 + d, a);
-      else
+      if (w.active > 1) {
+        if constexpr (E::kLastAdds)
+          store4(through, row * kDim + m * kMeet * 32 + d, a);
+        else
+          *reinterpret_cast<float4v*>(mine + row * kDim + m * kMeet * 32 + d) = a;
+      } else {
         store_row(p, w.row_first, w.head, w.row0 + row, kDim, m * kMeet * 32 + d, a, row_ends<PARTS, kRows>(tops, totals, row)[1]);
+      }
     }
   }
   if (w.active == 1) return;
-  for (int row = threadIdx.x; row < live_rows; row += kThreads) store2(mine, p.partial_rows * kDim + 2 * row, row_ends<PARTS, kRows>(tops, totals, row));
-
-  // The last workgroup to arrive adds the splits.
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (threadIdx.x == 0)
-    *last = __hip_atomic_fetch_add(p.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w.active - 1) ? 1u : 0u;
-  __syncthreads();
-  if (*last == 0u) return;
-  const Buffer all = buffer_of(unit_partial, p.splits * split_floats);
-  float* split_top = lds;                       // [live_rows][active], then the splits' factors
-  float* split_total = lds + kMostSplitRows;
-  float* row_total = lds + 2 * kMostSplitRows;  // [kRows]
-  float* shares = row_total + kRows;            // [kThreads][4]
-  for (int i = threadIdx.x; i < live_rows * w.active; i += kThreads) {
-    const int split = i / live_rows, row = i - split * live_rows;
-    const float2v end = load2(all, (int)(split * split_floats) + p.partial_rows * kDim + 2 * row);
-    split_top[row * w.active + split] = end[0];
-    split_total[row * w.active + split] = end[1];
+  for (int row = threadIdx.x; row < live_rows; row += kThreads) {
+    const float2v end = row_ends<PARTS, kRows>(tops, totals, row);
+    if constexpr (E::kLastAdds)
+      store2(through, p.partial_rows * kDim + 2 * row, end);
+    else
+      *reinterpret_cast<float2v*>(mine + p.partial_rows * kDim + 2 * row) = end;
   }
-  __syncthreads();
-  for (int row = threadIdx.x >> 4; row < live_rows; row += kThreads / 16) {      // sixteen lanes a row
-    float raised = -__builtin_inff(), sum = 0.0f;
-    for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, split_top[row * w.active + i]);
+  if constexpr (E::kLastAdds) {
+    uint32_t* last = reinterpret_cast<uint32_t*>(lds);            // (what was there has been added)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int64_t unit = ((int64_t)w.seq * p.heads + w.head) * p.row_blocks + w.row_block;
+    if (threadIdx.x == 0)
+      *last = __hip_atomic_fetch_add(p.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w.active - 1) ? 1u : 0u;
+    __syncthreads();
+    const bool mine_to_do = *last != 0u;
+    __syncthreads();
+    if (!mine_to_do) return;
+    const Buffer all = buffer_of(partial_of(p, w, 0, kDim), p.splits * split_floats);
+    float2v* ends = reinterpret_cast<float2v*>(lds);              // [live_rows][active]: top and total, then factor and total
+    float* row_total = lds + 2 * kRows * kMostSplits;             // [kRows]
+    float* shares = row_total + kRows;                            // [kThreads][4]
+    // An item is four channels of a row; where there are fewer items than threads, several threads share one's splits.  The first
+    // loads of an item do not wait for the splits' factors.
+    constexpr int kFours = kDim / 4, kAhead = 8;
+    const int items = live_rows * kFours;
+    int sharers = 1;
+    while (sharers < 16 && 2 * sharers * items <= kThreads && 2 * sharers <= w.active) sharers *= 2;
+    const int side = kThreads / sharers, share = threadIdx.x / side;
+    float4v ahead[kAhead];
+    auto load_ahead = [&](int i, int split) {
+      const int at = i / kFours * kDim + i % kFours * 4;
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, 16));
-    for (int i = column; i < w.active; i += 16) {
-      const float total = split_total[row * w.active + i], factor = part_factor(split_top[row * w.active + i], raised, total);
-      split_top[row * w.active + i] = factor;
-      sum += factor * total;
+      for (int k = 0; k < kAhead; ++k)
+        if (i < items && split + k * sharers < w.active) ahead[k] = load4(all, (int)((split + k * sharers) * split_floats) + at);
+    };
+    load_ahead(threadIdx.x - share * side, share);
+    for (int i = threadIdx.x; i < live_rows * w.active; i += kThreads) {
+      const int split = i / live_rows, row = i - split * live_rows;
+      ends[row * w.active + split] = load2(all, (int)(split * split_floats) + p.partial_rows * kDim + 2 * row);
     }
+    __syncthreads();
+    for (int row = threadIdx.x >> 4; row < live_rows; row += kThreads / 16) {      // sixteen lanes a row
+      float raised = -__builtin_inff(), sum = 0.0f;
+      for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, ends[row * w.active + i][0]);
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 16);
-    if (column == 0) row_total[row] = sum;
-  }
-  __syncthreads();
-  // An item is four channels of a row; where there are fewer items than threads, several threads share one's splits.
-  constexpr int kFours = kDim / 4;
-  const int items = live_rows * kFours;
-  int sharers = 1;
-  while (sharers < 16 && 2 * sharers * items <= kThreads && 2 * sharers <= w.active) sharers *= 2;
-  const int side = kThreads / sharers, share = threadIdx.x / side;
-  for (int base = 0; base < items; base += side) {
-    const int i = base + threadIdx.x - share * side;
-    const int row = i / kFours, d = i % kFours * 4;
-    const bool item = i < items && share < sharers;
-    float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (item) {
-      const int at = row * kDim + d;
-      int split = share;
-      for (; split + 7 * sharers < w.active; split += 8 * sharers) {
-        float4v v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = load4(all, (int)((split + k * sharers) * split_floats) + at);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) a += v[k] * split_top[row * w.active + split + k * sharers];
+      for (int d = 8; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, 16));
+      for (int i = column; i < w.active; i += 16) {
+        const float2v end = ends[row * w.active + i];
+        const float factor = part_factor(end[0], raised, end[1]);
+        ends[row * w.active + i][0] = factor;
+        sum += factor * end[1];
       }
-      for (; split < w.active; split += sharers) a += load4(all, (int)(split * split_floats) + at) * split_top[row * w.active + split];
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) sum += __shfl_xor(sum, d, 16);
+      if (column == 0) row_total[row] = sum;
     }
-    if (sharers > 1) {
-      __syncthreads();
-      *reinterpret_cast<float4v*>(&shares[threadIdx.x * 4]) = a;
-      __syncthreads();
-      if (item && share == 0)
-        for (int k = 1; k < sharers; ++k) a += *reinterpret_cast<const float4v*>(&shares[(threadIdx.x + k * side) * 4]);
+    __syncthreads();
+    for (int base = 0; base < items; base += side) {
+      const int i = base + threadIdx.x - share * side;
+      const int row = i / kFours, d = i % kFours * 4;
+      const bool item = i < items;
+      float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int split = share; split < w.active; split += kAhead * sharers) {
+        if (base > 0 || split != share) load_ahead(i, split);
+        if (item) {
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (split + k * sharers < w.active) a += ahead[k] * ends[row * w.active + split + k * sharers][0];
+        }
+      }
+      if (sharers > 1) {
+        __syncthreads();
+        *reinterpret_cast<float4v*>(&shares[threadIdx.x * 4]) = a;
+        __syncthreads();
+        if (item && share == 0)
+          for (int k = 1; k < sharers; ++k) a += *reinterpret_cast<const float4v*>(&shares[(threadIdx.x + k * side) * 4]);
+      }
+      if (item && share == 0) store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_total[row]);
     }
-    if (item && share == 0) store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_total[row]);
+    if (threadIdx.x == 0) __hip_atomic_store(p.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  if (threadIdx.x == 0) __hip_atomic_store(p.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Few rows: every wavefront takes all of them, and blocks of its own, from memory straight into registers.
+// The splits' sums meet, in their order.  DIM / 4 lanes take a row, four channels each; `sharers` such sets share a row's splits where
+// there are many.  blockIdx as in the kernels before, .x counting rows.  Nothing here is work: what it takes is
+// a trip to memory, so all of it is asked for at once, before the sequence's length says how many splits there are.
+template <int DIM>
+__global__ __launch_bounds__(kJoinThreads) void lutgemm_attention_join_kernel(Params p, int block_rows, int sharers) {
+  constexpr int kLanes = DIM / 4, kSets = kJoinThreads / kLanes, kAhead = 8;       // (48 lanes: some threads idle)
+  __shared__ __attribute__((aligned(16))) float shares[kSets][DIM];
+  __shared__ float share_total[kSets];
+  __shared__ float2v ends[kSets][kMostSplits];                    // of a row: top, total of every split
+  const int set = threadIdx.x / kLanes, lane = threadIdx.x - set * kLanes;
+  const int share = set % sharers, slot = set / sharers, row = blockIdx.x * (kSets / sharers) + slot;
+  Place w;
+  w.seq = blockIdx.z;
+  w.head = blockIdx.y / p.row_blocks;
+  w.row_block = blockIdx.y - w.head * p.row_blocks;
+  const float* partial = partial_of(p, w, 0, DIM);
+  const int64_t next = (int64_t)p.partial_rows * (DIM + 2);
+  const bool held = set < kSets && row < p.partial_rows;
+  const float* sums = partial + row * DIM + 4 * lane;
+  float4v ahead[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (held && share + k * sharers < p.splits) ahead[k] = *reinterpret_cast<const float4v*>(sums + (share + k * sharers) * next);
+  if (held)
+    for (int i = share * kLanes + lane; i < p.splits; i += sharers * kLanes)
+      ends[slot][i] = *reinterpret_cast<const float2v*>(partial + i * next + p.partial_rows * DIM + 2 * row);
+  const bool joined = find_place(p, block_rows, 0, &w) && w.active > 1;
+  const bool live = held && joined && row < min(w.rows - w.row0, block_rows);
+  __syncthreads();
+  float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
+  float total = 0.0f;
+  if (live) {
+    float raised = -__builtin_inff();
+    for (int i = 0; i < w.active; ++i) raised = fmaxf(raised, ends[slot][i][0]);
+    auto add = [&](float4v v, int split) {
+      const float2v end = ends[slot][split];
+      const float factor = part_factor(end[0], raised, end[1]);
+      total += factor * end[1];
+      a += v * factor;
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (share + k * sharers < w.active) add(ahead[k], share + k * sharers);
+#pragma unroll 2
+    for (int i = share + kAhead * sharers; i < w.active; i += sharers) add(*reinterpret_cast<const float4v*>(sums + i * next), i);
+    if (share != 0) {
+      *reinterpret_cast<float4v*>(&shares[set][4 * lane]) = a;
+      if (lane == 0) share_total[set] = total;
+    }
+  }
+  __syncthreads();
+  if (!live || share != 0) return;
+  for (int k = 1; k < sharers; ++k) {
+    a += *reinterpret_cast<const float4v*>(&shares[set + k][4 * lane]);
+    total += share_total[set + k];
+  }
+  store_row(p, w.row_first, w.head, w.row0 + row, DIM, 4 * lane, a, total);
+}
+
+// Whether a block's values have any that is not finite among those that exist.  Of quantised ones the scales say so: what they span
+// is looked at, which also takes in scales that no finite values have.
+template <int BITS, int DC, int GU>
+__device__ __forceinline__ bool values_odd(const ValueWords<BITS, DC, GU>& v, u32x4 exist) {
+  half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
+  if constexpr (BITS == 16) {
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) odd = oddness(masked(value_operand<BITS, DC, GU>(v, u / 2, u % 2), exist), odd);
+  } else {
+    const u32x4 positive = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+#pragma unroll
+    for (int g = 0; g < DC / GU; ++g) {
+      half8v span = masked(v.scale[g], positive & exist) * (_Float16)(BITS == 8 ? 128.0f : 16.0f);
+      if constexpr (BITS == 4) span += masked(v.offset[g], positive & exist);
+      odd = oddness(span, odd);
+    }
+  }
+  return any_odd(odd);
+}
+
+// Address of a block's codes: of the page that `page` numbers (0 where there is none: its values are not used).
+struct Blocks {
+  const char* head;            // the head's first block of page 0
+  int64_t page_bytes;
+  int block_bytes;
+};
+__device__ __forceinline__ Blocks blocks_of(const Params& p, int head) {
+  return {p.pool + (int64_t)head * p.page_blocks * p.block_bytes, (int64_t)p.heads * p.page_blocks * p.block_bytes, p.block_bytes};
+}
+__device__ __forceinline__ const char* block_address(const Blocks& b, int page, int in_page) {
+  return b.head + max(page, 0) * b.page_bytes + (int64_t)in_page * b.block_bytes;
+}
+
+// Few rows: every wavefront takes all of them, and blocks of its own, from memory straight into registers.  Two blocks are on
+// their way while one is worked on: a set's keys are asked for when the set's last ones have met the queries, its values
+// when those have been added.
 // BITS of a code, DC units of 32 channels to a head, GU of them to a scale, RT tiles of 16 rows.
 template <int BITS, int DC, int GU, int RT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, RT)) void lutgemm_attention_kernel(Params p) {
+__global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS, GU * 32, RT)) void lutgemm_attention_kernel(Params p) {
+  constexpr int kSets = attention_sets(DC * 32, BITS, GU * 32, RT);
   __shared__ __attribute__((aligned(16))) float lds[Ending<DC, RT, 1, WAVES>::kFloats];
-  __shared__ uint32_t last;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+  // The page table does not wait for the sequence's lengths (a split begins elsewhere only if it is longer than planned).
+  Walk<WAVES> walk;
+  walk.table = p.table + (int64_t)blockIdx.z * p.table_pages;
+  walk.pages = p.pages;
+  walk.table_pages = p.table_pages;
+  walk.page_blocks = p.page_blocks;
+  const int planned = (int)min((int64_t)blockIdx.x * (p.chunk / kBlock), (int64_t)p.table_pages * p.page_blocks) + wave;
+  walk_begin(walk, planned, lane);
   Place w;
-  if (!find_place(p, 16 * RT, &w)) return;
+  if (!find_place(p, 16 * RT, blockIdx.x, &w)) return;
+  if (w.first_block + wave != planned) walk_begin(walk, w.first_block + wave, lane);
 
   Sums<DC, RT> s;
   clear_sums(s);
   const half2v one = both((_Float16)1.0f);
   const half8v ones = join(one, one, one, one);
-  int block = w.first_block + wave;
-  if (block < w.end_block) {
-    Walk<WAVES> walk;
-    walk.table = p.table + (int64_t)w.seq * p.table_pages;
-    walk.pages = p.pages;
-    walk.table_pages = p.table_pages;
-    walk.page_blocks = p.page_blocks;
-    walk_begin(walk, block, lane);
-    const int64_t page_bytes = (int64_t)p.heads * p.page_blocks * p.block_bytes;
-    const char* head_base = p.pool + (int64_t)w.head * p.page_blocks * p.block_bytes;
-    const int value_offset = p.block_bytes / 2;
+  const Blocks blocks = blocks_of(p, w.head);
+  const int value_offset = p.block_bytes / 2;
+  KeyWords<BITS, DC, GU> keys[kSets];
+  ValueWords<BITS, DC, GU> values[kSets];
+  uint64_t sees[RT];
 
-    int page = walk_page(walk);
-    const char* at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
-    KeyWords<BITS, DC, GU> keys;
-    ValueWords<BITS, DC, GU> values;
-    load_keys<BITS, DC, GU>(keys, at, lane);
-    load_values<BITS, DC, GU>(values, at + value_offset, lane);
-    uint64_t sees[RT];
-    load_queries<DC, RT>(p, w, w.row0, lane, s, sees);
+  // Blocks that every row sees all of: the past but for its last few positions.
+  const int whole_end = min(w.past / kBlock, w.end_block);
+  int block = w.first_block + wave;           // the next to be worked on
+  int ahead = block;                          // the next to be asked for
+  bool dead[kSets];
+  const char* at = nullptr;
+  auto find = [&](int set) {                  // the block `ahead`
+    if (ahead != w.first_block + wave) walk_on(walk, lane);
+    const int page = walk_page(walk);
+    dead[set] = page < 0;
+    at = block_address(blocks, page, walk.in_page);
+    ahead += WAVES;
+  };
+  if (ahead < whole_end) {
+    find(0);
+    load_keys<BITS, DC, GU>(keys[0], at, lane);
+    load_values<BITS, DC, GU>(values[0], at + value_offset, lane);
+  }
+  load_queries<DC, RT>(p, w, w.row0, lane, s, sees);
 
-    // Blocks that every row sees all of: the past but for its last few positions.  A block's keys are asked for when the one before
-    // has met the queries, its values when that one's have been added.
-    const int whole_end = w.past / kBlock;
-    while (block < whole_end) {
+  // First the others, in the last set: the last positions of the past, the new ones, and what is behind them in the last block.
+  for (int b = block < whole_end ? block + (whole_end - block + WAVES - 1) / WAVES * WAVES : block; b < w.end_block; b += WAVES) {
+    KeyWords<BITS, DC, GU>& k = keys[kSets - 1];
+    ValueWords<BITS, DC, GU>& v = values[kSets - 1];
+    const int col = b / p.page_blocks;
+    const int listed = col < p.table_pages ? walk.table[col] : -1, page = listed < p.pages ? listed : -1;
+    const char* from = block_address(blocks, page, b - col * p.page_blocks);
+    load_keys<BITS, DC, GU>(k, from, lane);
+    load_values<BITS, DC, GU>(v, from + value_offset, lane);
+    const int place = b * kBlock + 8 * quarter - w.past;                  // of the lane's first position, counted from the new ones
+    const int limit = page < 0 ? -(1 << 30) : (int)(w.length - w.past);   // positions from here on do not exist
+    float4v score[RT][2];
+    block_scores<BITS, DC, GU, RT>(score, k, s);
+    half8v weight[RT];
+    uint32_t visible[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      visible[t] = visible_places(place, limit, sees[t]);
+      weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
+    }
+    const u32x4 exist = existing_places(place, limit);
+    const bool odd = values_odd<BITS, DC, GU>(v, exist);
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) {
+      half8v x = masked(value_operand<BITS, DC, GU>(v, u / 2, u % 2), exist);
+      if (__builtin_expect(odd, 0)) x = take_odd<DC, RT>(x, visible, s, u);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(x, weight[t], s.out[t][u]);
+    }
+    if (kSets == 1 && block < whole_end && b + WAVES >= w.end_block) {    // (one set only: fetch the first block again)
+      load_keys<BITS, DC, GU>(keys[0], at, lane);
+      load_values<BITS, DC, GU>(values[0], at + value_offset, lane);
+    }
+  }
+#pragma unroll
+  for (int set = 1; set < kSets; ++set)
+    if (ahead < whole_end) {
+      find(set);
+      load_keys<BITS, DC, GU>(keys[set], at, lane);
+      load_values<BITS, DC, GU>(values[set], at + value_offset, lane);
+    }
+  bool more = block < whole_end;
+  while (more) {
+#pragma unroll
+    for (int set = 0; set < kSets; ++set) {
+      if (!more) break;
       float4v score[RT][2];
-      block_scores<BITS, DC, GU, RT>(score, keys, s);
-      const int next = block + WAVES;
-      const bool dead = page < 0;
-      if (next < w.end_block) {
-        walk_on(walk, lane);
-        page = walk_page(walk);
-        at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
-        load_keys<BITS, DC, GU>(keys, at, lane);
+      block_scores<BITS, DC, GU, RT>(score, keys[set], s);
+      const bool skip = dead[set], again = ahead < whole_end;
+      if (again) {
+        find(set);
+        load_keys<BITS, DC, GU>(keys[set], at, lane);
       }
-      if (!dead) {
+      if (!skip) {
         half8v weight[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) weight[t] = block_weights<DC, RT, false>(score[t], s, t, p.scale, 0u, ones);
@@ -676,48 +872,18 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, RT)) 
         for (int c = 0; c < DC; ++c) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const half8v v = value_operand<BITS, DC, GU>(values, c, j);
+            const half8v v = value_operand<BITS, DC, GU>(values[set], c, j);
 #pragma unroll
             for (int t = 0; t < RT; ++t) s.out[t][2 * c + j] = mfma(v, weight[t], s.out[t][2 * c + j]);
           }
         }
       }
-      block = next;
-      if (block >= w.end_block) break;
-      load_values<BITS, DC, GU>(values, at + value_offset, lane);
-    }
-
-    // The others: the last positions of the past, the new ones, and what is behind them in the last block.
-    while (block < w.end_block) {
-      float4v score[RT][2];
-      block_scores<BITS, DC, GU, RT>(score, keys, s);
-      const int next = block + WAVES;
-      const int place = block * kBlock + 8 * quarter - w.past;              // of the lane's first position, counted from the new ones
-      const int limit = page < 0 ? -(1 << 30) : (int)(w.length - w.past);   // positions from here on do not exist
-      if (next < w.end_block) {
-        walk_on(walk, lane);
-        page = walk_page(walk);
-        at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
-        load_keys<BITS, DC, GU>(keys, at, lane);
-      }
-      half8v weight[RT];
-      uint32_t visible[RT];
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        visible[t] = visible_places(place, limit, sees[t]);
-        weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
-      }
-#pragma unroll
-      for (int c = 0; c < DC; ++c) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) add_masked<DC, RT>(value_operand<BITS, DC, GU>(values, c, j), place, limit, weight, visible, s, 2 * c + j);
-      }
-      block = next;
-      if (block >= w.end_block) break;
-      load_values<BITS, DC, GU>(values, at + value_offset, lane);
+      if (again) load_values<BITS, DC, GU>(values[set], at + value_offset, lane);
+      block += WAVES;
+      more = block < whole_end;
     }
   }
-  end_workgroup<DC, RT, 1, WAVES>(p, w, lds, &last, s, 0, wave, lane);
+  end_workgroup<DC, RT, 1, WAVES>(arguments_again(), w, lds, s, 0, wave, lane);
 }
 
 // Many rows: GROUPS_R wavefronts share a block, RT tiles of rows each, so that its codes are fetched and made fp16 once for all of them:
@@ -729,14 +895,14 @@ template <int BITS, int DC, int GU, int RT, int GROUPS_R, int PARTS>
 __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_shared_kernel(Params p) {
   constexpr int kEach = (2 * DC + GROUPS_R - 1) / GROUPS_R;        // units of a wavefront
   constexpr int kOperands = 2 * DC * 2 * 1024;                     // bytes of a block's: units x runs
+  constexpr int kDepth = kEach * BITS <= 32 && kEach * DC < 32 ? 2 : 1;               // blocks of codes on their way
   using E = Ending<DC, RT, GROUPS_R, PARTS>;
   constexpr int kBytes = 2 * PARTS * kOperands > E::kFloats * 4 ? 2 * PARTS * kOperands : E::kFloats * 4;
   __shared__ __attribute__((aligned(16))) char lds[kBytes];
-  __shared__ uint32_t last;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
   const int group = wave % GROUPS_R, part = wave / GROUPS_R;
   Place w;
-  if (!find_place(p, 16 * RT * GROUPS_R, &w)) return;
+  if (!find_place(p, 16 * RT * GROUPS_R, blockIdx.x, &w)) return;
 
   Sums<DC, RT> s;
   clear_sums(s);
@@ -748,30 +914,35 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
   walk.table_pages = p.table_pages;
   walk.page_blocks = p.page_blocks;
   walk_begin(walk, w.first_block + part, lane);
-  const int64_t page_bytes = (int64_t)p.heads * p.page_blocks * p.block_bytes;
-  const char* head_base = p.pool + (int64_t)w.head * p.page_blocks * p.block_bytes;
+  const Blocks blocks = blocks_of(p, w.head);
 
   constexpr int kCode = kBlock * DC * 32 * BITS / 8;
-  Unit<BITS> unit[kEach];
-  half8v scale[kEach], offset[BITS == 4 ? kEach : 1];              // of a value unit; of a key unit in the first words
-  int page;
-  auto fetch = [&]() {                                             // this wavefront's units of the block that `walk` is at
-    page = walk_page(walk);
-    const char* at = head_base + max(page, 0) * page_bytes + (int64_t)walk.in_page * p.block_bytes;
+  Unit<BITS> unit[kDepth][kEach];
+  half8v scale[kDepth][BITS == 16 ? 1 : kEach], offset[kDepth][BITS == 4 ? kEach : 1];       // of a value unit; of a key unit in the first words
+  bool dead[2] = {false, false};
+  int ahead = w.first_block + part;                                // the next block to be fetched
+  // This wavefront's units of the block `ahead`; `half`: of the LDS, where they are to go.
+  auto fetch = [&](const int half) {
+    const int set = kDepth == 2 ? half : 0;
+    if (ahead >= w.end_block) return;
+    if (ahead != w.first_block + part) walk_on(walk, lane);
+    const int page = walk_page(walk);
+    dead[half] = page < 0;
+    const char* at = block_address(blocks, page, walk.in_page);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int u = group + i * GROUPS_R;
       if (u >= 2 * DC) continue;
       const int c = u < DC ? u : u - DC, g = c / GU;
       const char* half_block = at + (u < DC ? 0 : p.block_bytes / 2);
-      load_unit<BITS>(unit[i], half_block, c, lane);
+      load_unit<BITS>(unit[set][i], half_block, c, lane);
       if constexpr (BITS == 8) {
         u32x4 v = {0u, 0u, 0u, 0u};
         if (u < DC)
           v[0] = reinterpret_cast<const uint32_t*>(half_block + kCode + g * 64)[lane & 15];
         else
           v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 64)[lane >> 4];
-        scale[i] = __builtin_bit_cast(half8v, v);
+        scale[set][i] = __builtin_bit_cast(half8v, v);
       }
       if constexpr (BITS == 4) {
         u32x4 v = {0u, 0u, 0u, 0u}, z = v;
@@ -783,13 +954,17 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
           v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128)[lane >> 4];
           z = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128 + 64)[lane >> 4];
         }
-        scale[i] = __builtin_bit_cast(half8v, v);
-        offset[i] = __builtin_bit_cast(half8v, z);
+        scale[set][i] = __builtin_bit_cast(half8v, v);
+        offset[set][i] = __builtin_bit_cast(half8v, z);
       }
     }
+    ahead += PARTS;
   };
-  auto operands = [&](int half) { return lds + (half * PARTS + part) * kOperands; };
-  auto put = [&](int half) {                                       // the fetched units, as operands
+  auto operands = [&](const int half) { return lds + (half * PARTS + part) * kOperands; };
+  // The fetched units of `block`, as operands.
+  auto put = [&](const int half, int block) {
+    const int set = kDepth == 2 ? half : 0;
+    if (block >= w.end_block) return;
     u32x4* to = reinterpret_cast<u32x4*>(operands(half)) + lane;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -798,89 +973,98 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         half8v v;
-        if (BITS == 16 || u >= DC)
-          v = value_values<BITS>(unit[i], j, scale[i], offset[BITS == 4 ? i : 0]);
-        else if (BITS == 8)
-          v = key_values<BITS>(unit[i], j, scale[i][j], (_Float16)0);
-        else
-          v = key_values<BITS>(unit[i], j, scale[i][2 * j], scale[i][2 * j + 1]);
+        if constexpr (BITS == 16) {
+          const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
+          v = value_values<16>(unit[set][i], j, none, none);
+        } else if (u >= DC) {
+          v = value_values<BITS>(unit[set][i], j, scale[set][i], offset[set][BITS == 4 ? i : 0]);
+        } else {
+          v = BITS == 8 ? key_values<BITS>(unit[set][i], j, scale[set][i][j], (_Float16)0)
+                        : key_values<BITS>(unit[set][i], j, scale[set][i][2 * j], scale[set][i][2 * j + 1]);
+        }
         to[(u * 2 + j) * 64] = __builtin_bit_cast(u32x4, v);
       }
     }
   };
 
   int block = w.first_block + part;                                // this part's
-  const int stages = (w.end_block - w.first_block + PARTS - 1) / PARTS;
-  if (block < w.end_block) fetch();
+  fetch(0);
+  if (kDepth == 2) fetch(1);
   uint64_t sees[RT];
   load_queries<DC, RT>(p, w, w.row0 + 16 * RT * group, lane, s, sees);
-  bool dead = false, next_dead = false;
-  if (block < w.end_block) {
-    put(0);
-    dead = page < 0;
-  }
-  const int whole_end = w.past / kBlock;
+  put(0, block);
+  const int stages = (w.end_block - w.first_block + PARTS - 1) / PARTS;
+  const int whole_end = w.past / kBlock;                           // every row sees all of the blocks before it
+  const int whole_stages = whole_end >= w.end_block ? stages : max(0, whole_end - w.first_block) / PARTS;
   const bool idle = w.row0 + 16 * RT * group >= w.rows;            // no row of this wavefront's lives: it only helps with the operands
-  for (int stage = 0; stage < stages; ++stage) {
-    const int next = block + PARTS;
-    if (next < w.end_block) {
-      walk_on(walk, lane);
-      fetch();
-      next_dead = page < 0;
-    }
+  auto stage = [&](const int half, auto mask) {
+    constexpr bool kMasked = decltype(mask)::value;
+    const bool skip = idle || block >= w.end_block || (!kMasked && dead[half]);
+    const int limit = dead[half] ? -(1 << 30) : (int)(w.length - w.past), place = block * kBlock + 8 * quarter - w.past;
+    fetch(kDepth == 2 ? half : half ^ 1);                          // (what was in those registers has been put)
     __syncthreads();
-    if (block < w.end_block && !idle) {
-      const half8v* from = reinterpret_cast<const half8v*>(operands(stage & 1)) + lane;
+    if (!skip) {
+      const half8v* from = reinterpret_cast<const half8v*>(operands(half)) + lane;
       float4v score[RT][2];
 #pragma unroll
       for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int c = 0; c < DC; ++c) {
+      for (int u = 0; u < 2 * DC; ++u) {
+        const half8v k = from[u * 64];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const half8v k = from[(c * 2 + j) * 64];
-#pragma unroll
-          for (int t = 0; t < RT; ++t) score[t][j] = mfma(k, s.query[t][c], score[t][j]);
-        }
+        for (int t = 0; t < RT; ++t) score[t][u % 2] = mfma(k, s.query[t][u / 2], score[t][u % 2]);
       }
       half8v weight[RT];
-      if (block < whole_end) {
-        if (!dead) {
+      uint32_t visible[RT];
 #pragma unroll
-          for (int t = 0; t < RT; ++t) weight[t] = block_weights<DC, RT, false>(score[t], s, t, p.scale, 0u, ones);
+      for (int t = 0; t < RT; ++t) {
+        visible[t] = kMasked ? visible_places(place, limit, sees[t]) : 0u;
+        weight[t] = block_weights<DC, RT, kMasked>(score[t], s, t, p.scale, visible[t], ones);
+      }
+      u32x4 exist;
+      bool rare = false;
+      if constexpr (kMasked) {
+        exist = existing_places(place, limit);
+        half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-          for (int u = 0; u < 2 * DC; ++u) {
-            const half8v v = from[(2 * DC + u) * 64];
+        for (int u = 0; u < 2 * DC; ++u) odd = oddness(masked(from[(2 * DC + u) * 64], exist), odd);
+        rare = any_odd(odd);
+      }
 #pragma unroll
-            for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
-          }
+      for (int u = 0; u < 2 * DC; ++u) {
+        half8v v = from[(2 * DC + u) * 64];
+        if constexpr (kMasked) {
+          v = masked(v, exist);
+          if (__builtin_expect(rare, 0)) v = take_odd<DC, RT>(v, visible, s, u);
         }
-      } else {
-        const int place = block * kBlock + 8 * quarter - w.past, limit = dead ? -(1 << 30) : (int)(w.length - w.past);
-        uint32_t visible[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          visible[t] = visible_places(place, limit, sees[t]);
-          weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
-        }
-#pragma unroll
-        for (int u = 0; u < 2 * DC; ++u) add_masked<DC, RT>(from[(2 * DC + u) * 64], place, limit, weight, visible, s, u);
+        for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
       }
     }
-    if (next < w.end_block) put((stage + 1) & 1);
-    block = next;
-    dead = next_dead;
+    block += PARTS;
+    put(half ^ 1, block);
+  };
+  int done = 0;
+  for (; done + 2 <= whole_stages; done += 2) {
+    stage(0, std::false_type());
+    stage(1, std::false_type());
+  }
+  for (; done < stages; done += 2) {
+    stage(0, std::true_type());
+    if (done + 1 < stages) stage(1, std::true_type());
   }
   __syncthreads();
-  end_workgroup<DC, RT, GROUPS_R, PARTS>(p, w, reinterpret_cast<float*>(lds), &last, s, group, part, lane);
+  end_workgroup<DC, RT, GROUPS_R, PARTS>(arguments_again(), w, reinterpret_cast<float*>(lds), s, group, part, lane);
 }
 
 template <int BITS, int DC, int GU>
 const void* pick_tiles(int row_tiles, int waves) {
-  constexpr int kAll = 4 * attention_waves_per_simd(DC * 32, 1);
+  constexpr int kAll = 4 * attention_waves_per_simd(DC * 32, BITS, GU * 32, 1);
   if (row_tiles == 1 && waves == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 1, 4>);
   if (row_tiles == 1 && waves == kAll) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 1, kAll>);
-  if (row_tiles == 2 && waves == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 2, 4>);
+  if constexpr (DC <= 4) {
+    if (row_tiles == 2 && waves == 4) return reinterpret_cast<const void*>(lutgemm_attention_kernel<BITS, DC, GU, 2, 4>);
+  }
   if (waves != 8) return nullptr;
   if constexpr (DC <= 4) {
     if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 2, 4>);
@@ -939,7 +1123,7 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
   if (held > (int64_t)1 << 30) return LUTGEMM_EUNSUPPORTED;
   if (most_positions == 0 || most_positions > held) most_positions = held;
   const int group = group_of(cache->head_dim, cache->bits, cache->group);
-  const AttentionPlan plan = plan_attention(cache->heads, cache->head_dim, cache->bits, q_heads, step->seqs, step->most_tokens, most_positions);
+  const AttentionPlan plan = plan_attention(cache->heads, cache->head_dim, cache->bits, group, q_heads, step->seqs, step->most_tokens, most_positions);
   if (workspace_bytes < 32768 + 4 * (size_t)attention_partial_floats(plan, cache->heads, cache->head_dim, q_heads, step->seqs, step->most_tokens))
     return LUTGEMM_EWORKSPACE;
   if (step->tokens == 0 || step->most_tokens == 0) return LUTGEMM_OK;
@@ -979,6 +1163,21 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
   if (!kern) return LUTGEMM_EUNSUPPORTED;
   void* args[] = {&p};
   if (hipLaunchKernel(kern, dim3(plan.splits, cache->heads * plan.row_blocks, step->seqs), dim3(plan.waves * 64), args, 0,
+                      static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    return LUTGEMM_EHIP;
+  if (plan.splits == 1 || plan.row_tiles == 1) return LUTGEMM_OK;      // (of 16 rows the last workgroup adds the splits)
+  // Sets of DIM / 4 lanes in a workgroup; up to eight splits a set.
+  const int sets = kJoinThreads / (d / 4);
+  int sharers = 1, block_rows = 16 * plan.row_tiles;
+  while (2 * sharers <= sets && sharers * 8 < plan.splits) sharers *= 2;
+  const int rows = sets / sharers;
+  const void* join = d == 64    ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<64>)
+                     : d == 96  ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<96>)
+                     : d == 128 ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<128>)
+                     : d == 192 ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<192>)
+                                : reinterpret_cast<const void*>(lutgemm_attention_join_kernel<256>);
+  void* join_args[] = {&p, &block_rows, &sharers};
+  if (hipLaunchKernel(join, dim3((p.partial_rows + rows - 1) / rows, cache->heads * plan.row_blocks, step->seqs), dim3(kJoinThreads), join_args, 0,
                       static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return LUTGEMM_EHIP;
   return LUTGEMM_OK;

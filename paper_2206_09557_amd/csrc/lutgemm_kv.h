@@ -11,7 +11,7 @@
 namespace lutgemm_kv_detail {
 
 constexpr int kBlock = 32;        // positions of a block, channels of a unit
-constexpr int kMostSplitRows = 2048;   // splits of the positions times rows of a partial result
+constexpr int kMostSplits = 128;  // of the positions
 constexpr int kMostTokens = 64;   // new tokens of a sequence that attention takes: one bit each in a mask word
 
 // Bytes of one block's keys (or values): codes, then scales.
@@ -50,10 +50,20 @@ inline int check_step(const lutgemm_kv_step* s) {
   return LUTGEMM_OK;
 }
 
-// Wavefronts a SIMD of the kernel that holds `row_tiles` tiles of 16 rows, by what its registers take (without scratch memory):
-// queries and results 12 registers a unit and tile, keys and values in flight up to 16 a unit.
-constexpr int attention_waves_per_simd(int head_dim, int row_tiles) {
-  return row_tiles == 1 ? (head_dim <= 64 ? 4 : (head_dim <= 128 ? 3 : 2)) : (row_tiles == 2 && head_dim <= 128 ? 2 : 1);
+// The kernel whose wavefronts hold all rows (`row_tiles` of 16, 1 or 2): registers, as compiled, with `sets` blocks of
+// codes and scales in them; and what follows from it: two sets where that leaves two wavefronts a SIMD, else one;
+// one wavefront where not even one set does.
+constexpr int attention_registers(int head_dim, int bits, int group, int row_tiles, int sets) {
+  const int units = head_dim / 32, scales = bits == 8 ? 5 * (head_dim / group) : (bits == 4 ? 10 * (head_dim / group) : 0);
+  return 30 + row_tiles * (12 * units + 26) + sets * (units * bits + scales) + (bits == 16 ? 5 * units : 0);
+}
+constexpr int attention_sets(int head_dim, int bits, int group, int row_tiles) {
+  const int two = attention_registers(head_dim, bits, group, row_tiles, 2);
+  return two <= 252 || (attention_registers(head_dim, bits, group, row_tiles, 1) > 252 && two <= 400) ? 2 : 1;
+}
+constexpr int attention_waves_per_simd(int head_dim, int bits, int group, int row_tiles) {
+  const int r = attention_registers(head_dim, bits, group, row_tiles, attention_sets(head_dim, bits, group, row_tiles));
+  return r <= 124 ? 4 : (r <= 164 ? 3 : (r <= 252 ? 2 : 1));
 }
 
 // How lutgemm_attention splits its work; see plan_attention in lutgemm_kv_host.cpp.
@@ -64,7 +74,7 @@ struct AttentionPlan {
   int chunk;        // positions of a split: a multiple of 32
   int waves;        // wavefronts of a workgroup
 };
-AttentionPlan plan_attention(int heads, int head_dim, int bits, int q_heads, int seqs, int most_tokens, int64_t most_positions);
+AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q_heads, int seqs, int most_tokens, int64_t most_positions);
 // Floats of the partial results behind the workspace's counters (0: nothing is split).
 int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens);
 

@@ -8,30 +8,27 @@
 namespace lutgemm_kv_detail {
 
 namespace {
-constexpr int64_t kCounters = 8192;      // arrival counters of a workspace (32 KB)
 constexpr int64_t kComputeUnits = 256;
 }  // namespace
 
-AttentionPlan plan_attention(int heads, int head_dim, int bits, int q_heads, int seqs, int most_tokens, int64_t most_positions) {
-  (void)bits;
+AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q_heads, int seqs, int most_tokens, int64_t most_positions) {
   AttentionPlan p;
   const int64_t rows = (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads);
-  // Up to 32 rows each wavefront holds all of them; beyond, eight wavefronts share them out (of 32 each, 16 of long heads) and
+  // Up to 32 rows (16 of long heads) each wavefront holds all of them; beyond, eight wavefronts share them out (32 each, or 16) and
   // the blocks' operands.
   const int most_tiles = head_dim <= 128 ? 16 : 8;
-  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 && head_dim <= 128 ? 2 : 4);
   while (p.row_tiles >= 4 && p.row_tiles < most_tiles && 16 * p.row_tiles < rows) p.row_tiles *= 2;
   p.row_blocks = (int)std::max<int64_t>(1, (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
   const int64_t units = (int64_t)seqs * heads * p.row_blocks;
   const int64_t blocks = std::max<int64_t>(1, (most_positions + kBlock - 1) / kBlock);
   // Few units get a compute unit's wavefronts in one workgroup, whose sums meet in LDS; many get four each.
-  const int simd = p.row_tiles >= 4 ? 2 : attention_waves_per_simd(head_dim, p.row_tiles);
+  const int simd = p.row_tiles >= 4 ? 2 : attention_waves_per_simd(head_dim, bits, group, p.row_tiles);
   p.waves = p.row_tiles >= 4 ? 8 : (p.row_tiles == 1 && units < kComputeUnits * simd ? 4 * simd : 4);
   const int64_t room = kComputeUnits * 4 * simd / p.waves;
-  // Splits until the device is full, of no fewer than two blocks a wavefront (a split's partial results are written
-  // and read once more by the last workgroup), where there are counters for them.
-  int64_t splits = units > kCounters ? 1 : std::min(room / units, (blocks + 2 * p.waves - 1) / (2 * p.waves));
-  splits = std::max<int64_t>(1, std::min(splits, kMostSplitRows / std::max<int64_t>(1, std::min<int64_t>(rows, 16 * p.row_tiles))));
+  // Splits until the device is full, of no fewer than two blocks a wavefront.
+  int64_t splits = std::min(room / units, (blocks + 2 * p.waves - 1) / (2 * p.waves));
+  splits = std::max<int64_t>(1, std::min<int64_t>(splits, kMostSplits));
   const int64_t per = (blocks + splits - 1) / splits;
   p.chunk = (int)std::min<int64_t>(per, 1 << 24) * kBlock;
   p.splits = (int)((blocks + per - 1) / per);
@@ -59,7 +56,7 @@ int plan_of(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_he
   if (step->seqs > 65535 || step->most_tokens > kMostTokens || q_heads > 1 << 14) return LUTGEMM_EUNSUPPORTED;
   const int64_t held = (int64_t)step->table_pages * cache->page_tokens;
   if (most_positions == 0 || most_positions > held) most_positions = held;
-  *plan = plan_attention(cache->heads, cache->head_dim, cache->bits, q_heads, step->seqs, step->most_tokens, most_positions);
+  *plan = plan_attention(cache->heads, cache->head_dim, cache->bits, group_of(cache->head_dim, cache->bits, cache->group), q_heads, step->seqs, step->most_tokens, most_positions);
   return LUTGEMM_OK;
 }
 
