@@ -14,7 +14,7 @@
 // At the end the wavefronts' sums meet in LDS, and where the positions are split the splits' sums meet in memory: of up to 16 rows the
 // last workgroup to arrive adds them (the hand-off is the one of finish_row_range in lutgemm_device.hip: write-through
 // stores, a wait for them, a barrier, a relaxed counter), of more rows a second small kernel.  Both add in the order of
-// the splits.  JOIN_FIGURES
+// the splits.  131072 positions of one sequence in 32 splits: meeting in LDS, handing off and adding take 8 us of 42.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -43,6 +43,7 @@ struct Params {
   int64_t q_stride, y_stride, pages;
   int tokens, most_tokens, table_pages, page_blocks, heads, shared;   // shared: query heads of a key head
   int block_bytes, splits, chunk, row_blocks, partial_rows;
+  float inverse_shared;
   float scale;                                           // of the scores, times log2 e; not negative ...
   uint32_t flip;                                         // ... the queries' signs are
 };
@@ -194,6 +195,10 @@ __device__ __forceinline__ half8v value_values(const Unit<BITS>& u, int j, const
 
 __device__ __forceinline__ _Float16 half_of(uint32_t word, int which) { return __builtin_bit_cast(_Float16, (uint16_t)(which ? word >> 16 : word)); }
 
+template <int I>
+__device__ __forceinline__ uint32_t word_of(u32x4 v) { return v[I]; }
+__device__ __forceinline__ uint32_t one_of(uint32_t a, uint32_t b, uint32_t second) { return (a & ~second) | (b & second); }   // second: a mask
+
 // Codes and scales of a block's keys or values on their way: DC units, and DC / GU groups' scales.
 template <int BITS, int DC, int GU>
 struct KeyWords {
@@ -251,46 +256,50 @@ __device__ __forceinline__ half8v value_operand(const ValueWords<BITS, DC, GU>& 
 
 __device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// A walk over every WAVES-th block of a split: which page a block is in, without a division a block.  The table's entries are
-// fetched 64 at a time, one a lane.
-template <int WAVES>
+// A walk over every STEP-th block of a split: which page a block is in, without a division a block.  The next block's entry of the
+// page table is on its way while a block is worked on, by a scalar load: a wait for it is no wait for the codes in flight.
+typedef const __attribute__((address_space(4))) int32_t* Table;
+template <int STEP>
 struct Walk {
-  const int32_t* table;        // of the sequence
+  Table table;                 // of the sequence
+  int last_col, page_blocks;
   int64_t pages;
-  int table_pages, page_blocks;
   int col, in_page;            // page of the sequence, block in it
   int col_step, block_step;
-  int base;                    // first table entry held
-  int held;                    // this lane's
+  int entry;                   // of the table
 };
-template <int WAVES>
-__device__ __forceinline__ void walk_fetch(Walk<WAVES>& w, int lane) {
-  w.base = w.col;
-  w.held = w.col + lane < w.table_pages ? w.table[w.col + lane] : -1;
-}
-template <int WAVES>
-__device__ __forceinline__ void walk_begin(Walk<WAVES>& w, int block, int lane) {
+template <int STEP>
+__device__ __forceinline__ void walk_begin(Walk<STEP>& w, int block) {
   w.col = block / w.page_blocks;
   w.in_page = block - w.col * w.page_blocks;
-  w.col_step = WAVES / w.page_blocks;
-  w.block_step = WAVES - w.col_step * w.page_blocks;
-  walk_fetch(w, lane);
+  w.entry = w.table[min(w.col, w.last_col)];
 }
-template <int WAVES>
-__device__ __forceinline__ void walk_on(Walk<WAVES>& w, int lane) {
+template <int STEP>
+__device__ __forceinline__ Walk<STEP> walk_of(const Params& p, int seq, int block) {
+  Walk<STEP> w;
+  w.table = (Table)(p.table + (int64_t)seq * p.table_pages);
+  w.last_col = p.table_pages - 1;
+  w.page_blocks = p.page_blocks;
+  w.pages = p.pages;
+  w.col_step = STEP / p.page_blocks;
+  w.block_step = STEP - w.col_step * p.page_blocks;
+  walk_begin(w, block);
+  return w;
+}
+template <int STEP>
+__device__ __forceinline__ void walk_on(Walk<STEP>& w) {
   w.col += w.col_step;
   w.in_page += w.block_step;
   if (w.in_page >= w.page_blocks) {
     w.in_page -= w.page_blocks;
     ++w.col;
   }
-  if (w.col - w.base >= 64) walk_fetch(w, lane);
+  w.entry = w.table[min(w.col, w.last_col)];
 }
-// Number of the page (-1: none).
-template <int WAVES>
-__device__ __forceinline__ int walk_page(const Walk<WAVES>& w) {
-  const int page = __builtin_amdgcn_readlane(w.held, w.col - w.base);
-  return page >= 0 && page < w.pages ? page : -1;
+// Number of the block's page (-1: none).
+template <int STEP>
+__device__ __forceinline__ int walk_page(const Walk<STEP>& w) {
+  return w.col <= w.last_col && w.entry >= 0 && w.entry < w.pages ? w.entry : -1;
 }
 
 // Factor of a part's sums where parts meet: its top is at most `raised`.  A part that saw nothing has none; a NaN stays one.
@@ -298,26 +307,18 @@ __device__ __forceinline__ float part_factor(float top, float raised, float tota
   if (top == -__builtin_inff()) return total == total ? 0.0f : total;
   return __builtin_amdgcn_exp2f(top - raised);
 }
-// Top and total of a row over the wavefronts.
-template <int WAVES, int ROWS>
-__device__ __forceinline__ float2v row_ends(const float* tops, const float* totals, int row) {
-  float raised = -__builtin_inff(), sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) raised = fmaxf(raised, tops[w * ROWS + row]);
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    const float t = totals[w * ROWS + row];
-    sum += part_factor(tops[w * ROWS + row], raised, t) * t;
-  }
-  return (float2v){raised, sum};
-}
+// Row / query heads of a key head.  (row + 1/2) / shared is at least 1/2 / shared away from a whole number: 3e-5 at least, where the
+// product is off by 64 * 2^-23 at most.
+__device__ __forceinline__ int token_of(const Params& p, int row) { return (int)(((float)row + 0.5f) * p.inverse_shared); }
 // Four channels of a row's result (a row that saw nothing has a total of zero).
 __device__ __forceinline__ void store_row(const Params& p, int row_first, int head, int row, int dim, int d, float4v a, float total) {
-  const int token = row / p.shared;
+  const int token = token_of(p, row);
   const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
   *reinterpret_cast<half4v*>(p.y + (int64_t)(row_first + token) * p.y_stride + ((int64_t)head * p.shared + row - token * p.shared) * dim + d) =
       __builtin_convertvector(a * inverse, half4v);
 }
+
+__device__ __forceinline__ half8v masked(half8v v, u32x4 mask) { return __builtin_bit_cast(half8v, __builtin_bit_cast(u32x4, v) & mask); }
 
 // What a wavefront carries from block to block.
 template <int DC, int RT>
@@ -343,15 +344,17 @@ __device__ __forceinline__ void block_scores(float4v (&score)[RT][2], const KeyW
   }
 }
 
-// The weights' turn: of one tile's eight positions a lane, as the next product's operand.  MASKED: visible has a bit for each.
-template <int DC, int RT, bool MASKED>
-__device__ __forceinline__ half8v block_weights(const float4v (&score)[2], Sums<DC, RT>& s, int t, float scale, uint32_t visible, half8v ones) {
-  float most = -__builtin_inff();
+// The weights' turn: of one tile's eight positions a lane, as the next product's operand.  Of a block that not every row sees all of,
+// `visible` has a bit for each position (4 j + i: position 8 quarter + 4 j + i of the block).
+template <int DC, int RT>
+__device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT>& s, int t, float scale, bool whole, uint32_t visible, half8v ones) {
+  if (!whole) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float v = score[i >> 2][i & 3];
-    most = fmaxf(most, !MASKED || (visible >> i & 1u) ? v : -__builtin_inff());
+    for (int i = 0; i < 8; ++i) score[i >> 2][i & 3] = visible >> i & 1u ? score[i >> 2][i & 3] : -__builtin_inff();
   }
+  float most = score[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) most = fmaxf(most, score[i >> 2][i & 3]);
   most *= scale;
   if (__any(most > s.top[t] + kSlack)) {
     most = max_of_column(most);
@@ -367,13 +370,16 @@ __device__ __forceinline__ half8v block_weights(const float4v (&score)[2], Sums<
   for (int i = 0; i < 4; ++i) {
     float2v e;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], scale, -s.top[t]));
-      if (MASKED) e[k] = visible >> (2 * i + k) & 1u ? e[k] : 0.0f;
-    }
+    for (int k = 0; k < 2; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], scale, -s.top[t]));
     w[i] = __builtin_convertvector(e, half2v);
   }
-  const half8v weight = join(w[0], w[1], w[2], w[3]);
+  half8v weight = join(w[0], w[1], w[2], w[3]);
+  if (!whole) {                                  // (where a row has seen nothing yet its weights are no numbers)
+    u32x4 m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = (visible >> (2 * i) & 1u ? 0x0000ffffu : 0u) | (visible >> (2 * i + 1) & 1u ? 0xffff0000u : 0u);
+    weight = masked(weight, m);
+  }
   s.total[t] = mfma(ones, weight, s.total[t]);
   return weight;
 }
@@ -426,7 +432,7 @@ __device__ __forceinline__ void load_queries(const Params& p, const Place& w, in
   for (int t = 0; t < RT; ++t) {
     const int r = row + 16 * t + column;
     const bool live = r < w.rows;
-    const int token = live ? r / p.shared : 0;
+    const int token = live ? token_of(p, r) : 0;
     const _Float16* q = p.q + (int64_t)(w.row_first + token) * p.q_stride + ((int64_t)w.head * p.shared + (live ? r - token * p.shared : 0)) * (DC * 32);
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
@@ -454,7 +460,6 @@ __device__ __forceinline__ u32x4 existing_places(int place, int limit) {
   for (int i = 0; i < 4; ++i) m[i] = (place + 2 * i < limit ? 0x0000ffffu : 0u) | (place + 2 * i + 1 < limit ? 0xffff0000u : 0u);
   return m;
 }
-__device__ __forceinline__ half8v masked(half8v v, u32x4 mask) { return __builtin_bit_cast(half8v, __builtin_bit_cast(u32x4, v) & mask); }
 // Zero, or a NaN where some of v is not finite.
 __device__ __forceinline__ half8v oddness(half8v v, half8v sum) {
   const half8v zero = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -467,19 +472,17 @@ __device__ __forceinline__ bool any_odd(half8v sum) {
   for (int i = 0; i < 8; ++i) odd |= t[i] != t[i];
   return __any(odd);
 }
-// A weight of zero must not meet an infinity or a NaN: where a block that some rows do not see has any, what is not finite is taken
-// out of the operand (returned) and counted for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there are at most 32 of
-// each); they get it added.
+// A weight of zero must not meet an infinity or a NaN: of a block that not every row sees all of, what is not finite is taken out of
+// the values, after this has counted it for the rows that see it: +inf as 1, -inf as 64, NaN as 4096 (there are at most
+// 32 of each), which get it added.
 template <int DC, int RT>
-__device__ __forceinline__ half8v take_odd(half8v v, const uint32_t (&visible)[RT], Sums<DC, RT>& s, int u) {
+__device__ __forceinline__ void add_odd(half8v v, const uint32_t (&visible)[RT], Sums<DC, RT>& s, int u) {
+  __builtin_amdgcn_sched_barrier(0);             // (seldom run: one tile after the other, for the sake of the registers)
   half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t bits = bits_of(v[i]);
-    if ((bits & 0x7c00u) == 0x7c00u) {
-      odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
-      v[i] = (_Float16)0;
-    }
+    if ((bits & 0x7c00u) == 0x7c00u) odd[i] = (_Float16)((bits & 0x3ffu) ? 4096.0f : (bits & 0x8000u ? 64.0f : 1.0f));
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -494,6 +497,10 @@ __device__ __forceinline__ half8v take_odd(half8v v, const uint32_t (&visible)[R
       s.out[t][u][i] += nan ? __builtin_nanf("") : (plus ? __builtin_inff() : (minus ? -__builtin_inff() : 0.0f));
     }
   }
+}
+__device__ __forceinline__ half8v finite_only(half8v v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (bits_of(v[i]) & 0x7c00u) == 0x7c00u ? (_Float16)0 : v[i];
   return v;
 }
 
@@ -515,81 +522,79 @@ __device__ __forceinline__ Params arguments_again() {
 // that took different rows.  The parts' sums meet in LDS in their order, then the splits' through memory.
 template <int DC, int RT, int GROUPS_R, int PARTS>
 struct Ending {
-  static constexpr int kRows = 16 * RT * GROUPS_R, kThreads = 64 * GROUPS_R * PARTS, kDim = DC * 32;
-  // Units of channels that meet at a time: what 40 KB hold, or 72 KB where a workgroup has the compute unit to itself.
-  static constexpr int kFit = (PARTS * kRows <= 64 ? 40960 : 73728) / (PARTS * kRows * 128 + PARTS * kRows * 24);
-  static constexpr int kMeet = kFit >= DC ? DC : (kFit >= 4 && DC % 4 == 0 ? 4 : (kFit >= 3 && DC % 3 == 0 ? 3 : (kFit >= 2 && DC % 2 == 0 ? 2 : 1)));
-  static constexpr int kPitch = kMeet * 32 + 4;
+  static constexpr int kRows = 16 * RT * GROUPS_R, kThreads = 64 * GROUPS_R * PARTS, kDim = DC * 32, kPitch = kDim + 4;
   static constexpr bool kLastAdds = kRows == 16;
-  static constexpr int kMeetFloats = PARTS * kRows * (kPitch + 2);
+  static constexpr int kMeetFloats = PARTS * kRows * (kPitch + 3) + 2 * kRows;
   static constexpr int kJoinFloats = kLastAdds ? 2 * kRows * kMostSplits + kRows + kThreads * 4 : 0;
   static constexpr int kFloats = kMeetFloats > kJoinFloats ? kMeetFloats : kJoinFloats;
 };
 template <int DC, int RT, int GROUPS_R, int PARTS>
 __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, float* lds, Sums<DC, RT>& s, int group, int part, int lane) {
   using E = Ending<DC, RT, GROUPS_R, PARTS>;
-  constexpr int kRows = E::kRows, kThreads = E::kThreads, kDim = E::kDim, kMeet = E::kMeet, kPitch = E::kPitch;
+  constexpr int kRows = E::kRows, kThreads = E::kThreads, kDim = E::kDim, kPitch = E::kPitch, kFours = kDim / 4;
   const int column = lane & 15, quarter = lane >> 4;
-  float* sums = lds;                            // [PARTS][kRows][kPitch]
-  float* tops = lds + PARTS * kRows * kPitch;   // [PARTS][kRows]
-  float* totals = tops + PARTS * kRows;
+  float* sums = lds;                                                              // [PARTS][kRows][kPitch]
+  float2v* ends = reinterpret_cast<float2v*>(lds + PARTS * kRows * kPitch);       // [PARTS][kRows]: top, total
+  float* factors = reinterpret_cast<float*>(ends + PARTS * kRows);                // [PARTS][kRows]
+  float2v* row_ends = reinterpret_cast<float2v*>(factors + PARTS * kRows);        // [kRows]
   const int live_rows = min(w.rows - w.row0, kRows), mine0 = 16 * RT * group + column;   // (the lane's first row)
   if (quarter == 0) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      tops[part * kRows + mine0 + 16 * t] = s.top[t];
-      totals[part * kRows + mine0 + 16 * t] = s.total[t][0];
+      ends[part * kRows + mine0 + 16 * t][0] = s.top[t];
+      ends[part * kRows + mine0 + 16 * t][1] = s.total[t][0];
     }
   }
   __syncthreads();
-  if constexpr (PARTS > 1) {
+  constexpr int kLanes = PARTS <= 1 ? 1 : (PARTS <= 2 ? 2 : (PARTS <= 4 ? 4 : (PARTS <= 8 ? 8 : 16)));      // a row's parts side by side
+  static_assert(kRows * kLanes <= kThreads, "");
+  if ((int)threadIdx.x < kRows * kLanes) {
+    const int row = threadIdx.x / kLanes, k = threadIdx.x % kLanes;
+    float2v end = {-__builtin_inff(), 0.0f};
+    if (k < PARTS) end = ends[k * kRows + row];
+    float raised = end[0];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      float raised = -__builtin_inff();
+    for (int d = kLanes / 2; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, kLanes));
+    const float factor = part_factor(end[0], raised, end[1]);
+    float total = factor * end[1];
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k) raised = fmaxf(raised, tops[k * kRows + mine0 + 16 * t]);
-      const float factor = part_factor(s.top[t], raised, s.total[t][0]);
+    for (int d = kLanes / 2; d >= 1; d >>= 1) total += __shfl_xor(total, d, kLanes);
+    if (k < PARTS) factors[k * kRows + row] = factor;
+    if (k == 0) row_ends[row] = (float2v){raised, total};
+  }
+  __syncthreads();
 #pragma unroll
-      for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= factor;
+  for (int t = 0; t < RT; ++t) {
+    const int row = mine0 + 16 * t;
+    if (row < live_rows) {
+      const float factor = factors[part * kRows + row];
+#pragma unroll
+      for (int u = 0; u < 2 * DC; ++u) *reinterpret_cast<float4v*>(&sums[(part * kRows + row) * kPitch + 16 * u + 4 * quarter]) = s.out[t][u] * factor;
     }
   }
+  __syncthreads();
   float* mine = partial_of(p, w, blockIdx.x, kDim);
   const int64_t split_floats = (int64_t)p.partial_rows * (kDim + 2);
   const Buffer through = buffer_of(mine, split_floats);
+#pragma unroll 1
+  for (int i = threadIdx.x; i < live_rows * kFours; i += kThreads) {              // a thread takes four channels
+    const int row = i / kFours, d = i % kFours * 4;
+    float4v a = *reinterpret_cast<const float4v*>(&sums[row * kPitch + d]);
 #pragma unroll
-  for (int m = 0; m < DC / kMeet; ++m) {
-    if (m > 0) __syncthreads();
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-      if (mine0 + 16 * t < live_rows) {
-#pragma unroll
-        for (int u = 0; u < 2 * kMeet; ++u)
-          *reinterpret_cast<float4v*>(&sums[(part * kRows + mine0 + 16 * t) * kPitch + 16 * u + 4 * quarter]) = s.out[t][2 * kMeet * m + u];
-      }
-    __syncthreads();
-    constexpr int kFours = kMeet * 8;           // a thread takes four channels
-    for (int i = threadIdx.x; i < live_rows * kFours; i += kThreads) {
-      const int row = i / kFours, d = i % kFours * 4;
-      float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int k = 0; k < PARTS; ++k) a += *reinterpret_cast<const float4v*>(&sums[(k * kRows + row) * kPitch + d]);
-      if (w.active > 1) {
-        if constexpr (E::kLastAdds)
-          store4(through, row * kDim + m * kMeet * 32 + d, a);
-        else
-          *reinterpret_cast<float4v*>(mine + row * kDim + m * kMeet * 32 + d) = a;
-      } else {
-        store_row(p, w.row_first, w.head, w.row0 + row, kDim, m * kMeet * 32 + d, a, row_ends<PARTS, kRows>(tops, totals, row)[1]);
-      }
-    }
+    for (int k = 1; k < PARTS; ++k) a += *reinterpret_cast<const float4v*>(&sums[(k * kRows + row) * kPitch + d]);
+    if (w.active == 1)
+      store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_ends[row][1]);
+    else if (E::kLastAdds)
+      store4(through, row * kDim + d, a);
+    else
+      *reinterpret_cast<float4v*>(mine + row * kDim + d) = a;
   }
   if (w.active == 1) return;
-  for (int row = threadIdx.x; row < live_rows; row += kThreads) {
-    const float2v end = row_ends<PARTS, kRows>(tops, totals, row);
-    if constexpr (E::kLastAdds)
-      store2(through, p.partial_rows * kDim + 2 * row, end);
+  if ((int)threadIdx.x < live_rows) {
+    if (E::kLastAdds)
+      store2(through, p.partial_rows * kDim + 2 * threadIdx.x, row_ends[threadIdx.x]);
     else
-      *reinterpret_cast<float2v*>(mine + p.partial_rows * kDim + 2 * row) = end;
+      *reinterpret_cast<float2v*>(mine + p.partial_rows * kDim + 2 * threadIdx.x) = row_ends[threadIdx.x];
   }
   if constexpr (E::kLastAdds) {
     uint32_t* last = reinterpret_cast<uint32_t*>(lds);            // (what was there has been added)
@@ -599,42 +604,45 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
     if (threadIdx.x == 0)
       *last = __hip_atomic_fetch_add(p.counters + unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w.active - 1) ? 1u : 0u;
     __syncthreads();
-    const bool mine_to_do = *last != 0u;
+    const bool adds = *last != 0u;
     __syncthreads();
-    if (!mine_to_do) return;
+    if (!adds) return;
     const Buffer all = buffer_of(partial_of(p, w, 0, kDim), p.splits * split_floats);
-    float2v* ends = reinterpret_cast<float2v*>(lds);              // [live_rows][active]: top and total, then factor and total
+    float2v* split_ends = reinterpret_cast<float2v*>(lds);        // [live_rows][active]: top and total, then factor and total
     float* row_total = lds + 2 * kRows * kMostSplits;             // [kRows]
     float* shares = row_total + kRows;                            // [kThreads][4]
     // An item is four channels of a row; where there are fewer items than threads, several threads share one's splits.  The first
     // loads of an item do not wait for the splits' factors.
-    constexpr int kFours = kDim / 4, kAhead = 8;
+    constexpr int kAhead = 8;
     const int items = live_rows * kFours;
     int sharers = 1;
     while (sharers < 16 && 2 * sharers * items <= kThreads && 2 * sharers <= w.active) sharers *= 2;
-    const int side = kThreads / sharers, share = threadIdx.x / side;
+    const int side = kThreads / sharers, share = threadIdx.x / side, place = threadIdx.x - share * side;
     float4v ahead[kAhead];
     auto load_ahead = [&](int i, int split) {
-      const int at = i / kFours * kDim + i % kFours * 4;
+      const int at = min(i, items - 1) * 4;                       // row * kDim + d
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (i < items && split + k * sharers < w.active) ahead[k] = load4(all, (int)((split + k * sharers) * split_floats) + at);
+      for (int k = 0; k < kAhead; ++k) ahead[k] = load4(all, min(split + k * sharers, w.active - 1) * (int)split_floats + at);
     };
-    load_ahead(threadIdx.x - share * side, share);
+    load_ahead(place, share);
+#pragma unroll 1
     for (int i = threadIdx.x; i < live_rows * w.active; i += kThreads) {
       const int split = i / live_rows, row = i - split * live_rows;
-      ends[row * w.active + split] = load2(all, (int)(split * split_floats) + p.partial_rows * kDim + 2 * row);
+      split_ends[row * w.active + split] = load2(all, split * (int)split_floats + p.partial_rows * kDim + 2 * row);
     }
     __syncthreads();
+#pragma unroll 1
     for (int row = threadIdx.x >> 4; row < live_rows; row += kThreads / 16) {      // sixteen lanes a row
       float raised = -__builtin_inff(), sum = 0.0f;
-      for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, ends[row * w.active + i][0]);
+#pragma unroll 1
+      for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, split_ends[row * w.active + i][0]);
 #pragma unroll
       for (int d = 8; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, 16));
+#pragma unroll 1
       for (int i = column; i < w.active; i += 16) {
-        const float2v end = ends[row * w.active + i];
+        const float2v end = split_ends[row * w.active + i];
         const float factor = part_factor(end[0], raised, end[1]);
-        ends[row * w.active + i][0] = factor;
+        split_ends[row * w.active + i][0] = factor;
         sum += factor * end[1];
       }
 #pragma unroll
@@ -642,27 +650,25 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
       if (column == 0) row_total[row] = sum;
     }
     __syncthreads();
+#pragma unroll 1
     for (int base = 0; base < items; base += side) {
-      const int i = base + threadIdx.x - share * side;
-      const int row = i / kFours, d = i % kFours * 4;
-      const bool item = i < items;
+      const int i = base + place, row = min(i, items - 1) / kFours;
       float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
       for (int split = share; split < w.active; split += kAhead * sharers) {
         if (base > 0 || split != share) load_ahead(i, split);
-        if (item) {
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k)
-            if (split + k * sharers < w.active) a += ahead[k] * ends[row * w.active + split + k * sharers][0];
-        }
+        for (int k = 0; k < kAhead; ++k)
+          if (split + k * sharers < w.active) a += ahead[k] * split_ends[row * w.active + split + k * sharers][0];
       }
       if (sharers > 1) {
         __syncthreads();
         *reinterpret_cast<float4v*>(&shares[threadIdx.x * 4]) = a;
         __syncthreads();
-        if (item && share == 0)
+        if (share == 0)
           for (int k = 1; k < sharers; ++k) a += *reinterpret_cast<const float4v*>(&shares[(threadIdx.x + k * side) * 4]);
       }
-      if (item && share == 0) store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_total[row]);
+      if (i < items && share == 0) store_row(p, w.row_first, w.head, w.row0 + row, kDim, i % kFours * 4, a, row_total[row]);
     }
     if (threadIdx.x == 0) __hip_atomic_store(p.counters + unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
@@ -727,24 +733,56 @@ __global__ __launch_bounds__(kJoinThreads) void lutgemm_attention_join_kernel(Pa
   store_row(p, w.row_first, w.head, w.row0 + row, DIM, 4 * lane, a, total);
 }
 
-// Whether a block's values have any that is not finite among those that exist.  Of quantised ones the scales say so: what they span
-// is looked at, which also takes in scales that no finite values have.
-template <int BITS, int DC, int GU>
-__device__ __forceinline__ bool values_odd(const ValueWords<BITS, DC, GU>& v, u32x4 exist) {
+// The values of a block that not every row sees all of: those that do not exist become zero, and those that are not finite are
+// added to the rows that see them and become zero.  Of quantised ones the scales say which they are.
+template <int BITS, int DC, int GU, int RT>
+__device__ __forceinline__ void mask_values(ValueWords<BITS, DC, GU>& v, int place, int limit, const uint32_t (&visible)[RT], Sums<DC, RT>& s) {
+  const u32x4 exist = existing_places(place, limit);
   half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
   if constexpr (BITS == 16) {
 #pragma unroll
-    for (int u = 0; u < 2 * DC; ++u) odd = oddness(masked(value_operand<BITS, DC, GU>(v, u / 2, u % 2), exist), odd);
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v.unit[c].w[i] &= exist[i & 3];
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) odd = oddness(value_operand<BITS, DC, GU>(v, u / 2, u % 2), odd);
   } else {
-    const u32x4 positive = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
 #pragma unroll
     for (int g = 0; g < DC / GU; ++g) {
-      half8v span = masked(v.scale[g], positive & exist) * (_Float16)(BITS == 8 ? 128.0f : 16.0f);
-      if constexpr (BITS == 4) span += masked(v.offset[g], positive & exist);
-      odd = oddness(span, odd);
+      v.scale[g] = masked(v.scale[g], exist);
+      odd = oddness(v.scale[g], odd);
+      if constexpr (BITS == 4) {
+        v.offset[g] = masked(v.offset[g], exist);
+        odd = oddness(v.offset[g], odd);
+      }
     }
   }
-  return any_odd(odd);
+  if (__builtin_expect(any_odd(odd), 0)) {
+#pragma unroll
+    for (int u = 0; u < 2 * DC; ++u) add_odd<DC, RT>(value_operand<BITS, DC, GU>(v, u / 2, u % 2), visible, s, u);
+    if constexpr (BITS == 16) {
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const u32x4 w = __builtin_bit_cast(u32x4, finite_only(value_operand<BITS, DC, GU>(v, c, j)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v.unit[c].w[4 * j + i] = w[i];
+        }
+    } else {
+      // a scale or an offset that is not finite makes all it stands for so: both go
+#pragma unroll
+      for (int g = 0; g < DC / GU; ++g) {
+        const half8v both_sum = oddness(v.scale[g], oddness(BITS == 4 ? v.offset[BITS == 4 ? g : 0] : v.scale[g], (half8v){0, 0, 0, 0, 0, 0, 0, 0}));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool gone = both_sum[i] != both_sum[i];
+          v.scale[g][i] = gone ? (_Float16)0 : v.scale[g][i];
+          if constexpr (BITS == 4) v.offset[g][i] = gone ? (_Float16)0 : v.offset[g][i];
+        }
+      }
+    }
+  }
 }
 
 // Address of a block's codes: of the page that `page` numbers (0 where there is none: its values are not used).
@@ -770,16 +808,11 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS,
   __shared__ __attribute__((aligned(16))) float lds[Ending<DC, RT, 1, WAVES>::kFloats];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
   // The page table does not wait for the sequence's lengths (a split begins elsewhere only if it is longer than planned).
-  Walk<WAVES> walk;
-  walk.table = p.table + (int64_t)blockIdx.z * p.table_pages;
-  walk.pages = p.pages;
-  walk.table_pages = p.table_pages;
-  walk.page_blocks = p.page_blocks;
   const int planned = (int)min((int64_t)blockIdx.x * (p.chunk / kBlock), (int64_t)p.table_pages * p.page_blocks) + wave;
-  walk_begin(walk, planned, lane);
+  Walk<WAVES> walk = walk_of<WAVES>(p, blockIdx.z, planned);
   Place w;
   if (!find_place(p, 16 * RT, blockIdx.x, &w)) return;
-  if (w.first_block + wave != planned) walk_begin(walk, w.first_block + wave, lane);
+  if (w.first_block + wave != planned) walk_begin(walk, w.first_block + wave);
 
   Sums<DC, RT> s;
   clear_sums(s);
@@ -791,96 +824,65 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS,
   ValueWords<BITS, DC, GU> values[kSets];
   uint64_t sees[RT];
 
-  // Blocks that every row sees all of: the past but for its last few positions.
-  const int whole_end = min(w.past / kBlock, w.end_block);
-  int block = w.first_block + wave;           // the next to be worked on
-  int ahead = block;                          // the next to be asked for
-  bool dead[kSets];
-  const char* at = nullptr;
-  auto find = [&](int set) {                  // the block `ahead`
-    if (ahead != w.first_block + wave) walk_on(walk, lane);
-    const int page = walk_page(walk);
-    dead[set] = page < 0;
-    at = block_address(blocks, page, walk.in_page);
-    ahead += WAVES;
-  };
-  if (ahead < whole_end) {
-    find(0);
-    load_keys<BITS, DC, GU>(keys[0], at, lane);
-    load_values<BITS, DC, GU>(values[0], at + value_offset, lane);
-  }
-  load_queries<DC, RT>(p, w, w.row0, lane, s, sees);
-
-  // First the others, in the last set: the last positions of the past, the new ones, and what is behind them in the last block.
-  for (int b = block < whole_end ? block + (whole_end - block + WAVES - 1) / WAVES * WAVES : block; b < w.end_block; b += WAVES) {
-    KeyWords<BITS, DC, GU>& k = keys[kSets - 1];
-    ValueWords<BITS, DC, GU>& v = values[kSets - 1];
-    const int col = b / p.page_blocks;
-    const int listed = col < p.table_pages ? walk.table[col] : -1, page = listed < p.pages ? listed : -1;
-    const char* from = block_address(blocks, page, b - col * p.page_blocks);
-    load_keys<BITS, DC, GU>(k, from, lane);
-    load_values<BITS, DC, GU>(v, from + value_offset, lane);
-    const int place = b * kBlock + 8 * quarter - w.past;                  // of the lane's first position, counted from the new ones
-    const int limit = page < 0 ? -(1 << 30) : (int)(w.length - w.past);   // positions from here on do not exist
-    float4v score[RT][2];
-    block_scores<BITS, DC, GU, RT>(score, k, s);
-    half8v weight[RT];
-    uint32_t visible[RT];
+  // A block's keys are asked for when those kSets blocks before have met the queries, its values when those before have been added.
+  // The fetches are free of branches, so that the compiler knows at every wait how many loads are younger than the one it waits
+  // for: a wavefront that runs out of blocks fetches its last one again.
+  const int whole_end = w.past / kBlock;      // every row sees all of the blocks before it
+  int block = w.first_block + wave;
+  if (block < w.end_block) {
+    bool dead[kSets];
+    const char* at = nullptr;
+    int ahead = block;                        // the next block to be asked for
+    auto find = [&](int set) {
+      if (ahead < w.end_block) {
+        const int page = walk_page(walk);
+        dead[set] = page < 0;
+        at = block_address(blocks, page, walk.in_page);
+        ahead += WAVES;
+        walk_on(walk);
+      }
+      asm("" : "+s"(at));                     // (the same address again is not the same load again)
+    };
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      visible[t] = visible_places(place, limit, sees[t]);
-      weight[t] = block_weights<DC, RT, true>(score[t], s, t, p.scale, visible[t], ones);
-    }
-    const u32x4 exist = existing_places(place, limit);
-    const bool odd = values_odd<BITS, DC, GU>(v, exist);
-#pragma unroll
-    for (int u = 0; u < 2 * DC; ++u) {
-      half8v x = masked(value_operand<BITS, DC, GU>(v, u / 2, u % 2), exist);
-      if (__builtin_expect(odd, 0)) x = take_odd<DC, RT>(x, visible, s, u);
-#pragma unroll
-      for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(x, weight[t], s.out[t][u]);
-    }
-    if (kSets == 1 && block < whole_end && b + WAVES >= w.end_block) {    // (one set only: fetch the first block again)
-      load_keys<BITS, DC, GU>(keys[0], at, lane);
-      load_values<BITS, DC, GU>(values[0], at + value_offset, lane);
-    }
-  }
-#pragma unroll
-  for (int set = 1; set < kSets; ++set)
-    if (ahead < whole_end) {
+    for (int set = 0; set < kSets; ++set) {
       find(set);
       load_keys<BITS, DC, GU>(keys[set], at, lane);
       load_values<BITS, DC, GU>(values[set], at + value_offset, lane);
     }
-  bool more = block < whole_end;
-  while (more) {
+    load_queries<DC, RT>(p, w, w.row0, lane, s, sees);
+    bool more = true;
+    while (more) {
 #pragma unroll
-    for (int set = 0; set < kSets; ++set) {
-      if (!more) break;
-      float4v score[RT][2];
-      block_scores<BITS, DC, GU, RT>(score, keys[set], s);
-      const bool skip = dead[set], again = ahead < whole_end;
-      if (again) {
+      for (int set = 0; set < kSets; ++set) {
+        float4v score[RT][2];
+        block_scores<BITS, DC, GU, RT>(score, keys[set], s);
+        const bool skip = dead[set], whole = block < whole_end;
         find(set);
         load_keys<BITS, DC, GU>(keys[set], at, lane);
-      }
-      if (!skip) {
-        half8v weight[RT];
+        if (!skip) {
+          const int place = block * kBlock + 8 * quarter - w.past;      // of the lane's first position, counted from the new ones
+          const int limit = (int)(w.length - w.past);                   // positions from here on do not exist
+          half8v weight[RT];
+          uint32_t visible[RT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) weight[t] = block_weights<DC, RT, false>(score[t], s, t, p.scale, 0u, ones);
+          for (int t = 0; t < RT; ++t) {
+            visible[t] = 0u;
+            if (!whole) visible[t] = visible_places(place, limit, sees[t]);
+            weight[t] = block_weights<DC, RT>(score[t], s, t, p.scale, whole, visible[t], ones);
+          }
+          if (!whole) mask_values<BITS, DC, GU, RT>(values[set], place, limit, visible, s);
 #pragma unroll
-        for (int c = 0; c < DC; ++c) {
+          for (int u = 0; u < 2 * DC; ++u) {
+            const half8v v = value_operand<BITS, DC, GU>(values[set], u / 2, u % 2);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const half8v v = value_operand<BITS, DC, GU>(values[set], c, j);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) s.out[t][2 * c + j] = mfma(v, weight[t], s.out[t][2 * c + j]);
+            for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
           }
         }
+        load_values<BITS, DC, GU>(values[set], at + value_offset, lane);
+        block += WAVES;
+        more = block < w.end_block;
+        if (!more) break;
       }
-      if (again) load_values<BITS, DC, GU>(values[set], at + value_offset, lane);
-      block += WAVES;
-      more = block < whole_end;
     }
   }
   end_workgroup<DC, RT, 1, WAVES>(arguments_again(), w, lds, s, 0, wave, lane);
@@ -895,7 +897,8 @@ template <int BITS, int DC, int GU, int RT, int GROUPS_R, int PARTS>
 __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_shared_kernel(Params p) {
   constexpr int kEach = (2 * DC + GROUPS_R - 1) / GROUPS_R;        // units of a wavefront
   constexpr int kOperands = 2 * DC * 2 * 1024;                     // bytes of a block's: units x runs
-  constexpr int kDepth = kEach * BITS <= 32 && kEach * DC < 32 ? 2 : 1;               // blocks of codes on their way
+  constexpr int kHeld = kEach >= 4 ? DC : 2 * DC;                  // operands that a wavefront takes from LDS at a time
+  constexpr int kDepth = kEach * BITS <= 32 && DC < 8 ? 2 : 1;             // blocks of codes on their way
   using E = Ending<DC, RT, GROUPS_R, PARTS>;
   constexpr int kBytes = 2 * PARTS * kOperands > E::kFloats * 4 ? 2 * PARTS * kOperands : E::kFloats * 4;
   __shared__ __attribute__((aligned(16))) char lds[kBytes];
@@ -908,57 +911,41 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
   clear_sums(s);
   const half2v one = both((_Float16)1.0f);
   const half8v ones = join(one, one, one, one);
-  Walk<PARTS> walk;
-  walk.table = p.table + (int64_t)w.seq * p.table_pages;
-  walk.pages = p.pages;
-  walk.table_pages = p.table_pages;
-  walk.page_blocks = p.page_blocks;
-  walk_begin(walk, w.first_block + part, lane);
+  Walk<PARTS> walk = walk_of<PARTS>(p, w.seq, w.first_block + part);
   const Blocks blocks = blocks_of(p, w.head);
 
   constexpr int kCode = kBlock * DC * 32 * BITS / 8;
   Unit<BITS> unit[kDepth][kEach];
-  half8v scale[kDepth][BITS == 16 ? 1 : kEach], offset[kDepth][BITS == 4 ? kEach : 1];       // of a value unit; of a key unit in the first words
+  u32x4 scale[kDepth][BITS == 16 ? 1 : kEach], offset[kDepth][BITS == 4 ? kEach : 1];
+  const uint32_t odd_lane = lane & 1 ? ~0u : 0u, upper_lane = lane & 2 ? ~0u : 0u;
   bool dead[2] = {false, false};
   int ahead = w.first_block + part;                                // the next block to be fetched
+  const char* at = blocks.head;                                    // (of page 0: a part without a block fetches that)
   // This wavefront's units of the block `ahead`; `half`: of the LDS, where they are to go.
   auto fetch = [&](const int half) {
     const int set = kDepth == 2 ? half : 0;
-    if (ahead >= w.end_block) return;
-    if (ahead != w.first_block + part) walk_on(walk, lane);
-    const int page = walk_page(walk);
-    dead[half] = page < 0;
-    const char* at = block_address(blocks, page, walk.in_page);
+    if (ahead < w.end_block) {                                     // (else the last one again: the loads are free of branches)
+      const int page = walk_page(walk);
+      dead[half] = page < 0;
+      at = block_address(blocks, page, walk.in_page);
+      ahead += PARTS;
+      walk_on(walk);
+    }
+    asm("" : "+s"(at));                                            // (the same address again is not the same load again)
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int u = group + i * GROUPS_R;
-      if (u >= 2 * DC) continue;
-      const int c = u < DC ? u : u - DC, g = c / GU;
-      const char* half_block = at + (u < DC ? 0 : p.block_bytes / 2);
+      const int u = min(group + i * GROUPS_R, 2 * DC - 1);
+      const bool key = u < DC;
+      const int c = key ? u : u - DC, g = c / GU;
+      const char* half_block = at + (key ? 0 : p.block_bytes / 2);
       load_unit<BITS>(unit[set][i], half_block, c, lane);
-      if constexpr (BITS == 8) {
-        u32x4 v = {0u, 0u, 0u, 0u};
-        if (u < DC)
-          v[0] = reinterpret_cast<const uint32_t*>(half_block + kCode + g * 64)[lane & 15];
-        else
-          v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 64)[lane >> 4];
-        scale[set][i] = __builtin_bit_cast(half8v, v);
-      }
-      if constexpr (BITS == 4) {
-        u32x4 v = {0u, 0u, 0u, 0u}, z = v;
-        if (u < DC) {
-          const u32x2 k = reinterpret_cast<const u32x2*>(half_block + kCode + g * 128)[lane & 15];
-          v[0] = k[0];
-          v[1] = k[1];
-        } else {
-          v = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128)[lane >> 4];
-          z = reinterpret_cast<const u32x4*>(half_block + kCode + g * 128 + 64)[lane >> 4];
-        }
-        scale[set][i] = __builtin_bit_cast(half8v, v);
-        offset[set][i] = __builtin_bit_cast(half8v, z);
+      // Scales: the sixteen bytes that the lane's are among, of a key's or a value's unit by the same loads.
+      if constexpr (BITS != 16) {
+        const char* scales = half_block + kCode + g * (BITS == 8 ? 64 : 128) + (key ? (lane & (BITS == 8 ? 12 : 14)) * (BITS == 8 ? 4 : 8) : (lane >> 4) * 16);
+        scale[set][i] = *reinterpret_cast<const u32x4*>(scales);
+        if constexpr (BITS == 4) offset[set][i] = *reinterpret_cast<const u32x4*>(scales + (key ? 0 : 64));
       }
     }
-    ahead += PARTS;
   };
   auto operands = [&](const int half) { return lds + (half * PARTS + part) * kOperands; };
   // The fetched units of `block`, as operands.
@@ -969,7 +956,7 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int u = group + i * GROUPS_R;
-      if (u >= 2 * DC) continue;
+      if (kEach * GROUPS_R > 2 * DC && u >= 2 * DC) continue;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         half8v v;
@@ -977,10 +964,14 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
           const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
           v = value_values<16>(unit[set][i], j, none, none);
         } else if (u >= DC) {
-          v = value_values<BITS>(unit[set][i], j, scale[set][i], offset[set][BITS == 4 ? i : 0]);
+          v = value_values<BITS>(unit[set][i], j, __builtin_bit_cast(half8v, scale[set][i]), __builtin_bit_cast(half8v, offset[set][BITS == 4 ? i : 0]));
+        } else if constexpr (BITS == 8) {
+          v = key_values<BITS>(unit[set][i], j, half_of(one_of(one_of(word_of<0>(scale[set][i]), word_of<1>(scale[set][i]), odd_lane),
+                                                               one_of(word_of<2>(scale[set][i]), word_of<3>(scale[set][i]), odd_lane), upper_lane), j), (_Float16)0);
         } else {
-          v = BITS == 8 ? key_values<BITS>(unit[set][i], j, scale[set][i][j], (_Float16)0)
-                        : key_values<BITS>(unit[set][i], j, scale[set][i][2 * j], scale[set][i][2 * j + 1]);
+          const uint32_t word = j ? one_of(word_of<1>(scale[set][i]), word_of<3>(scale[set][i]), odd_lane)
+                                  : one_of(word_of<0>(scale[set][i]), word_of<2>(scale[set][i]), odd_lane);
+          v = key_values<BITS>(unit[set][i], j, half_of(word, 0), half_of(word, 1));
         }
         to[(u * 2 + j) * 64] = __builtin_bit_cast(u32x4, v);
       }
@@ -1008,18 +999,29 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
       float4v score[RT][2];
 #pragma unroll
       for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
+      // (All of a half's operands are asked for before the first is used, the values' before the weights are worked out: left alone, the
+      // compiler asks for one or two at a time, and waits for each.)
+      half8v held[kHeld];
 #pragma unroll
-      for (int u = 0; u < 2 * DC; ++u) {
-        const half8v k = from[u * 64];
+      for (int first = 0; first < 2 * DC; first += kHeld) {
 #pragma unroll
-        for (int t = 0; t < RT; ++t) score[t][u % 2] = mfma(k, s.query[t][u / 2], score[t][u % 2]);
+        for (int u = 0; u < kHeld; ++u) held[u] = from[(first + u) * 64];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) score[t][u % 2] = mfma(held[u], s.query[t][(first + u) / 2], score[t][u % 2]);
+        }
       }
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) held[u] = from[(2 * DC + u) * 64];
+      __builtin_amdgcn_sched_barrier(0);
       half8v weight[RT];
       uint32_t visible[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         visible[t] = kMasked ? visible_places(place, limit, sees[t]) : 0u;
-        weight[t] = block_weights<DC, RT, kMasked>(score[t], s, t, p.scale, visible[t], ones);
+        weight[t] = block_weights<DC, RT>(score[t], s, t, p.scale, !kMasked, visible[t], ones);
       }
       u32x4 exist;
       bool rare = false;
@@ -1032,10 +1034,18 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
       }
 #pragma unroll
       for (int u = 0; u < 2 * DC; ++u) {
-        half8v v = from[(2 * DC + u) * 64];
+        if (u > 0 && u % kHeld == 0) {
+#pragma unroll
+          for (int k = 0; k < kHeld; ++k) held[k] = from[(2 * DC + u + k) * 64];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        half8v v = held[u % kHeld];
         if constexpr (kMasked) {
           v = masked(v, exist);
-          if (__builtin_expect(rare, 0)) v = take_odd<DC, RT>(v, visible, s, u);
+          if (__builtin_expect(rare, 0)) {
+            add_odd<DC, RT>(v, visible, s, u);
+            v = finite_only(v);
+          }
         }
 #pragma unroll
         for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
@@ -1147,6 +1157,7 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
   p.page_blocks = cache->page_tokens / kBlock;
   p.heads = cache->heads;
   p.shared = q_heads / cache->heads;
+  p.inverse_shared = 1.0f / (float)p.shared;
   p.block_bytes = block_bytes(cache->head_dim, cache->bits, group);
   p.splits = plan.splits;
   p.chunk = plan.chunk;

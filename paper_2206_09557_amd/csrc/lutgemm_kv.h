@@ -55,7 +55,7 @@ inline int check_step(const lutgemm_kv_step* s) {
 // one wavefront where not even one set does.
 constexpr int attention_registers(int head_dim, int bits, int group, int row_tiles, int sets) {
   const int units = head_dim / 32, scales = bits == 8 ? 5 * (head_dim / group) : (bits == 4 ? 10 * (head_dim / group) : 0);
-  return 30 + row_tiles * (12 * units + 26) + sets * (units * bits + scales) + (bits == 16 ? 5 * units : 0);
+  return 32 + row_tiles * (12 * units + 26) + sets * (units * bits + scales) + (bits == 16 ? 5 * units : 0);
 }
 constexpr int attention_sets(int head_dim, int bits, int group, int row_tiles) {
   const int two = attention_registers(head_dim, bits, group, row_tiles, 2);
@@ -63,7 +63,7 @@ constexpr int attention_sets(int head_dim, int bits, int group, int row_tiles) {
 }
 constexpr int attention_waves_per_simd(int head_dim, int bits, int group, int row_tiles) {
   const int r = attention_registers(head_dim, bits, group, row_tiles, attention_sets(head_dim, bits, group, row_tiles));
-  return r <= 124 ? 4 : (r <= 164 ? 3 : (r <= 252 ? 2 : 1));
+  return r <= 122 ? 4 : (r <= 168 ? 3 : (r <= 252 ? 2 : 1));
 }
 
 // How lutgemm_attention splits its work; see plan_attention in lutgemm_kv_host.cpp.
