@@ -13,9 +13,13 @@ using namespace lutgemm_kv_detail;
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t ushort2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+constexpr int64_t kCacheBytes = 32 << 20;      // of the L2 caches
 
 // ---- rotary positions ----------------------------------------------------------------------------
 
@@ -159,11 +163,7 @@ struct KvParams {
   int64_t k_stride, v_stride;
   int64_t pages;
   int block_bytes, value_offset;       // of a block; of its value half
-  int tokens, seqs, table_pages, page_blocks, heads, group;
-};
-
-struct Codes8 {                // eight values of a run: the bytes of a piece of the layout
-  uint32_t w[4];               // 16 bits: all; 8 bits: two; 4 bits: one (keys), or one nibble a byte in two (values)
+  int tokens, seqs, table_pages, page_blocks, heads;
 };
 
 // Where the tokens of a sequence are, checked against what the host said.
@@ -187,306 +187,450 @@ __device__ __forceinline__ char* block_at(const KvParams& p, int seq, int block,
   return p.pool + (((int64_t)page * p.heads + head) * p.page_blocks + (block - col * p.page_blocks)) * p.block_bytes;
 }
 
-// Lane, run and place of a value in the layout's units.
-__device__ __forceinline__ int key_lane(int place, int g) { return 16 * g + 4 * (place >> 3) + (place & 3); }
-__device__ __forceinline__ int key_run(int place) { return (place >> 2) & 1; }
-
-// Byte of a key piece (eight channels of one place, unit c, quarter g) within the key codes.
-template <int BITS>
-__device__ __forceinline__ int key_piece(int place, int c, int g) {
-  const int lane = key_lane(place, g), j = key_run(place);
-  return BITS == 16 ? ((c * 2 + j) * 64 + lane) * 16 : ((c * 64 + lane) * 2 + j) * BITS;
-}
-// Byte of one value code (channel d of a place; with 4 bits of channels d and d + 16, d % 32 < 16).
-template <int BITS>
-__device__ __forceinline__ int value_byte(int place, int d) {
-  const int c = d >> 5, j = (d >> 4) & 1, lane = 16 * (place >> 3) + (d & 15), e = place & 7;
-  if (BITS == 16) return (((c * 2 + j) * 64 + lane) * 8 + e) * 2;
-  if (BITS == 8) return ((c * 64 + lane) * 2 + j) * 8 + e;
-  return (c * 64 + lane) * 8 + (e & 4) + (((e & 1) << 1) | ((e >> 1) & 1));   // 0 2 1 3
-}
-// Half word of a scale (the offset's, with 4 bits: 1 behind for keys, 32 for values).
-template <int BITS>
-__device__ __forceinline__ int key_scale(int group, int place) {
-  return (BITS == 8 ? 1 : 2) * (group * 32 + (4 * (place >> 3) + (place & 3)) * 2 + key_run(place));
-}
-template <int BITS>
-__device__ __forceinline__ int value_scale(int group, int place) {
-  return (BITS == 8 ? 32 : 64) * group + place;
-}
-
 // (By value: a bit cast of a vector's element in place takes the vector's first.)
 __device__ __forceinline__ uint32_t bits_of(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
+__device__ __forceinline__ _Float16 half_of(uint32_t bits) { return __builtin_bit_cast(_Float16, (uint16_t)bits); }
 
-// What a run of eight values adds to its group's statistics.
-struct Stats {
-  uint32_t magnitude;          // largest bits of |x|: infinities and NaNs come out on top
-  _Float16 low, high;
+// Both kernels give a wavefront the keys of 32 positions of a head, or the values.  A lane has runs of eight channels: run `quarter` of
+// every unit of 32 channels, of two places, 4 apart.  In memory that is 64 bytes of a row for each four lanes, which are also
+// what a group's statistics need first; and both places' codes of a key lie side by side in the cache, so that keys
+// pass through no LDS.
+struct Seat {
+  int quarter, place[2];       // place of run j in the block
+  int lane;                    // of the layout's units: where its keys are
 };
-__device__ __forceinline__ Stats stats_of(const half8 x) {
-  Stats s = {0u, x[0], x[0]};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s.magnitude = max(s.magnitude, bits_of(x[i]) & 0x7fffu);
-    s.low = x[i] < s.low ? x[i] : s.low;
-    s.high = x[i] > s.high ? x[i] : s.high;
-  }
+__device__ __forceinline__ Seat seat_of(int lane) {
+  const int r = lane >> 2 & 3, eight = lane >> 4;
+  return {lane & 3, {8 * eight + r, 8 * eight + r + 4}, 16 * (lane & 3) + 4 * eight + r};
+}
+
+// The block of this wavefront and its live places.
+struct Span {
+  char* base;                  // of its keys or values; null: there is no page
+  int64_t row0;                // row of place 0
+  int from, to;                // live places; from >= to: nothing to do
+  bool whole;
+};
+__device__ __forceinline__ Span span_of(const KvParams& p, int value) {
+  const Rows rows = rows_of(p, blockIdx.z);
+  const int64_t end = (int64_t)rows.past + rows.count, block = rows.past / kBlock + (int64_t)blockIdx.x;
+  Span s = {nullptr, rows.row + block * kBlock - rows.past, 0, 0, false};
+  if (block * kBlock >= end || rows.count == 0) return s;
+  s.from = (int)max(rows.past - block * kBlock, (int64_t)0);
+  s.to = (int)min(end - block * kBlock, (int64_t)kBlock);
+  s.base = block > INT32_MAX ? nullptr : block_at(p, blockIdx.z, (int)block, blockIdx.y);
+  if (s.base && value) s.base += p.value_offset;
+  s.whole = s.from == 0 && s.to == kBlock && !p.rows;
   return s;
 }
-__device__ __forceinline__ Stats joined(Stats a, Stats b) {
-  a.magnitude = max(a.magnitude, b.magnitude);
-  a.low = b.low < a.low ? b.low : a.low;
-  a.high = b.high > a.high ? b.high : a.high;
-  return a;
+
+// Most of the four lanes that hold a unit's runs.
+__device__ __forceinline__ uint32_t other_lane(uint32_t v, bool two) {
+  return two ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true) : (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true);
 }
-// A group's scale and offset.  fp32 division is IEEE's here, as it is in what checks it.
-template <int BITS>
-__device__ __forceinline__ void scale_of_group(Stats s, _Float16* scale, _Float16* offset) {
-  const float range = BITS == 8 ? (float)__builtin_bit_cast(_Float16, (uint16_t)s.magnitude) / 127.0f : ((float)s.high - (float)s.low) / 15.0f;
-  const auto down = __builtin_amdgcn_cvt_pkrtz(range, 0.0f);   // towards zero
-  const bool bad = s.magnitude >= 0x7c00u;
-  *scale = bad ? __builtin_bit_cast(_Float16, (uint16_t)0x7e00u) : (_Float16)down[0];
-  *offset = s.low;
+__device__ __forceinline__ uint32_t most_of(uint32_t a, uint32_t b) {        // of both 16-bit halves
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
 }
-template <int BITS>
-__device__ __forceinline__ uint32_t code_of(_Float16 x, float scale, float offset) {
-  if (BITS == 8) {
-    const float u = scale > 0.0f ? rintf((float)x / scale) : 0.0f;
-    return (uint32_t)((int)fminf(fmaxf(u, -127.0f), 127.0f) + 128);
-  }
-  const float u = scale > 0.0f ? rintf(((float)x - offset) / scale) : 0.0f;
-  return (uint32_t)(int)fminf(fmaxf(u, 0.0f), 15.0f);
+// (NaN if either is.)
+__device__ __forceinline__ half2v most_of(half2v a, half2v b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ half2v least_of(half2v a, half2v b) { return __builtin_elementwise_minimum(a, b); }
+
+// Correctly rounded n / d for a d of at most 11 bits, by its correctly rounded reciprocal: the quotient's error, which is exact, times the
+// reciprocal is right to far less than the 2^-12 of a last place that such a quotient is away from the middle of two numbers.
+__device__ __forceinline__ float divided(float n, float d, float reciprocal) {
+  const float q = n * reciprocal;
+  return fmaf(fmaf(-q, d, n), reciprocal, q);
 }
-template <int BITS>
-__device__ __forceinline__ _Float16 value_of(uint32_t code, _Float16 scale, _Float16 offset) {
-  if (BITS == 8) return scale * (_Float16)(int)(code - 128);              // one rounding each
-  return __builtin_elementwise_fma(scale, (_Float16)(int)code, offset);
+__device__ __forceinline__ float reciprocal_of(float d) {                    // 0 for 0
+  const float r = __builtin_amdgcn_rcpf(d);
+  return d > 0.0f ? fmaf(fmaf(-d, r, 1.0f), r, r) : 0.0f;
 }
 
-constexpr int kKvThreads = 256;
+// A group's scale and offset, ready for use.
+struct Group {
+  float scale, reciprocal, offset;
+  _Float16 scale_bits, offset_bits;      // as stored
+  bool bad;                              // it holds an infinity or a NaN
+};
+// With 8 bits the largest |x| as bits (infinities and NaNs come out on top); with 4 the largest -x and x (NaNs come through).
+template <int BITS>
+__device__ __forceinline__ Group group_of_ends(uint32_t magnitude, half2v ends) {
+  Group g;
+  g.bad = BITS == 8 ? magnitude >= 0x7c00u : !((float)ends[0] < __builtin_inff() && (float)ends[1] < __builtin_inff());
+  const float range = BITS == 8 ? divided((float)half_of(magnitude), 127.0f, 1.0f / 127.0f) : divided((float)ends[1] + (float)ends[0], 15.0f, 1.0f / 15.0f);
+  const auto down = __builtin_amdgcn_cvt_pkrtz(range, 0.0f);                 // towards zero
+  const _Float16 scale = (_Float16)down[0];
+  g.scale = g.bad ? 0.0f : (float)scale;
+  g.reciprocal = reciprocal_of(g.scale);
+  g.scale_bits = g.bad ? half_of(0x7e00u) : scale;
+  g.offset_bits = g.bad ? (_Float16)0.0f : -ends[0];
+  g.offset = (float)g.offset_bits;
+  return g;
+}
+// A code in the low bits of a float's: adding 3 * 2^22 rounds to a whole number, to even.
+// With 8 bits x / s, both of 11 bits, is either midway between two whole numbers or more than 2^-12.1 from it.  Rounded to
+// 2^-13 (by adding 3 * 2^9) x times the reciprocal keeps its side of the middle, or is the middle: that saves the quotient's correction.
+// With 4 bits x - z may have more bits than 11, and the quotient is worked out.
+constexpr float kWhole = 12582912.0f, kGrid = 1536.0f;
+template <int BITS>
+__device__ __forceinline__ uint32_t code_of(_Float16 x, const Group& g) {
+  const float least = BITS == 8 ? kWhole - 127.0f : kWhole, most = BITS == 8 ? kWhole + 127.0f : kWhole + 15.0f;
+  const float u = BITS == 8 ? fmaf((float)x, g.reciprocal, kGrid) + (kWhole - kGrid) : divided((float)x - g.offset, g.scale, g.reciprocal) + kWhole;
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(u, least, most));
+}
+__device__ __forceinline__ uint32_t bytes_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {       // their low bytes, a's lowest
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
+constexpr int kKvThreads = 128;          // two wavefronts: keys and values
 
 // Writes the block of 32 positions that blockIdx.x counts from the one with the sequence's first new position, for one
-// head.  An item is a run of eight channels of one place, of the key or of the value; what quantising needs of the
-// whole group goes through LDS.  Codes are put together in LDS in the layout's order and copied out 16 or 8 bytes a
-// thread: values are transposed on the way, and whole lines leave together.
-template <int BITS, int DIM>
+// head.  Values are transposed on the way, through LDS; whole units leave together, 16 bytes a lane.  Of a block that holds others'
+// positions too only the live places' codes are stored, to the byte.
+template <int BITS, int DC, int GU>
 __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p) {
-  constexpr int kRuns = DIM / 8;                    // of a place
-  constexpr int kItems = 2 * kBlock * kRuns;
-  constexpr int kEach = (kItems + kKvThreads - 1) / kKvThreads;
-  constexpr int kCode = kBlock * DIM * BITS / 8;
-  __shared__ __attribute__((aligned(16))) unsigned char codes[2 * kCode];
-  __shared__ Stats stats[BITS == 16 ? 1 : kItems];
-  const int seq = blockIdx.z, head = blockIdx.y;
-  const Rows rows = rows_of(p, seq);
-  const int64_t end = (int64_t)rows.past + rows.count;
-  const int64_t block = rows.past / kBlock + (int64_t)blockIdx.x;
-  if (block * kBlock >= end || rows.count == 0 || block > INT32_MAX) return;
-  char* base = block_at(p, seq, (int)block, head);
-  if (!base) return;
-  const int from = (int)max(rows.past - block * kBlock, (int64_t)0), to = (int)min(end - block * kBlock, (int64_t)kBlock);   // live places
-  const int64_t row0 = rows.row + block * kBlock - rows.past;   // of place 0
+  constexpr int kCode = kBlock * DC * 4 * BITS;
+  constexpr int kPitch = DC * 4 * BITS + 16;        // of a row of codes in LDS
+  __shared__ __attribute__((aligned(16))) unsigned char codes[kBlock * kPitch];
+  const int lane = threadIdx.x & 63, value = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const _Float16* source = static_cast<const _Float16*>(value ? p.v : p.k);
+  const int64_t stride = value ? p.v_stride : p.k_stride;
+  if (!source) return;
+  const Span span = span_of(p, value);
+  if (!span.base) return;
+  const Seat seat = seat_of(lane);
 
-  half8 x[kEach];
-  bool live[kEach];
+  u32x4 x[DC][2];
+  bool live[2];
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
-    const int item = threadIdx.x + k * kKvThreads;
-    const int value = item / (kBlock * kRuns), place = item / kRuns % kBlock, run = item % kRuns;
-    live[k] = item < kItems && place >= from && place < to && (value ? p.v : p.k) != nullptr;
-    int64_t row = row0 + place;
-    if (live[k] && p.rows) {
+  for (int j = 0; j < 2; ++j) {
+    live[j] = seat.place[j] >= span.from && seat.place[j] < span.to;
+    int64_t row = span.row0 + min(max(seat.place[j], span.from), span.to - 1);      // (a dead place's lane reads a live one's row)
+    if (p.rows) {
       row = p.rows[row];
-      live[k] = row >= 0;
+      live[j] = live[j] && row >= 0;
     }
-    const half8 none = {0, 0, 0, 0, 0, 0, 0, 0};
-    x[k] = none;
-    if (live[k])
-      x[k] = *reinterpret_cast<const half8*>(static_cast<const _Float16*>(value ? p.v : p.k) + row * (value ? p.v_stride : p.k_stride) +
-                                             (int64_t)head * DIM + run * 8);
-    if (BITS != 16 && item < kItems) stats[item] = stats_of(x[k]);
-  }
-  if (BITS != 16) __syncthreads();
+    const u32x4* from = reinterpret_cast<const u32x4*>(source + row * stride + (int64_t)blockIdx.y * DC * 32 + seat.quarter * 8);
+    if (!p.rows || row >= 0) {
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
-    const int item = threadIdx.x + k * kKvThreads;
-    const int value = item / (kBlock * kRuns), place = item / kRuns % kBlock, run = item % kRuns;
-    if (!live[k]) continue;
-    uint32_t u[8];
-    if constexpr (BITS != 16) {
-      const int runs = p.group / 8, g0 = run / runs * runs;
-      Stats s = stats[item - run + g0];
-      for (int i = 1; i < runs; ++i) s = joined(s, stats[item - run + g0 + i]);
-      _Float16 scale, offset;
-      scale_of_group<BITS>(s, &scale, &offset);
-      if (run == g0) {
-        _Float16* scales = reinterpret_cast<_Float16*>(base + (value ? p.value_offset : 0) + kCode);
-        const int at = value ? value_scale<BITS>(run / runs, place) : key_scale<BITS>(run / runs, place);
-        scales[at] = scale;
-        if (BITS == 4) scales[at + (value ? 32 : 1)] = offset;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = code_of<BITS>(x[k][i], (float)scale, (float)offset);
+      for (int c = 0; c < DC; ++c) x[c][j] = __builtin_nontemporal_load(from + c * 4);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = bits_of(x[k][i]);
+      for (int c = 0; c < DC; ++c) x[c][j] = (u32x4){0u, 0u, 0u, 0u};
     }
-    unsigned char* to_lds = codes + value * kCode;
-    if (!value) {
-      uint32_t* w = reinterpret_cast<uint32_t*>(to_lds + key_piece<BITS>(place, run >> 2, run & 3));
+  }
+
+  _Float16* scales = reinterpret_cast<_Float16*>(span.base + kCode);
+#pragma unroll
+  for (int first = 0; first < DC; first += GU) {
+    Group group[2];
+    if constexpr (BITS != 16) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t magnitude = 0;
+        half2v low = half2v{half_of(x[first][j][0]), half_of(x[first][j][0])}, high = low, ends = {0, 0};
+#pragma unroll
+        for (int c = first; c < first + GU; ++c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (BITS == 8) magnitude = most_of(magnitude, x[c][j][i] & 0x7fff7fffu);
+            const uint32_t w = x[c][j][i];
+            if (BITS == 4) {
+              low = least_of(low, __builtin_bit_cast(half2v, w));
+              high = most_of(high, __builtin_bit_cast(half2v, w));
+            }
+          }
+        }
+        magnitude = max(magnitude & 0xffffu, magnitude >> 16);
+        if constexpr (BITS == 8) {
+          magnitude = max(magnitude, other_lane(magnitude, false));
+          magnitude = max(magnitude, other_lane(magnitude, true));
+        } else {
+          ends = half2v{(_Float16)-__builtin_elementwise_minimum(low[0], low[1]), __builtin_elementwise_maximum(high[0], high[1])};
+          ends = most_of(ends, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, ends), false)));
+          ends = most_of(ends, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, ends), true)));
+        }
+        group[j] = group_of_ends<BITS>(magnitude, ends);
+      }
+      if (__any(group[0].bad || group[1].bad)) {     // their codes are zeros'
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int c = first; c < first + GU; ++c) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[c][j][i] = group[j].bad ? 0u : x[c][j][i];
+          }
+        }
+      }
+      if (seat.quarter == 0) {
+        constexpr int kHalves = BITS == 8 ? 32 : 64;  // of a group
+        _Float16* to = scales + first / GU * kHalves;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (!live[j]) continue;
+          if (value) {
+            to[seat.place[j]] = group[j].scale_bits;
+            if (BITS == 4) to[seat.place[j] + 32] = group[j].offset_bits;
+          } else if (BITS == 8) {
+            to[seat.lane * 2 + j] = group[j].scale_bits;
+          } else {
+            reinterpret_cast<uint32_t*>(to)[seat.lane * 2 + j] = bits_of(group[j].scale_bits) | bits_of(group[j].offset_bits) << 16;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int c = first; c < first + GU; ++c) {
+      uint32_t words[2][4];                          // codes of the two runs: 4, 2 or 1 words (of values with 4 bits, two of a byte each)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if constexpr (BITS == 16) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) words[j][i] = x[c][j][i];
+        } else {
+          uint32_t u[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t w = x[c][j][i / 2];
+            u[i] = code_of<BITS>(half_of(i % 2 ? w >> 16 : w & 0xffffu), group[j]);
+          }
+          if (BITS == 4 && !value) {
+            words[j][0] = __builtin_amdgcn_perm(u[1] | u[3] << 4 | u[5] << 8 | u[7] << 12, u[0] | u[2] << 4 | u[4] << 8 | u[6] << 12, 0x05040100u);
+          } else {
+            words[j][0] = bytes_of(u[0], u[1], u[2], u[3]) ^ (BITS == 8 ? 0x80808080u : 0u);
+            words[j][1] = bytes_of(u[4], u[5], u[6], u[7]) ^ (BITS == 8 ? 0x80808080u : 0u);
+          }
+          if (BITS == 4 && value) {                   // channels d and d + 16 share a byte: the lower ones' lane has both
+#pragma unroll
+            for (int i = 0; i < 2; ++i) words[j][i] = (words[j][i] & 0x0f0f0f0fu) | (other_lane(words[j][i], true) & 0x0f0f0f0fu) << 4;
+          }
+        }
+      }
+      if (value) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          unsigned char* to = codes + seat.place[j] * kPitch + c * 4 * BITS;
+          if constexpr (BITS == 16) *reinterpret_cast<u32x4*>(to + seat.quarter * 16) = (u32x4){words[j][0], words[j][1], words[j][2], words[j][3]};
+          if constexpr (BITS == 8) *reinterpret_cast<u32x2*>(to + seat.quarter * 8) = (u32x2){words[j][0], words[j][1]};
+          if constexpr (BITS == 4)
+            if (seat.quarter < 2) *reinterpret_cast<u32x2*>(to + seat.quarter * 8) = (u32x2){words[j][0], words[j][1]};
+        }
+      } else {
+        char* to = span.base + (BITS == 16 ? (c * 128 + seat.lane) * 16 : (c * 64 + seat.lane) * 2 * BITS);
+        if constexpr (BITS == 16) {
+          if (live[0]) *reinterpret_cast<u32x4*>(to) = (u32x4){words[0][0], words[0][1], words[0][2], words[0][3]};
+          if (live[1]) *reinterpret_cast<u32x4*>(to + 1024) = (u32x4){words[1][0], words[1][1], words[1][2], words[1][3]};
+        } else if (span.whole) {
+          if constexpr (BITS == 8) *reinterpret_cast<u32x4*>(to) = (u32x4){words[0][0], words[0][1], words[1][0], words[1][1]};
+          if constexpr (BITS == 4) *reinterpret_cast<u32x2*>(to) = (u32x2){words[0][0], words[1][0]};
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if (!live[j]) continue;
+            if constexpr (BITS == 8) *reinterpret_cast<u32x2*>(to + j * 8) = (u32x2){words[j][0], words[j][1]};
+            if constexpr (BITS == 4) *reinterpret_cast<uint32_t*>(to + j * 4) = words[j][0];
+          }
+        }
+      }
+    }
+  }
+  if (!value) return;
+  // Values: a lane has two channels, 16 apart, of eight places.  (The rows were written by this wavefront itself.)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int eight = lane >> 4, channel = lane & 15;
+  const bool all = span.whole || (!p.rows && 8 * eight >= span.from && 8 * eight + 8 <= span.to);
+  if (all) {
+    const unsigned char* from = codes + 8 * eight * kPitch;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
       if constexpr (BITS == 16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = u[2 * i] | (u[2 * i + 1] << 16);
-      } else if constexpr (BITS == 8) {
-        w[0] = u[0] | (u[1] << 8) | (u[2] << 16) | (u[3] << 24);
-        w[1] = u[4] | (u[5] << 8) | (u[6] << 16) | (u[7] << 24);
-      } else {
-        w[0] = u[0] | (u[2] << 4) | (u[4] << 8) | (u[6] << 12) | (u[1] << 16) | (u[3] << 20) | (u[5] << 24) | (u[7] << 28);
-      }
-    } else {
+        for (int j = 0; j < 2; ++j) {
+          u32x4 w;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = run * 8 + i;
-        unsigned char* b = to_lds + value_byte<BITS>(place, d);
-        if constexpr (BITS == 16) *reinterpret_cast<uint16_t*>(b) = (uint16_t)u[i];
-        if constexpr (BITS == 8) *b = (unsigned char)u[i];
-        // 4 bits: channels d and d + 16 share a byte: the lower ones' thread writes it, once it has both
-        if constexpr (BITS == 4) {
-          const uint32_t other = (uint32_t)__shfl_xor((int)u[i], 2, 64);   // run ^ 2: the channel 16 away
-          if ((run & 2) == 0) *b = (unsigned char)(u[i] | (other << 4));
+          for (int i = 0; i < 4; ++i) {
+            const unsigned char* pair = from + 2 * i * kPitch + (c * 32 + j * 16 + channel) * 2;
+            w[i] = *reinterpret_cast<const uint16_t*>(pair) | (uint32_t)*reinterpret_cast<const uint16_t*>(pair + kPitch) << 16;
+          }
+          *reinterpret_cast<u32x4*>(span.base + ((c * 2 + j) * 64 + lane) * 16) = w;
         }
+      } else {
+        constexpr int kWords = BITS / 2;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          const int e = 4 * (i & 1), at = c * 4 * BITS + i / 2 * 16 + channel;
+          const unsigned char* b = from + e * kPitch + at;
+          w[i] = BITS == 8 ? bytes_of(b[0], b[kPitch], b[2 * kPitch], b[3 * kPitch]) : bytes_of(b[0], b[2 * kPitch], b[kPitch], b[3 * kPitch]);
+        }
+        if constexpr (BITS == 8) *reinterpret_cast<u32x4*>(span.base + (c * 64 + lane) * 16) = (u32x4){w[0], w[1], w[2], w[3]};
+        if constexpr (BITS == 4) *reinterpret_cast<u32x2*>(span.base + (c * 64 + lane) * 8) = (u32x2){w[0], w[1]};
       }
     }
   }
-  __syncthreads();
-  // Pieces of eight values: of one place (keys), of places 8 g .. 8 g + 7 (values).
-  constexpr int kPiece = BITS == 16 ? 16 : 8;      // bytes; with 4 bits two key places, or a byte for two channels
-  constexpr int kPieces = kCode / kPiece;
-  for (int i = threadIdx.x; i < 2 * kPieces; i += kKvThreads) {
-    const int value = i / kPieces, piece = i % kPieces;
-    if ((value ? p.v : p.k) == nullptr) continue;
-    const unsigned char* src = codes + value * kCode + piece * kPiece;
-    char* dst = base + (value ? p.value_offset : 0) + piece * kPiece;
-    const int lane = BITS == 8 ? (piece >> 1) & 63 : piece & 63;
-    if (p.rows == nullptr) {
-      bool all, any;
-      if (!value && BITS != 4) {
-        const int j = BITS == 8 ? piece & 1 : (piece >> 6) & 1, place = 8 * ((lane >> 2) & 3) + 4 * j + (lane & 3);
-        all = any = place >= from && place < to;
-      } else {
-        const int place = 8 * (value ? lane >> 4 : (lane >> 2) & 3);
-        all = place >= from && place + 8 <= to;
-        any = place + 8 > from && place < to;
-      }
-      if (!any) continue;
-      if (all) {
-        if constexpr (kPiece == 16)
-          *reinterpret_cast<u32x4*>(dst) = *reinterpret_cast<const u32x4*>(src);
-        else
-          *reinterpret_cast<uint64_t*>(dst) = *reinterpret_cast<const uint64_t*>(src);
-        continue;
-      }
-    }
-    // a piece that others' positions share: only the live places
-    if (!value) {
+  if (span.whole) return;
+  for (int place = span.from; place < span.to; ++place) {
+    if (p.rows && p.rows[span.row0 + place] < 0) continue;
+    if (place >> 3 != eight || all) continue;
+    const int e = place & 7, byte = BITS == 4 ? (e & 4) + ((e & 1) << 1 | (e >> 1 & 1)) : e;
 #pragma unroll
-      for (int j = 0; j < (BITS == 4 ? 2 : 1); ++j) {
-        const int run = BITS == 4 ? j : (BITS == 8 ? piece & 1 : (piece >> 6) & 1), place = 8 * ((lane >> 2) & 3) + 4 * run + (lane & 3);
-        if (place < from || place >= to || (p.rows && p.rows[row0 + place] < 0)) continue;
-        constexpr int kWords = BITS == 16 ? 4 : (BITS == 8 ? 2 : 1);
+    for (int c = 0; c < DC; ++c) {
 #pragma unroll
-        for (int w = 0; w < kWords; ++w)
-          reinterpret_cast<uint32_t*>(dst)[j + w] = reinterpret_cast<const uint32_t*>(src)[j + w];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int place = 8 * (lane >> 4) + e;
-        if (place < from || place >= to || (p.rows && p.rows[row0 + place] < 0)) continue;
-        if constexpr (BITS == 16) {
-          reinterpret_cast<uint16_t*>(dst)[e] = reinterpret_cast<const uint16_t*>(src)[e];
-        } else {
-          const int byte = BITS == 8 ? e : (e & 4) + (((e & 1) << 1) | ((e >> 1) & 1));
-          dst[byte] = (char)src[byte];
-        }
+      for (int j = 0; j < (BITS == 4 ? 1 : 2); ++j) {
+        const unsigned char* from = codes + place * kPitch + c * 4 * BITS + (j * 16 + channel) * (BITS == 16 ? 2 : 1);
+        if constexpr (BITS == 16) *reinterpret_cast<uint16_t*>(span.base + ((c * 2 + j) * 64 + lane) * 16 + e * 2) = *reinterpret_cast<const uint16_t*>(from);
+        if constexpr (BITS != 16) span.base[(c * 64 + lane) * 2 * BITS + j * 8 + byte] = (char)*from;
       }
     }
   }
 }
 
-// The reverse, the same grid: codes of the block come whole into LDS, items leave as rows.
-template <int BITS, int DIM>
+// Two codes, each in the low byte of 16 bits, as the fp16 values 1024 + code.
+__device__ __forceinline__ half2v above_1024(uint32_t codes) { return __builtin_bit_cast(half2v, codes | 0x64006400u); }
+// Their values: one rounding each.
+template <int BITS>
+__device__ __forceinline__ uint32_t values_of(uint32_t codes, _Float16 scale, _Float16 offset) {
+  const half2v s = {scale, scale}, o = {offset, offset}, zero = BITS == 8 ? half2v{(_Float16)1152.0f, (_Float16)1152.0f} : half2v{(_Float16)1024.0f, (_Float16)1024.0f};
+  const half2v u = above_1024(codes) - zero;
+  return __builtin_bit_cast(uint32_t, BITS == 8 ? u * s : __builtin_elementwise_fma(u, s, o));
+}
+
+// The reverse, with the same grid.  The half block passes through LDS as it is in the cache, codes and scales; an item is a run of eight
+// channels of a live place, and neighbouring lanes have neighbouring runs: stores of whole rows, 256 bytes at 128
+// channels (stores of 64 bytes a place, as the write's loads are, took 60 us where these take 39: 4096 rows of 64 heads of 128
+// channels, 4 bits).  Rows that no cache keeps till they are read go past it (29 us).
+template <int BITS, int DC, int GU, bool PAST>
 __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_read_kernel(KvParams p) {
-  constexpr int kRuns = DIM / 8;
-  constexpr int kItems = 2 * kBlock * kRuns;
-  constexpr int kCode = kBlock * DIM * BITS / 8;
-  __shared__ __attribute__((aligned(16))) unsigned char codes[2 * kCode];
-  const int seq = blockIdx.z, head = blockIdx.y;
-  const Rows rows = rows_of(p, seq);
-  const int64_t end = (int64_t)rows.past + rows.count;
-  const int64_t block = rows.past / kBlock + (int64_t)blockIdx.x;
-  if (block * kBlock >= end || rows.count == 0) return;
-  const char* base = block > INT32_MAX ? nullptr : block_at(p, seq, (int)block, head);
-  const int from = (int)max(rows.past - block * kBlock, (int64_t)0), to = (int)min(end - block * kBlock, (int64_t)kBlock);
-  const int64_t row0 = rows.row + block * kBlock - rows.past;
-  if (base) {
-    for (int i = threadIdx.x; i < 2 * kCode / 16; i += kKvThreads) {
-      const int value = i / (kCode / 16), piece = i % (kCode / 16);
-      reinterpret_cast<u32x4*>(codes)[i] = *reinterpret_cast<const u32x4*>(base + (value ? p.value_offset : 0) + piece * 16);
+  constexpr int kCode = kBlock * DC * 4 * BITS, kHalves = BITS == 16 ? 0 : (BITS == 8 ? 32 : 64) * (DC / GU);
+  constexpr int kBytes = kCode + 2 * kHalves, kRuns = 4 * DC;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kBytes];
+  const int lane = threadIdx.x & 63, value = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  _Float16* target = static_cast<_Float16*>(const_cast<void*>(value ? p.v : p.k));
+  const int64_t stride = value ? p.v_stride : p.k_stride;
+  if (!target) return;
+  const Span span = span_of(p, value);
+  if (span.from >= span.to) return;
+  unsigned char* half = lds + value * kBytes;
+  if (span.base) {
+    u32x4 piece[(kBytes / 16 + 63) / 64];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(piece) / 16); ++i) {
+      const int at = i * 64 + lane;
+      if (at < kBytes / 16) piece[i] = reinterpret_cast<const u32x4*>(span.base)[at];
+    }
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(piece) / 16); ++i) {
+      const int at = i * 64 + lane;
+      if (at < kBytes / 16) reinterpret_cast<u32x4*>(half)[at] = piece[i];
     }
   }
-  __syncthreads();
-  for (int item = threadIdx.x; item < kItems; item += kKvThreads) {
-    const int value = item / (kBlock * kRuns), place = item / kRuns % kBlock, run = item % kRuns;
-    void* out = const_cast<void*>(value ? p.v : p.k);
-    if (place < from || place >= to || !out) continue;
-    half8 x = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (base) {
-      _Float16 scale = 0, offset = 0;
-      if constexpr (BITS != 16) {
-        const _Float16* scales = reinterpret_cast<const _Float16*>(base + (value ? p.value_offset : 0) + kCode);
-        const int group = run / (p.group / 8), at = value ? value_scale<BITS>(group, place) : key_scale<BITS>(group, place);
-        scale = scales[at];
-        if (BITS == 4) offset = scales[at + (value ? 32 : 1)];
-      }
-      const unsigned char* src = codes + value * kCode;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const _Float16* scales = reinterpret_cast<const _Float16*>(half + kCode);
+  const int first = (span.from >> 3) * 4 * kRuns, end = ((span.to + 7) >> 3) * 4 * kRuns;
+#pragma unroll 4
+  for (int item = first + lane; item < end; item += 64) {
+    const int pair = item / kRuns, run = item % kRuns, c = run >> 2, quarter = run & 3, eight = pair >> 2, r = pair & 3;
+    const int key_lane = 16 * quarter + pair;                                        // of a key's codes
+    const int value_lane = 16 * eight + 8 * (quarter & 1), upper = quarter >> 1;     // of the first of eight values' codes
+    u32x4 x[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+    if (span.base) {
+      if constexpr (BITS == 16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+        for (int j = 0; j < 2; ++j) {
+          if (!value) {
+            x[j] = *reinterpret_cast<const u32x4*>(half + ((c * 2 + j) * 64 + key_lane) * 16);
+          } else {
+            const unsigned char* from = half + ((c * 2 + upper) * 64 + value_lane) * 16 + j * 8 + r * 2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              x[j][i] = *reinterpret_cast<const uint16_t*>(from + 32 * i) | (uint32_t)*reinterpret_cast<const uint16_t*>(from + 32 * i + 16) << 16;
+          }
+        }
+      } else {
+        uint32_t pairs[2][4];                         // two codes in a word
+        const unsigned char* from = half + (c * 64 + (value ? value_lane : key_lane)) * 2 * BITS;
         if (!value) {
-          const unsigned char* b = src + key_piece<BITS>(place, run >> 2, run & 3);
-          if constexpr (BITS == 16) x[i] = reinterpret_cast<const _Float16*>(b)[i];
-          if constexpr (BITS == 8) x[i] = value_of<BITS>(b[i], scale, offset);
-          if constexpr (BITS == 4) x[i] = value_of<BITS>(*reinterpret_cast<const uint32_t*>(b) >> (4 * (i / 2 + 4 * (i % 2))) & 15u, scale, offset);
+          uint32_t w[BITS / 2];
+          if constexpr (BITS == 8) *reinterpret_cast<u32x4*>(w) = *reinterpret_cast<const u32x4*>(from);
+          if constexpr (BITS == 4) *reinterpret_cast<u32x2*>(w) = *reinterpret_cast<const u32x2*>(from);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              pairs[j][i] = BITS == 8 ? __builtin_amdgcn_perm(0u, w[BITS == 8 ? 2 * j + i / 2 : 0], i % 2 ? 0x0c030c02u : 0x0c010c00u) : w[j] >> (4 * i) & 0x000f000fu;
+          }
         } else {
-          const unsigned char* b = src + value_byte<BITS>(place, run * 8 + i);
-          if constexpr (BITS == 16) x[i] = *reinterpret_cast<const _Float16*>(b);
-          if constexpr (BITS == 8) x[i] = value_of<BITS>(*b, scale, offset);
-          if constexpr (BITS == 4) x[i] = value_of<BITS>(*b >> (4 * ((run >> 1) & 1)) & 15u, scale, offset);
+          if (BITS == 8) from += upper * 8;
+          const uint32_t b = BITS == 8 ? r : ((r & 1) << 1 | r >> 1), pick = b | 0x0c00u | (4 + b) << 16 | 0x0c000000u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const u32x2 one = *reinterpret_cast<const u32x2*>(from + 4 * BITS * i), two = *reinterpret_cast<const u32x2*>(from + 4 * BITS * i + 2 * BITS);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              pairs[j][i] = __builtin_amdgcn_perm(two[j], one[j], pick);
+              if (BITS == 4) pairs[j][i] = pairs[j][i] >> (4 * upper) & 0x000f000fu;
+            }
+          }
+        }
+        const _Float16* of = scales + c / GU * (BITS == 8 ? 32 : 64);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int k = value ? 8 * eight + r + 4 * j : (BITS == 8 ? 1 : 2) * (pair * 2 + j);
+          const _Float16 scale = of[k], offset = BITS == 4 ? of[k + (value ? 32 : 1)] : (_Float16)0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[j][i] = values_of<BITS>(pairs[j][i], scale, offset);
         }
       }
     }
-    *reinterpret_cast<half8*>(static_cast<_Float16*>(out) + (row0 + place) * (value ? p.v_stride : p.k_stride) + (int64_t)head * DIM + run * 8) = x;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int place = 8 * eight + r + 4 * j;
+      u32x4* to = reinterpret_cast<u32x4*>(target + (span.row0 + place) * stride + (int64_t)blockIdx.y * DC * 32 + run * 8);
+      if (place < span.from || place >= span.to) continue;
+      if constexpr (PAST)
+        __builtin_nontemporal_store(x[j], to);
+      else
+        *to = x[j];
+    }
   }
 }
 
-template <int BITS>
-const void* pick_write(int dim) {
-  switch (dim) {
-    case 64: return reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, 64>);
-    case 96: return reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, 96>);
-    case 128: return reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, 128>);
-    case 192: return reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, 192>);
-    default: return reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, 256>);
+enum Move { kWrite, kRead, kReadPast };          // the last: rows go past the caches
+
+template <int BITS, int DC, int GU>
+const void* kernel_of(Move move) {
+  return move == kWrite  ? reinterpret_cast<const void*>(lutgemm_kv_write_kernel<BITS, DC, GU>)
+         : move == kRead ? reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, DC, GU, false>)
+                         : reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, DC, GU, true>);
+}
+template <int BITS, int DC>
+const void* pick_group(Move move, int units) {
+  if (BITS == 16 || units == DC) return kernel_of<BITS, DC, DC>(move);
+  if constexpr (BITS != 16) {
+    if (units == 1) return kernel_of<BITS, DC, 1>(move);
+    if constexpr (DC % 2 == 0 && DC > 2) {
+      if (units == 2) return kernel_of<BITS, DC, 2>(move);
+    }
+    if constexpr (DC == 6) {
+      if (units == 3) return kernel_of<BITS, DC, 3>(move);
+    }
+    if constexpr (DC == 8) {
+      if (units == 4) return kernel_of<BITS, DC, 4>(move);
+    }
   }
+  return nullptr;
 }
 template <int BITS>
-const void* pick_read(int dim) {
+const void* pick_kernel(Move move, int dim, int units) {
   switch (dim) {
-    case 64: return reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, 64>);
-    case 96: return reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, 96>);
-    case 128: return reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, 128>);
-    case 192: return reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, 192>);
-    default: return reinterpret_cast<const void*>(lutgemm_kv_read_kernel<BITS, 256>);
+    case 64: return pick_group<BITS, 2>(move, units);
+    case 96: return pick_group<BITS, 3>(move, units);
+    case 128: return pick_group<BITS, 4>(move, units);
+    case 192: return pick_group<BITS, 6>(move, units);
+    case 256: return pick_group<BITS, 8>(move, units);
+    default: return nullptr;
   }
 }
 
@@ -520,10 +664,11 @@ int move_rows(bool write, const void* k, const void* v, const int32_t* rows, con
   p.table_pages = step->table_pages;
   p.page_blocks = cache->page_tokens / kBlock;
   p.heads = cache->heads;
-  p.group = group;
   const int most = step->most_tokens < step->tokens ? step->most_tokens : step->tokens;
-  const void* kern = write ? (cache->bits == 16 ? pick_write<16>(cache->head_dim) : cache->bits == 8 ? pick_write<8>(cache->head_dim) : pick_write<4>(cache->head_dim))
-                           : (cache->bits == 16 ? pick_read<16>(cache->head_dim) : cache->bits == 8 ? pick_read<8>(cache->head_dim) : pick_read<4>(cache->head_dim));
+  const int units = group / 32, d = cache->head_dim;
+  const Move move = write ? kWrite : ((int64_t)step->tokens * row * 4 > kCacheBytes ? kReadPast : kRead);
+  const void* kern = cache->bits == 16 ? pick_kernel<16>(move, d, units) : cache->bits == 8 ? pick_kernel<8>(move, d, units) : pick_kernel<4>(move, d, units);
+  if (!kern) return LUTGEMM_EUNSUPPORTED;
   void* args[] = {&p};
   // positions past .. past + most - 1 touch at most this many blocks
   const dim3 grid((most + 2 * kBlock - 2) / kBlock, cache->heads, step->seqs);
