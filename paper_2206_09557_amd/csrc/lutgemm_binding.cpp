@@ -21,9 +21,16 @@ typedef int (*StaticFn)(const void*, const void*, const void*, const void*, void
 typedef int (*GroupFn)(const void* const*, const void* const*, const void* const*, const void* const*, void* const*, const int64_t*,
                        const int64_t*, int, int, int, int, unsigned, void*, size_t, void*);
 
-enum Which { kGemv, kGemm, kMfma, kDequant, kStatic, kGroup, kCount };
+typedef int (*RopeFn)(const void*, void*, const void*, const void*, int, int, int, int, int64_t, int64_t, float, unsigned, void*);
+typedef int (*WriteFn)(const void*, const void*, const void*, const void*, const void*, int64_t, int64_t, void*);
+typedef int (*ReadFn)(const void*, const void*, void*, void*, int64_t, int64_t, void*);
+typedef int (*AttentionFn)(const void*, const void*, const void*, const void*, void*, int, int64_t, int64_t, float, int64_t, void*, size_t,
+                           void*);
+
+// Products of layers, then the attention half of a step; either set can be loaded without the other.
+enum Which { kGemv, kGemm, kMfma, kDequant, kStatic, kGroup, kProducts, kRope = kProducts, kKvWrite, kKvRead, kAttention, kCount };
 const char* const kNames[kCount] = {"lutgemm_gemv", "lutgemm_gemm", "lutgemm_gemm_mfma", "lutgemm_gemm_dequant_mfma", "lutgemm_gemv_static",
-                                    "lutgemm_gemv_group"};
+                                    "lutgemm_gemv_group", "lutgemm_rope", "lutgemm_kv_write", "lutgemm_kv_read", "lutgemm_attention"};
 
 void* g_function[kCount];        // of the loaded library, null until then
 PyObject* g_ctypes[kCount];      // lutgemm.py's functions
@@ -69,6 +76,11 @@ bool c_int(PyObject* o, int* out) {
   int64_t v;
   if (!integer(o, INT_MIN, INT_MAX, &v)) return false;
   *out = (int)v;
+  return true;
+}
+bool real(PyObject* o, float* out) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *out = (float)PyFloat_AS_DOUBLE(o);
   return true;
 }
 
@@ -166,8 +178,80 @@ PyObject* group(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
   return result(w, code);
 }
 
+// x, y, positions, turns, tokens, heads, head_dim, rot_dim, x_stride, y_stride, amplitude, flags, stream=0
+PyObject* rope(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  const Which w = kRope;
+  if (!g_function[w] || (kwnames && PyTuple_GET_SIZE(kwnames) != 0) || (nargs != 12 && nargs != 13)) return by_ctypes(w, args, nargs, kwnames);
+  void *buf[4], *stream = nullptr;
+  int shape[4];
+  int64_t stride[2], flags;
+  float amplitude;
+  bool ok = true;
+  for (int i = 0; i < 4 && ok; ++i) ok = address(args[i], &buf[i]);
+  for (int i = 0; i < 4 && ok; ++i) ok = c_int(args[4 + i], &shape[i]);
+  for (int i = 0; i < 2 && ok; ++i) ok = integer(args[8 + i], INT64_MIN, INT64_MAX, &stride[i]);
+  ok = ok && real(args[10], &amplitude) && integer(args[11], 0, UINT_MAX, &flags);
+  if (nargs == 13) ok = ok && PyLong_CheckExact(args[12]) && address(args[12], &stream);
+  if (!ok) return by_ctypes(w, args, nargs, kwnames);
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = reinterpret_cast<RopeFn>(g_function[w])(buf[0], buf[1], buf[2], buf[3], shape[0], shape[1], shape[2], shape[3], stride[0], stride[1],
+                                                 amplitude, (unsigned)flags, stream);
+  Py_END_ALLOW_THREADS
+  return result(w, code);
+}
+
+// k, v, rows, cache, step, k_stride, v_stride, stream=0; or cache, step, k, v, ...
+PyObject* kv_rows(Which w, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  const int buffers = w == kKvWrite ? 5 : 4;
+  if (!g_function[w] || (kwnames && PyTuple_GET_SIZE(kwnames) != 0) || (nargs != buffers + 2 && nargs != buffers + 3))
+    return by_ctypes(w, args, nargs, kwnames);
+  void *buf[5], *stream = nullptr;
+  int64_t stride[2];
+  bool ok = true;
+  for (int i = 0; i < buffers && ok; ++i) ok = address(args[i], &buf[i]);
+  for (int i = 0; i < 2 && ok; ++i) ok = integer(args[buffers + i], INT64_MIN, INT64_MAX, &stride[i]);
+  if (nargs == buffers + 3) ok = ok && PyLong_CheckExact(args[buffers + 2]) && address(args[buffers + 2], &stream);
+  if (!ok) return by_ctypes(w, args, nargs, kwnames);
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  if (w == kKvWrite)
+    code = reinterpret_cast<WriteFn>(g_function[w])(buf[0], buf[1], buf[2], buf[3], buf[4], stride[0], stride[1], stream);
+  else
+    code = reinterpret_cast<ReadFn>(g_function[w])(buf[0], buf[1], buf[2], buf[3], stride[0], stride[1], stream);
+  Py_END_ALLOW_THREADS
+  return result(w, code);
+}
+
+// q, mask, cache, step, y, q_heads, q_stride, y_stride, scale, most_positions, workspace, workspace_bytes, stream=0
+PyObject* attention(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  const Which w = kAttention;
+  if (!g_function[w] || (kwnames && PyTuple_GET_SIZE(kwnames) != 0) || (nargs != 12 && nargs != 13)) return by_ctypes(w, args, nargs, kwnames);
+  void *buf[5], *ws, *stream = nullptr;
+  int q_heads;
+  int64_t stride[2], most, bytes;
+  float scale;
+  bool ok = true;
+  for (int i = 0; i < 5 && ok; ++i) ok = address(args[i], &buf[i]);
+  ok = ok && c_int(args[5], &q_heads);
+  for (int i = 0; i < 2 && ok; ++i) ok = integer(args[6 + i], INT64_MIN, INT64_MAX, &stride[i]);
+  ok = ok && real(args[8], &scale) && integer(args[9], INT64_MIN, INT64_MAX, &most) && address(args[10], &ws) &&
+       integer(args[11], 0, INT64_MAX, &bytes);
+  if (nargs == 13) ok = ok && PyLong_CheckExact(args[12]) && address(args[12], &stream);
+  if (!ok) return by_ctypes(w, args, nargs, kwnames);
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  code = reinterpret_cast<AttentionFn>(g_function[w])(buf[0], buf[1], buf[2], buf[3], buf[4], q_heads, stride[0], stride[1], scale, most, ws,
+                                                      (size_t)bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(w, code);
+}
+
 template <Which W>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  if (W == kRope) return rope(args, nargs, kwnames);
+  if (W == kKvWrite || W == kKvRead) return kv_rows(W, args, nargs, kwnames);
+  if (W == kAttention) return attention(args, nargs, kwnames);
   return W == kGroup ? group(args, nargs, kwnames) : one_layer(W, args, nargs, kwnames);
 }
 
@@ -177,6 +261,7 @@ PyObject* set_up(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "O!O", &PyDict_Type, &functions, &check)) return nullptr;
   for (int w = 0; w < kCount; ++w) {
     PyObject* f = PyDict_GetItemString(functions, kNames[w]);
+    if (!f && w >= kProducts) continue;
     if (!f) {
       PyErr_SetString(PyExc_KeyError, kNames[w]);
       return nullptr;
@@ -195,6 +280,7 @@ PyObject* load(PyObject*, PyObject* args) {
   for (int w = 0; w < kCount; ++w) {
     PyObject* a = PyDict_GetItemString(addresses, kNames[w]);   // (a host-only build of the library has none: ctypes then says so)
     void* p = nullptr;
+    if (!a && w >= kProducts) continue;
     if (a && !address(a, &p)) {
       PyErr_SetString(PyExc_TypeError, "an address is a non-negative int");
       return nullptr;
@@ -214,6 +300,10 @@ PyMethodDef g_methods[] = {
     ENTRY("lutgemm_gemm_dequant_mfma", kDequant, LAYER_ARGS "batch, flags, workspace, workspace_bytes, stream=0"),
     ENTRY("lutgemm_gemv_static", kStatic, LAYER_ARGS "flags, stream=0"),
     ENTRY("lutgemm_gemv_group", kGroup, "x, bits, alpha, z, y, m, n, q, g, mu, flags, workspace, workspace_bytes, stream=0"),
+    ENTRY("lutgemm_rope", kRope, "x, y, positions, turns, tokens, heads, head_dim, rot_dim, x_stride, y_stride, amplitude, flags, stream=0"),
+    ENTRY("lutgemm_kv_write", kKvWrite, "k, v, rows, cache, step, k_stride, v_stride, stream=0"),
+    ENTRY("lutgemm_kv_read", kKvRead, "cache, step, k, v, k_stride, v_stride, stream=0"),
+    ENTRY("lutgemm_attention", kAttention, "q, mask, cache, step, y, q_heads, q_stride, y_stride, scale, most_positions, workspace, workspace_bytes, stream=0"),
     {"set_up", set_up, METH_VARARGS, nullptr},
     {"load", load, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -111,7 +111,7 @@ def lib():
         _lib = handle
         if _binding is not None:
             _binding.load({name: ctypes.cast(getattr(handle, name), ctypes.c_void_p).value
-                           for name in _DEVICE_CALLS if hasattr(handle, name)})
+                           for name in _DEVICE_CALLS + _CACHE_CALLS if hasattr(handle, name)})
     return _lib
 
 
@@ -388,11 +388,13 @@ def lutgemm_plan_attention(cache, step, q_heads, most_positions=0):
 # slower each.
 _DEVICE_CALLS = ("lutgemm_gemv", "lutgemm_gemm", "lutgemm_gemm_mfma", "lutgemm_gemm_dequant_mfma", "lutgemm_gemv_static",
                  "lutgemm_gemv_group")
+_CACHE_CALLS = ("lutgemm_rope", "lutgemm_kv_write", "lutgemm_kv_read", "lutgemm_attention")
 try:
     _binding = importlib.import_module(__package__ + "._binding")
 except ImportError as e:
     if not isinstance(e, ModuleNotFoundError):   # built, but not for this process
         warnings.warn(f"the compiled marshalling of the device calls does not load, ctypes does it: {e}")
 else:
-    _binding.set_up({name: globals()[name] for name in _DEVICE_CALLS}, _check)
-    globals().update({name: getattr(_binding, name) for name in _DEVICE_CALLS})
+    _binding.set_up({name: globals()[name] for name in _DEVICE_CALLS + _CACHE_CALLS}, _check)
+    # (one that was built before a call was added has none for it, till it is built again)
+    globals().update({name: getattr(_binding, name) for name in _DEVICE_CALLS + _CACHE_CALLS if hasattr(_binding, name)})
