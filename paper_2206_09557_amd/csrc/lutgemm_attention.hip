@@ -128,21 +128,33 @@ template <int BITS>
 struct Unit {
   uint32_t w[BITS];            // 16, 8 or 4 words
 };
+// The cache's memory, by its address space: the compiler must not take it for memory that may be LDS, whose loads it can only wait for
+// all together.
+typedef const __attribute__((address_space(1))) char* Memory;
+template <typename T>
+__device__ __forceinline__ T load_at(Memory p, int i) {
+  return reinterpret_cast<const __attribute__((address_space(1))) T*>(p)[i];
+}
+template <typename T>
+__device__ __forceinline__ T load_past(Memory p, int i) {          // codes are read once
+  return __builtin_nontemporal_load(reinterpret_cast<const __attribute__((address_space(1))) T*>(p) + i);
+}
+
 template <int BITS>
-__device__ __forceinline__ void load_unit(Unit<BITS>& u, const char* codes, int c, int lane) {
+__device__ __forceinline__ void load_unit(Unit<BITS>& u, Memory codes, int c, int lane) {
   if constexpr (BITS == 16) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (c * 2 + j) * 1024) + lane);
+      const u32x4 v = load_past<u32x4>(codes + (c * 2 + j) * 1024, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i) u.w[4 * j + i] = v[i];
     }
   } else if constexpr (BITS == 8) {
-    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + c * 1024) + lane);
+    const u32x4 v = load_past<u32x4>(codes + c * 1024, lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) u.w[i] = v[i];
   } else {
-    const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(codes + c * 512) + lane);
+    const u32x2 v = load_past<u32x2>(codes + c * 512, lane);
     u.w[0] = v[0];
     u.w[1] = v[1];
   }
@@ -213,17 +225,17 @@ struct ValueWords {
 };
 
 template <int BITS, int DC, int GU>
-__device__ __forceinline__ void load_keys(KeyWords<BITS, DC, GU>& k, const char* block, int lane) {
+__device__ __forceinline__ void load_keys(KeyWords<BITS, DC, GU>& k, Memory block, int lane) {
 #pragma unroll
   for (int c = 0; c < DC; ++c) load_unit<BITS>(k.unit[c], block, c, lane);
   if constexpr (BITS != 16) {
-    const char* scales = block + kBlock * DC * 32 * BITS / 8;
+    const Memory scales = block + kBlock * DC * 32 * BITS / 8;
 #pragma unroll
     for (int g = 0; g < DC / GU; ++g) {
       if constexpr (BITS == 8) {
-        k.scale[g] = reinterpret_cast<const uint32_t*>(scales + g * 64)[lane & 15];
+        k.scale[g] = load_at<uint32_t>(scales + g * 64, lane & 15);
       } else {
-        const u32x2 v = reinterpret_cast<const u32x2*>(scales + g * 128)[lane & 15];
+        const u32x2 v = load_at<u32x2>(scales + g * 128, lane & 15);
         k.scale[2 * g] = v[0];
         k.scale[2 * g + 1] = v[1];
       }
@@ -231,15 +243,15 @@ __device__ __forceinline__ void load_keys(KeyWords<BITS, DC, GU>& k, const char*
   }
 }
 template <int BITS, int DC, int GU>
-__device__ __forceinline__ void load_values(ValueWords<BITS, DC, GU>& v, const char* block, int lane) {
+__device__ __forceinline__ void load_values(ValueWords<BITS, DC, GU>& v, Memory block, int lane) {
 #pragma unroll
   for (int c = 0; c < DC; ++c) load_unit<BITS>(v.unit[c], block, c, lane);
   if constexpr (BITS != 16) {
-    const char* scales = block + kBlock * DC * 32 * BITS / 8;
+    const Memory scales = block + kBlock * DC * 32 * BITS / 8;
 #pragma unroll
     for (int g = 0; g < DC / GU; ++g) {
-      v.scale[g] = reinterpret_cast<const half8v*>(scales + g * (BITS == 8 ? 64 : 128))[lane >> 4];
-      if constexpr (BITS == 4) v.offset[g] = reinterpret_cast<const half8v*>(scales + g * 128 + 64)[lane >> 4];
+      v.scale[g] = load_at<half8v>(scales + g * (BITS == 8 ? 64 : 128), lane >> 4);
+      if constexpr (BITS == 4) v.offset[g] = load_at<half8v>(scales + g * 128 + 64, lane >> 4);
     }
   }
 }
@@ -584,18 +596,11 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
     for (int k = 1; k < PARTS; ++k) a += *reinterpret_cast<const float4v*>(&sums[(k * kRows + row) * kPitch + d]);
     if (w.active == 1)
       store_row(p, w.row_first, w.head, w.row0 + row, kDim, d, a, row_ends[row][1]);
-    else if (E::kLastAdds)
-      store4(through, row * kDim + d, a);
     else
-      *reinterpret_cast<float4v*>(mine + row * kDim + d) = a;
+      store4(through, row * kDim + d, a);
   }
   if (w.active == 1) return;
-  if ((int)threadIdx.x < live_rows) {
-    if (E::kLastAdds)
-      store2(through, p.partial_rows * kDim + 2 * threadIdx.x, row_ends[threadIdx.x]);
-    else
-      *reinterpret_cast<float2v*>(mine + p.partial_rows * kDim + 2 * threadIdx.x) = row_ends[threadIdx.x];
-  }
+  if ((int)threadIdx.x < live_rows) store2(through, p.partial_rows * kDim + 2 * threadIdx.x, row_ends[threadIdx.x]);
   if constexpr (E::kLastAdds) {
     uint32_t* last = reinterpret_cast<uint32_t*>(lds);            // (what was there has been added)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -787,14 +792,14 @@ __device__ __forceinline__ void mask_values(ValueWords<BITS, DC, GU>& v, int pla
 
 // Address of a block's codes: of the page that `page` numbers (0 where there is none: its values are not used).
 struct Blocks {
-  const char* head;            // the head's first block of page 0
+  Memory head;                 // the head's first block of page 0
   int64_t page_bytes;
   int block_bytes;
 };
 __device__ __forceinline__ Blocks blocks_of(const Params& p, int head) {
-  return {p.pool + (int64_t)head * p.page_blocks * p.block_bytes, (int64_t)p.heads * p.page_blocks * p.block_bytes, p.block_bytes};
+  return {(Memory)p.pool + (int64_t)head * p.page_blocks * p.block_bytes, (int64_t)p.heads * p.page_blocks * p.block_bytes, p.block_bytes};
 }
-__device__ __forceinline__ const char* block_address(const Blocks& b, int page, int in_page) {
+__device__ __forceinline__ Memory block_address(const Blocks& b, int page, int in_page) {
   return b.head + max(page, 0) * b.page_bytes + (int64_t)in_page * b.block_bytes;
 }
 
@@ -831,7 +836,7 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS,
   int block = w.first_block + wave;
   if (block < w.end_block) {
     bool dead[kSets];
-    const char* at = nullptr;
+    Memory at = nullptr;
     int ahead = block;                        // the next block to be asked for
     auto find = [&](int set) {
       if (ahead < w.end_block) {
@@ -890,15 +895,22 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS,
 
 // Many rows: GROUPS_R wavefronts share a block, RT tiles of rows each, so that its codes are fetched and made fp16 once for all of them:
 // each does its share of the block's 2 DC units (keys, values) and puts the operands into LDS, in the order
-// in which the lanes want them back (16 bytes each, no bank conflicts).  The next block's codes are in registers meanwhile, its
-// operands go to the other half of the LDS; one barrier a block.  Where there are fewer rows than
-// eight wavefronts hold, PARTS sets of GROUPS_R take blocks in turn.
+// in which the lanes want them back (16 bytes each, no bank conflicts).  Where there are fewer rows than eight wavefronts
+// hold, PARTS sets of GROUPS_R take blocks in turn.
+// Two wavefronts share a SIMD, and a block is matrix work (scores, weighted values) and vector work (the weights) of about the same
+// length: so the first four wavefronts and the last four run half a block apart, held there by two barriers a block, and
+// the one's matrix work hides under the other's vector work.  Between its barriers a wavefront
+//     works out the weights of block n,  then  adds its weighted values, puts the operands of block n + 2 into LDS where block n's
+//                                              were, and forms the scores of block n + 1;
+// each operand of 16 bytes a lane is asked for as soon as the product before it has used the register, so a block's values are in
+// registers when its keys have been used.  (The last operands of a block are put one barrier before the early four
+// read them, and the late four have read a block one barrier before the early four put another in its place.)
 template <int BITS, int DC, int GU, int RT, int GROUPS_R, int PARTS>
 __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_shared_kernel(Params p) {
   constexpr int kEach = (2 * DC + GROUPS_R - 1) / GROUPS_R;        // units of a wavefront
   constexpr int kOperands = 2 * DC * 2 * 1024;                     // bytes of a block's: units x runs
-  constexpr int kHeld = kEach >= 4 ? DC : 2 * DC;                  // operands that a wavefront takes from LDS at a time
-  constexpr int kDepth = kEach * BITS <= 32 && DC < 8 ? 2 : 1;             // blocks of codes on their way
+  constexpr int kHeld = 2 * DC;                                    // of a block's keys, or of its values
+  static_assert(GROUPS_R * PARTS == 8, "");
   using E = Ending<DC, RT, GROUPS_R, PARTS>;
   constexpr int kBytes = 2 * PARTS * kOperands > E::kFloats * 4 ? 2 * PARTS * kOperands : E::kFloats * 4;
   __shared__ __attribute__((aligned(16))) char lds[kBytes];
@@ -915,44 +927,46 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
   const Blocks blocks = blocks_of(p, w.head);
 
   constexpr int kCode = kBlock * DC * 32 * BITS / 8;
-  Unit<BITS> unit[kDepth][kEach];
-  u32x4 scale[kDepth][BITS == 16 ? 1 : kEach], offset[kDepth][BITS == 4 ? kEach : 1];
+  Unit<BITS> unit[kEach];
+  u32x4 scale[BITS == 16 ? 1 : kEach], offset[BITS == 4 ? kEach : 1];
   const uint32_t odd_lane = lane & 1 ? ~0u : 0u, upper_lane = lane & 2 ? ~0u : 0u;
-  bool dead[2] = {false, false};
+  constexpr int kAhead = 2;                                        // blocks from the one at hand to the one found last
+  uint32_t dead = 0;                                               // which of the last fetched blocks have no page, the last in bit 0
   int ahead = w.first_block + part;                                // the next block to be fetched
-  const char* at = blocks.head;                                    // (of page 0: a part without a block fetches that)
-  // This wavefront's units of the block `ahead`; `half`: of the LDS, where they are to go.
-  auto fetch = [&](const int half) {
-    const int set = kDepth == 2 ? half : 0;
+  Memory at = blocks.head;                                         // (of page 0: a part without a block fetches that)
+  // Finds the block `ahead`, and fetches this wavefront's units of it.  (Apart: the page table's next entry is asked for where no product
+  // waits for operands, which could only wait for it too.)
+  auto find = [&]() {
+    dead <<= 1;
     if (ahead < w.end_block) {                                     // (else the last one again: the loads are free of branches)
       const int page = walk_page(walk);
-      dead[half] = page < 0;
+      dead |= page < 0;
       at = block_address(blocks, page, walk.in_page);
       ahead += PARTS;
       walk_on(walk);
     }
     asm("" : "+s"(at));                                            // (the same address again is not the same load again)
+  };
+  auto fetch = [&]() {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int u = min(group + i * GROUPS_R, 2 * DC - 1);
       const bool key = u < DC;
       const int c = key ? u : u - DC, g = c / GU;
-      const char* half_block = at + (key ? 0 : p.block_bytes / 2);
-      load_unit<BITS>(unit[set][i], half_block, c, lane);
+      const Memory half_block = at + (key ? 0 : p.block_bytes / 2);
+      load_unit<BITS>(unit[i], half_block, c, lane);
       // Scales: the sixteen bytes that the lane's are among, of a key's or a value's unit by the same loads.
       if constexpr (BITS != 16) {
-        const char* scales = half_block + kCode + g * (BITS == 8 ? 64 : 128) + (key ? (lane & (BITS == 8 ? 12 : 14)) * (BITS == 8 ? 4 : 8) : (lane >> 4) * 16);
-        scale[set][i] = *reinterpret_cast<const u32x4*>(scales);
-        if constexpr (BITS == 4) offset[set][i] = *reinterpret_cast<const u32x4*>(scales + (key ? 0 : 64));
+        const Memory scales = half_block + kCode + g * (BITS == 8 ? 64 : 128) + (key ? (lane & (BITS == 8 ? 12 : 14)) * (BITS == 8 ? 4 : 8) : (lane >> 4) * 16);
+        scale[i] = load_at<u32x4>(scales, 0);
+        if constexpr (BITS == 4) offset[i] = load_at<u32x4>(scales + (key ? 0 : 64), 0);
       }
     }
   };
-  auto operands = [&](const int half) { return lds + (half * PARTS + part) * kOperands; };
-  // The fetched units of `block`, as operands.
-  auto put = [&](const int half, int block) {
-    const int set = kDepth == 2 ? half : 0;
-    if (block >= w.end_block) return;
-    u32x4* to = reinterpret_cast<u32x4*>(operands(half)) + lane;
+  // The fetched units, as operands in a buffer (beyond the last block ones that nothing reads: a branch would hide from the compiler
+  // how many loads are younger than those it waits for).
+  auto put = [&](char* buffer) {
+    u32x4* to = reinterpret_cast<u32x4*>(buffer) + lane;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int u = group + i * GROUPS_R;
@@ -962,16 +976,16 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
         half8v v;
         if constexpr (BITS == 16) {
           const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
-          v = value_values<16>(unit[set][i], j, none, none);
+          v = value_values<16>(unit[i], j, none, none);
         } else if (u >= DC) {
-          v = value_values<BITS>(unit[set][i], j, __builtin_bit_cast(half8v, scale[set][i]), __builtin_bit_cast(half8v, offset[set][BITS == 4 ? i : 0]));
+          v = value_values<BITS>(unit[i], j, __builtin_bit_cast(half8v, scale[i]), __builtin_bit_cast(half8v, offset[BITS == 4 ? i : 0]));
         } else if constexpr (BITS == 8) {
-          v = key_values<BITS>(unit[set][i], j, half_of(one_of(one_of(word_of<0>(scale[set][i]), word_of<1>(scale[set][i]), odd_lane),
-                                                               one_of(word_of<2>(scale[set][i]), word_of<3>(scale[set][i]), odd_lane), upper_lane), j), (_Float16)0);
+          v = key_values<BITS>(unit[i], j, half_of(one_of(one_of(word_of<0>(scale[i]), word_of<1>(scale[i]), odd_lane),
+                                                               one_of(word_of<2>(scale[i]), word_of<3>(scale[i]), odd_lane), upper_lane), j), (_Float16)0);
         } else {
-          const uint32_t word = j ? one_of(word_of<1>(scale[set][i]), word_of<3>(scale[set][i]), odd_lane)
-                                  : one_of(word_of<0>(scale[set][i]), word_of<2>(scale[set][i]), odd_lane);
-          v = key_values<BITS>(unit[set][i], j, half_of(word, 0), half_of(word, 1));
+          const uint32_t word = j ? one_of(word_of<1>(scale[i]), word_of<3>(scale[i]), odd_lane)
+                                  : one_of(word_of<0>(scale[i]), word_of<2>(scale[i]), odd_lane);
+          v = key_values<BITS>(unit[i], j, half_of(word, 0), half_of(word, 1));
         }
         to[(u * 2 + j) * 64] = __builtin_bit_cast(u32x4, v);
       }
@@ -979,90 +993,103 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
   };
 
   int block = w.first_block + part;                                // this part's
-  fetch(0);
-  if (kDepth == 2) fetch(1);
+  char* buffer = lds + part * kOperands;                           // of its operands, and the next block's
+  char* buffer1 = buffer + PARTS * kOperands;
+  find();
+  fetch();
   uint64_t sees[RT];
   load_queries<DC, RT>(p, w, w.row0 + 16 * RT * group, lane, s, sees);
-  put(0, block);
+  put(buffer);
+  find();
+  fetch();
+  put(buffer1);
+  find();
+  fetch();
   const int stages = (w.end_block - w.first_block + PARTS - 1) / PARTS;
-  const int whole_end = w.past / kBlock;                           // every row sees all of the blocks before it
-  const int whole_stages = whole_end >= w.end_block ? stages : max(0, whole_end - w.first_block) / PARTS;
+  const int whole_end = min(w.past / kBlock, w.end_block);         // every row sees all of the blocks before it
+  const int whole_stages = max(0, whole_end - w.first_block) / PARTS;
   const bool idle = w.row0 + 16 * RT * group >= w.rows;            // no row of this wavefront's lives: it only helps with the operands
-  auto stage = [&](const int half, auto mask) {
-    constexpr bool kMasked = decltype(mask)::value;
-    const bool skip = idle || block >= w.end_block || (!kMasked && dead[half]);
-    const int limit = dead[half] ? -(1 << 30) : (int)(w.length - w.past), place = block * kBlock + 8 * quarter - w.past;
-    fetch(kDepth == 2 ? half : half ^ 1);                          // (what was in those registers has been put)
-    __syncthreads();
-    if (!skip) {
-      const half8v* from = reinterpret_cast<const half8v*>(operands(half)) + lane;
-      float4v score[RT][2];
+  const int limit_of_rows = (int)(w.length - w.past);
+  half8v held[kHeld];
+  float4v score[RT][2];
+  auto operand = [&](const char* from, int u) { return reinterpret_cast<const half8v*>(from)[u * 64 + lane]; };
+  // Scores of a block whose keys are held; leaves its values there.
+  auto form_scores = [&](const char* from) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
-      // (All of a half's operands are asked for before the first is used, the values' before the weights are worked out: left alone, the
-      // compiler asks for one or two at a time, and waits for each.)
-      half8v held[kHeld];
+    for (int t = 0; t < RT; ++t) score[t][0] = score[t][1] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int first = 0; first < 2 * DC; first += kHeld) {
+    for (int u = 0; u < kHeld; ++u) {
 #pragma unroll
-        for (int u = 0; u < kHeld; ++u) held[u] = from[(first + u) * 64];
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < kHeld; ++u) {
-#pragma unroll
-          for (int t = 0; t < RT; ++t) score[t][u % 2] = mfma(held[u], s.query[t][(first + u) / 2], score[t][u % 2]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kHeld; ++u) held[u] = from[(2 * DC + u) * 64];
+      for (int t = 0; t < RT; ++t) score[t][u % 2] = mfma(held[u], s.query[t][u / 2], score[t][u % 2]);
+      held[u] = operand(from, 2 * DC + u);
       __builtin_amdgcn_sched_barrier(0);
-      half8v weight[RT];
+    }
+  };
+  __syncthreads();
+  if (!idle) {
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) held[u] = operand(buffer, u);
+    form_scores(buffer);
+  }
+  if (wave >= 4) __syncthreads();
+  auto stage = [&](auto all_whole) {
+    constexpr bool kWhole = decltype(all_whole)::value;
+    const bool none = block >= w.end_block || (dead >> kAhead & 1u);
+    half8v weight[RT];
+    find();
+    if (!idle) {
+      const int limit = none ? -(1 << 30) : limit_of_rows, place = block * kBlock + 8 * quarter - w.past;
       uint32_t visible[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        visible[t] = kMasked ? visible_places(place, limit, sees[t]) : 0u;
-        weight[t] = block_weights<DC, RT>(score[t], s, t, p.scale, !kMasked, visible[t], ones);
+        visible[t] = kWhole ? 0u : visible_places(place, limit, sees[t]);
+        weight[t] = block_weights<DC, RT>(score[t], s, t, p.scale, kWhole, visible[t], ones);
       }
-      u32x4 exist;
-      bool rare = false;
-      if constexpr (kMasked) {
-        exist = existing_places(place, limit);
+      if constexpr (!kWhole) {
+        const u32x4 exist = existing_places(place, limit);
         half8v odd = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-        for (int u = 0; u < 2 * DC; ++u) odd = oddness(masked(from[(2 * DC + u) * 64], exist), odd);
-        rare = any_odd(odd);
-      }
-#pragma unroll
-      for (int u = 0; u < 2 * DC; ++u) {
-        if (u > 0 && u % kHeld == 0) {
-#pragma unroll
-          for (int k = 0; k < kHeld; ++k) held[k] = from[(2 * DC + u + k) * 64];
-          __builtin_amdgcn_sched_barrier(0);
+        for (int u = 0; u < kHeld; ++u) {
+          held[u] = masked(held[u], exist);
+          odd = oddness(held[u], odd);
         }
-        half8v v = held[u % kHeld];
-        if constexpr (kMasked) {
-          v = masked(v, exist);
-          if (__builtin_expect(rare, 0)) {
-            add_odd<DC, RT>(v, visible, s, u);
-            v = finite_only(v);
+        if (__builtin_expect(any_odd(odd), 0)) {
+#pragma unroll
+          for (int u = 0; u < kHeld; ++u) {
+            add_odd<DC, RT>(held[u], visible, s, u);
+            held[u] = finite_only(held[u]);
           }
         }
-#pragma unroll
-        for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(v, weight[t], s.out[t][u]);
       }
     }
+    __syncthreads();
+    __builtin_amdgcn_s_setprio(1);                                 // (the products' issue before the other wavefront's vector work: 107 -> 104 us)
+    if (!idle) {
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) s.out[t][u] = mfma(held[u], weight[t], s.out[t][u]);
+        held[u] = operand(buffer1, u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    put(buffer);
+    fetch();
+    if (!idle) form_scores(buffer1);
+    char* other = buffer;
+    buffer = buffer1;
+    buffer1 = other;
+    __builtin_amdgcn_s_setprio(0);
     block += PARTS;
-    put(half ^ 1, block);
+    __syncthreads();
   };
-  int done = 0;
-  for (; done + 2 <= whole_stages; done += 2) {
-    stage(0, std::false_type());
-    stage(1, std::false_type());
+  // (Whole blocks without a page go through the code that can mask them.)
+  for (int done = 0; done < stages; ++done) {
+    for (; done < whole_stages && !(dead >> kAhead & 1u); ++done) stage(std::true_type());
+    if (done >= stages) break;
+    stage(std::false_type());
   }
-  for (; done < stages; done += 2) {
-    stage(0, std::true_type());
-    if (done + 1 < stages) stage(1, std::true_type());
-  }
+  if (wave < 4) __syncthreads();
   __syncthreads();
   end_workgroup<DC, RT, GROUPS_R, PARTS>(arguments_again(), w, reinterpret_cast<float*>(lds), s, group, part, lane);
 }
@@ -1081,7 +1108,9 @@ const void* pick_tiles(int row_tiles, int waves) {
     if (row_tiles == 8) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 4, 2>);
     if (row_tiles == 16) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 2, 8, 1>);
   } else {
-    if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 1, 4, 2>);
+    if constexpr (DC == 6) {
+      if (row_tiles == 4) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 1, 4, 2>);
+    }
     if (row_tiles == 8) return reinterpret_cast<const void*>(lutgemm_attention_shared_kernel<BITS, DC, GU, 1, 8, 1>);
   }
   return nullptr;

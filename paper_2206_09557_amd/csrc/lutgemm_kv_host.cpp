@@ -15,9 +15,9 @@ AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q
   AttentionPlan p;
   const int64_t rows = (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads);
   // Up to 32 rows (16 of long heads) each wavefront holds all of them; beyond, eight wavefronts share them out (32 each, or 16) and
-  // the blocks' operands.
+  // the blocks' operands; of 256 channels 16 each, all eight of a block (two sets of four do not fit their registers).
   const int most_tiles = head_dim <= 128 ? 16 : 8;
-  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 && head_dim <= 128 ? 2 : 4);
+  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 && head_dim <= 128 ? 2 : (head_dim == 256 ? 8 : 4));
   while (p.row_tiles >= 4 && p.row_tiles < most_tiles && 16 * p.row_tiles < rows) p.row_tiles *= 2;
   p.row_blocks = (int)std::max<int64_t>(1, (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
   const int64_t units = (int64_t)seqs * heads * p.row_blocks;
