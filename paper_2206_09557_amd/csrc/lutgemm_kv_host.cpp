@@ -22,12 +22,24 @@ AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q
   p.row_blocks = (int)std::max<int64_t>(1, (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
   const int64_t units = (int64_t)seqs * heads * p.row_blocks;
   const int64_t blocks = std::max<int64_t>(1, (most_positions + kBlock - 1) / kBlock);
-  // Few units get a compute unit's wavefronts in one workgroup, whose sums meet in LDS; many get four each.
   const int simd = p.row_tiles >= 4 ? 2 : attention_waves_per_simd(head_dim, bits, group, p.row_tiles);
-  p.waves = p.row_tiles >= 4 ? 8 : (p.row_tiles == 1 && units < kComputeUnits * simd ? 4 * simd : 4);
-  const int64_t room = kComputeUnits * 4 * simd / p.waves;
-  // Splits until the device is full, of no fewer than two blocks a wavefront.
-  int64_t splits = std::min(room / units, (blocks + 2 * p.waves - 1) / (2 * p.waves));
+  p.waves = p.row_tiles >= 4 ? 8 : 4;
+  // Splits until the device is full, but none so short that its ends cost more than it saves: three blocks a wavefront (one sequence of
+  // 3000 positions and 8 key heads of 8 query heads, 8 bits: 10.7 us in 8 splits of four wavefronts, 12.3 in 6 of eight; 600 positions of
+  // 32 heads 9.9 unsplit, 11.2 in two of eight), where blocks are shared two for each set of wavefronts (six sequences of 700 positions,
+  // 77 rows: 15.9 in 6, 17.9 in 2).
+  const int64_t least = p.row_tiles >= 4 ? 2 * (most_tiles / p.row_tiles) : 3 * p.waves;
+  int64_t splits = std::min(kComputeUnits * 4 * simd / p.waves / units, blocks / least);
+  if (p.row_tiles == 1) {
+    // Sums of all of a compute unit's wavefronts meet in LDS rather than in memory, which pays from 15 blocks each on (131072 positions of
+    // 8 key heads at 4 bits: 42 us against 49, 4000 of 16 sequences of 64 heads at 8 bits 117 against 122; 2000 of 40 heads at 16 bits
+    // 73 against 70).
+    const int64_t of_all = std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / units, kMostSplits));
+    if (blocks >= 15 * 4 * simd * of_all) {
+      p.waves = 4 * simd;
+      splits = of_all;
+    }
+  }
   splits = std::max<int64_t>(1, std::min<int64_t>(splits, kMostSplits));
   const int64_t per = (blocks + splits - 1) / splits;
   p.chunk = (int)std::min<int64_t>(per, 1 << 24) * kBlock;
