@@ -68,7 +68,7 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinAhead = 4;      // splits that a thread asks for at once
 constexpr float kSlack = 8.0f;    // how far, in powers of two, a score may pass the kept maximum: weights up to 2^8 in fp16
 
 // Partial results that cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
@@ -681,10 +681,11 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
 
 // The splits' sums meet, in their order.  DIM / 4 lanes take a row, four channels each; `sharers` such sets share a row's splits where
 // there are many.  blockIdx as in the kernels before, .x counting rows.  Nothing here is work: what it takes is
-// a trip to memory, so all of it is asked for at once, before the sequence's length says how many splits there are.
+// a trip to memory, so all of it is asked for at once, before the sequence's length says how many splits there are, by as many wavefronts as
+// there is room for (16384 rows of 128 channels in 4 splits: 10 us; with eight splits a thread in flight, two wavefronts a SIMD, 19).
 template <int DIM>
-__global__ __launch_bounds__(kJoinThreads) void lutgemm_attention_join_kernel(Params p, int block_rows, int sharers) {
-  constexpr int kLanes = DIM / 4, kSets = kJoinThreads / kLanes, kAhead = 8;       // (48 lanes: some threads idle)
+__global__ __launch_bounds__(kJoinThreads, DIM == 64 ? 7 : 8) void lutgemm_attention_join_kernel(Params p, int block_rows, int sharers) {
+  constexpr int kLanes = DIM / 4, kSets = kJoinThreads / kLanes, kAhead = kJoinAhead;       // (48 lanes: some threads idle)
   __shared__ __attribute__((aligned(16))) float shares[kSets][DIM];
   __shared__ float share_total[kSets];
   __shared__ float2v ends[kSets][kMostSplits];                    // of a row: top, total of every split
@@ -1206,10 +1207,10 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
                       static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return LUTGEMM_EHIP;
   if (plan.splits == 1 || plan.row_tiles == 1) return LUTGEMM_OK;      // (of 16 rows the last workgroup adds the splits)
-  // Sets of DIM / 4 lanes in a workgroup; up to eight splits a set.
+  // Sets of DIM / 4 lanes in a workgroup; up to four splits a set.
   const int sets = kJoinThreads / (d / 4);
   int sharers = 1, block_rows = 16 * plan.row_tiles;
-  while (2 * sharers <= sets && sharers * 8 < plan.splits) sharers *= 2;
+  while (2 * sharers <= sets && sharers * kJoinAhead < plan.splits) sharers *= 2;
   const int rows = sets / sharers;
   const void* join = d == 64    ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<64>)
                      : d == 96  ? reinterpret_cast<const void*>(lutgemm_attention_join_kernel<96>)
