@@ -480,17 +480,21 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
     }
   }
   if (span.whole) return;
-  for (int place = span.from; place < span.to; ++place) {
-    if (p.rows && p.rows[span.row0 + place] < 0) continue;
-    if (place >> 3 != eight || all) continue;
-    const int e = place & 7, byte = BITS == 4 ? (e & 4) + ((e & 1) << 1 | (e >> 1 & 1)) : e;
+#pragma unroll 1
+  for (int e = 0; e < 8; ++e) {
+    const int place = 8 * eight + e, byte = BITS == 4 ? (e & 4) + ((e & 1) << 1 | (e >> 1 & 1)) : e;
+    if (all || place < span.from || place >= span.to || (p.rows && p.rows[span.row0 + place] < 0)) continue;
+    const unsigned char* from = codes + place * kPitch + channel * (BITS == 16 ? 2 : 1);
+    char* to = span.base + lane * (BITS == 4 ? 8 : 16) + byte * (BITS == 16 ? 2 : 1);
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
 #pragma unroll
       for (int j = 0; j < (BITS == 4 ? 1 : 2); ++j) {
-        const unsigned char* from = codes + place * kPitch + c * 4 * BITS + (j * 16 + channel) * (BITS == 16 ? 2 : 1);
-        if constexpr (BITS == 16) *reinterpret_cast<uint16_t*>(span.base + ((c * 2 + j) * 64 + lane) * 16 + e * 2) = *reinterpret_cast<const uint16_t*>(from);
-        if constexpr (BITS != 16) span.base[(c * 64 + lane) * 2 * BITS + j * 8 + byte] = (char)*from;
+        const unsigned char* code = from + c * 4 * BITS + j * BITS * 2;
+        if constexpr (BITS == 16)
+          *reinterpret_cast<uint16_t*>(to + (c * 2 + j) * 1024) = *reinterpret_cast<const uint16_t*>(code);
+        else
+          to[c * 128 * BITS + j * 8] = (char)*code;
       }
     }
   }

@@ -9,19 +9,25 @@ namespace lutgemm_kv_detail {
 
 namespace {
 constexpr int64_t kComputeUnits = 256;
+
+// Share of the device that is at work while workgroups come in rounds of `room`.
+double filled(int64_t workgroups, int64_t room) { return (double)workgroups / (double)(room * ((workgroups + room - 1) / room)); }
 }  // namespace
 
 AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q_heads, int seqs, int most_tokens, int64_t most_positions) {
   AttentionPlan p;
   const int64_t rows = (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads);
+  const int64_t blocks = std::max<int64_t>(1, (most_positions + kBlock - 1) / kBlock);
   // Up to 32 rows (16 of long heads) each wavefront holds all of them; beyond, eight wavefronts share them out (32 each, or 16) and
   // the blocks' operands; of 256 channels 16 each, all eight of a block (two sets of four do not fit their registers).
+  // A few blocks are worked on 32 rows at a time also where there are more, if the device has room for that many workgroups (265 rows over 81
+  // positions, 30 key heads: 9.5 us, all rows of a head in two workgroups 17.9).
   const int most_tiles = head_dim <= 128 ? 16 : 8;
-  p.row_tiles = rows <= 16 ? 1 : (rows <= 32 && head_dim <= 128 ? 2 : (head_dim == 256 ? 8 : 4));
+  const bool small = blocks <= 8 && (int64_t)seqs * heads * ((rows + 31) / 32) <= 4 * kComputeUnits;
+  p.row_tiles = rows <= 16 ? 1 : ((rows <= 32 || small) && head_dim <= 128 ? 2 : (head_dim == 256 ? 8 : 4));
   while (p.row_tiles >= 4 && p.row_tiles < most_tiles && 16 * p.row_tiles < rows) p.row_tiles *= 2;
   p.row_blocks = (int)std::max<int64_t>(1, (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
   const int64_t units = (int64_t)seqs * heads * p.row_blocks;
-  const int64_t blocks = std::max<int64_t>(1, (most_positions + kBlock - 1) / kBlock);
   const int simd = p.row_tiles >= 4 ? 2 : attention_waves_per_simd(head_dim, bits, group, p.row_tiles);
   p.waves = p.row_tiles >= 4 ? 8 : 4;
   // Splits until the device is full, but none so short that its ends cost more than it saves: three blocks a wavefront (one sequence of
@@ -29,18 +35,23 @@ AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q
   // 32 heads 9.9 unsplit, 11.2 in two of eight), where blocks are shared two for each set of wavefronts (six sequences of 700 positions,
   // 77 rows: 15.9 in 6, 17.9 in 2).
   const int64_t least = p.row_tiles >= 4 ? 2 * (most_tiles / p.row_tiles) : 3 * p.waves;
-  int64_t splits = std::min(kComputeUnits * 4 * simd / p.waves / units, blocks / least);
+  const int64_t room = kComputeUnits * 4 * simd / p.waves;
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>({room / units, blocks / least, kMostSplits}));
   if (p.row_tiles == 1) {
+    // What is added at the end grows with the splits, what is read before falls with them: no more than the square root of the blocks (80801
+    // positions of 4 key heads: 26 us in 50 to 64 splits, 32 in 127).
+    const int64_t root = (int64_t)std::sqrt((double)blocks);
+    splits = std::max<int64_t>(1, std::min(splits, root));
     // Sums of all of a compute unit's wavefronts meet in LDS rather than in memory, which pays from 15 blocks each on (131072 positions of
     // 8 key heads at 4 bits: 42 us against 49, 4000 of 16 sequences of 64 heads at 8 bits 117 against 122; 2000 of 40 heads at 16 bits
-    // 73 against 70).
-    const int64_t of_all = std::max<int64_t>(1, std::min<int64_t>(kComputeUnits / units, kMostSplits));
-    if (blocks >= 15 * 4 * simd * of_all) {
+    // 73 against 70) where that fills the device as well (20 sequences of 8 heads, 6600 positions: 160 workgroups 47, 480 of four
+    // wavefronts 41).
+    const int64_t of_all = std::max<int64_t>(1, std::min<int64_t>({kComputeUnits / units, root, kMostSplits}));
+    if (blocks >= 15 * 4 * simd * of_all && filled(units * of_all, kComputeUnits) >= 0.85 * filled(units * splits, room)) {
       p.waves = 4 * simd;
       splits = of_all;
     }
   }
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, kMostSplits));
   const int64_t per = (blocks + splits - 1) / splits;
   p.chunk = (int)std::min<int64_t>(per, 1 << 24) * kBlock;
   p.splits = (int)((blocks + per - 1) / per);
