@@ -234,10 +234,20 @@ __device__ __forceinline__ Span span_of(const KvParams& p, int value) {
   return s;
 }
 
-// Most of the four lanes that hold a unit's runs.
+// What another of the four lanes that hold a unit's runs has: the next, or the one after.
 __device__ __forceinline__ uint32_t other_lane(uint32_t v, bool two) {
   return two ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true) : (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true);
 }
+// (By value: a conditional operator between an array's elements is one between their addresses, and keeps the array in memory.)
+__device__ __forceinline__ uint32_t either(bool which, uint32_t a, uint32_t b) { return which ? a : b; }
+// What lane k of the four holds.
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int k) {
+  return k == 0   ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x00, 0xf, 0xf, true)
+         : k == 1 ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x55, 0xf, 0xf, true)
+         : k == 2 ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xaa, 0xf, 0xf, true)
+                  : (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xff, 0xf, 0xf, true);
+}
+__device__ __forceinline__ float of_lane(float v, int k) { return __builtin_bit_cast(float, of_lane(__builtin_bit_cast(uint32_t, v), k)); }
 __device__ __forceinline__ uint32_t most_of(uint32_t a, uint32_t b) {        // of both 16-bit halves
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(ushort2v, a), __builtin_bit_cast(ushort2v, b)));
 }
@@ -330,63 +340,86 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
     }
   }
 
-  _Float16* scales = reinterpret_cast<_Float16*>(span.base + kCode);
+  // The groups' statistics, run j of group k in ends[2 k + j], which the four lanes of a row then share out: each works out the scales of every
+  // fourth, stores them, and gives them to the others (all of it by every lane took 4 of the write's 15 instructions a value at groups of 32).
+  constexpr int kGroups = BITS == 16 ? 0 : 2 * (DC / GU), kMine = (kGroups + 3) / 4;
+  Group mine[kMine > 0 ? kMine : 1];
+  if constexpr (BITS != 16) {
+    uint32_t ends[4 * kMine];
+#pragma unroll
+    for (int k = 0; k < 4 * kMine; ++k) {
+      if (k >= kGroups) {
+        ends[k] = 0u;
+        continue;
+      }
+      const int first = k / 2 * GU, j = k % 2;
+      uint32_t magnitude = 0;
+      half2v low = __builtin_bit_cast(half2v, x[first][j][0]), high = low;
+#pragma unroll
+      for (int c = first; c < first + GU; ++c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w = x[c][j][i];
+          if (BITS == 8) magnitude = most_of(magnitude, w & 0x7fff7fffu);
+          if (BITS == 4) {
+            low = least_of(low, __builtin_bit_cast(half2v, w));
+            high = most_of(high, __builtin_bit_cast(half2v, w));
+          }
+        }
+      }
+      if constexpr (BITS == 8) {
+        magnitude = max(magnitude & 0xffffu, magnitude >> 16);
+        magnitude = max(magnitude, other_lane(magnitude, false));
+        ends[k] = max(magnitude, other_lane(magnitude, true));
+      } else {
+        half2v e = {(_Float16)-__builtin_elementwise_minimum(low[0], low[1]), __builtin_elementwise_maximum(high[0], high[1])};
+        e = most_of(e, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, e), false)));
+        e = most_of(e, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, e), true)));
+        ends[k] = __builtin_bit_cast(uint32_t, e);
+      }
+    }
+    bool bad = false;
+    _Float16* scales = reinterpret_cast<_Float16*>(span.base + kCode);
+#pragma unroll
+    for (int m = 0; m < kMine; ++m) {
+      const uint32_t e = either(seat.quarter & 2, either(seat.quarter & 1, ends[4 * m + 3], ends[4 * m + 2]), either(seat.quarter & 1, ends[4 * m + 1], ends[4 * m]));
+      mine[m] = group_of_ends<BITS>(e, __builtin_bit_cast(half2v, e));
+      bad = bad || mine[m].bad;
+      const int k = 4 * m + seat.quarter, j = k & 1;
+      if (k >= kGroups || !either(j, live[1], live[0])) continue;
+      _Float16* to = scales + (k >> 1) * (BITS == 8 ? 32 : 64);
+      const int place = (int)either(j, seat.place[1], seat.place[0]);
+      if (value) {
+        to[place] = mine[m].scale_bits;
+        if (BITS == 4) to[place + 32] = mine[m].offset_bits;
+      } else if (BITS == 8) {
+        to[seat.lane % 16 * 2 + j] = mine[m].scale_bits;
+      } else {
+        reinterpret_cast<uint32_t*>(to)[seat.lane % 16 * 2 + j] = bits_of(mine[m].scale_bits) | bits_of(mine[m].offset_bits) << 16;
+      }
+    }
+    if (__any(bad)) {                                // codes of a group with an infinity or a NaN are zeros'
+#pragma unroll
+      for (int k = 0; k < kGroups; ++k) {
+        const bool gone = of_lane(mine[k / 4].bad ? 1u : 0u, k % 4) != 0u;
+#pragma unroll
+        for (int c = k / 2 * GU; c < k / 2 * GU + GU; ++c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[c][k % 2][i] = gone ? 0u : x[c][k % 2][i];
+        }
+      }
+    }
+  }
 #pragma unroll
   for (int first = 0; first < DC; first += GU) {
     Group group[2];
     if constexpr (BITS != 16) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        uint32_t magnitude = 0;
-        half2v low = half2v{half_of(x[first][j][0]), half_of(x[first][j][0])}, high = low, ends = {0, 0};
-#pragma unroll
-        for (int c = first; c < first + GU; ++c) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (BITS == 8) magnitude = most_of(magnitude, x[c][j][i] & 0x7fff7fffu);
-            const uint32_t w = x[c][j][i];
-            if (BITS == 4) {
-              low = least_of(low, __builtin_bit_cast(half2v, w));
-              high = most_of(high, __builtin_bit_cast(half2v, w));
-            }
-          }
-        }
-        magnitude = max(magnitude & 0xffffu, magnitude >> 16);
-        if constexpr (BITS == 8) {
-          magnitude = max(magnitude, other_lane(magnitude, false));
-          magnitude = max(magnitude, other_lane(magnitude, true));
-        } else {
-          ends = half2v{(_Float16)-__builtin_elementwise_minimum(low[0], low[1]), __builtin_elementwise_maximum(high[0], high[1])};
-          ends = most_of(ends, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, ends), false)));
-          ends = most_of(ends, __builtin_bit_cast(half2v, other_lane(__builtin_bit_cast(uint32_t, ends), true)));
-        }
-        group[j] = group_of_ends<BITS>(magnitude, ends);
-      }
-      if (__any(group[0].bad || group[1].bad)) {     // their codes are zeros'
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int c = first; c < first + GU; ++c) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[c][j][i] = group[j].bad ? 0u : x[c][j][i];
-          }
-        }
-      }
-      if (seat.quarter == 0) {
-        constexpr int kHalves = BITS == 8 ? 32 : 64;  // of a group
-        _Float16* to = scales + first / GU * kHalves;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (!live[j]) continue;
-          if (value) {
-            to[seat.place[j]] = group[j].scale_bits;
-            if (BITS == 4) to[seat.place[j] + 32] = group[j].offset_bits;
-          } else if (BITS == 8) {
-            to[seat.lane * 2 + j] = group[j].scale_bits;
-          } else {
-            reinterpret_cast<uint32_t*>(to)[seat.lane * 2 + j] = bits_of(group[j].scale_bits) | bits_of(group[j].offset_bits) << 16;
-          }
-        }
+        const int k = first / GU * 2 + j;
+        group[j].scale = of_lane(mine[k / 4].scale, k % 4);
+        group[j].reciprocal = of_lane(mine[k / 4].reciprocal, k % 4);
+        group[j].offset = BITS == 4 ? of_lane(mine[k / 4].offset, k % 4) : 0.0f;
       }
     }
 #pragma unroll
