@@ -14,7 +14,7 @@
 // At the end the wavefronts' sums meet in LDS, and where the positions are split the splits' sums meet in memory: of up to 16 rows the
 // last workgroup to arrive adds them (the hand-off is the one of finish_row_range in lutgemm_device.hip: write-through
 // stores, a wait for them, a barrier, a relaxed counter), of more rows a second small kernel.  Both add in the order of
-// the splits.  131072 positions of one sequence in 32 splits: meeting in LDS, handing off and adding take 8 us of 42.
+// the splits.  131072 positions of one sequence in 32 splits: meeting in LDS, handing off and adding take 8 us of 40.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -806,7 +806,9 @@ __device__ __forceinline__ Memory block_address(const Blocks& b, int page, int i
 
 // Few rows: every wavefront takes all of them, and blocks of its own, from memory straight into registers.  Two blocks are on
 // their way while one is worked on: a set's keys are asked for when the set's last ones have met the queries, its values
-// when those have been added.
+// when those have been added.  Bound by the stream of codes where it is long (16 sequences of 64 heads, up to 4000 positions at 8 bits:
+// 654 MB in 113 us, 5.8 TB/s where a read-only kernel has 6.9), else by what begins and ends it: the chain lengths, page, codes,
+// and the sums (331 positions of 40 heads at 16 bits 6.2 us, of which an empty kernel takes 2).
 // BITS of a code, DC units of 32 channels to a head, GU of them to a scale, RT tiles of 16 rows.
 template <int BITS, int DC, int GU, int RT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS, GU * 32, RT)) void lutgemm_attention_kernel(Params p) {
@@ -906,6 +908,9 @@ __global__ __launch_bounds__(WAVES * 64, attention_waves_per_simd(DC * 32, BITS,
 // each operand of 16 bytes a lane is asked for as soon as the product before it has used the register, so a block's values are in
 // registers when its keys have been used.  (The last operands of a block are put one barrier before the early four
 // read them, and the late four have read a block one barrier before the early four put another in its place.)
+// Bound by both kinds of instruction, which hide under each other in part only: with 256 rows of 128 channels a block takes 1.0 us, its
+// products alone 0.5, its vector instructions alone 0.8 (64 tokens x 8 query heads a key head over 4 x 8192 positions at 8 bits: 93 us,
+// 750 TFLOP/s, of which the sums' way through memory and the second kernel are 20; all eight wavefronts in step, 112).
 template <int BITS, int DC, int GU, int RT, int GROUPS_R, int PARTS>
 __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_shared_kernel(Params p) {
   constexpr int kEach = (2 * DC + GROUPS_R - 1) / GROUPS_R;        // units of a wavefront
