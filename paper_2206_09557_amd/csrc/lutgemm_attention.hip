@@ -697,7 +697,7 @@ __global__ __launch_bounds__(kJoinThreads, DIM == 64 ? 7 : 8) void lutgemm_atten
   w.row_block = blockIdx.y - w.head * p.row_blocks;
   const float* partial = partial_of(p, w, 0, DIM);
   const int64_t next = (int64_t)p.partial_rows * (DIM + 2);
-  const bool held = set < kSets && row < p.partial_rows;
+  const bool held = set < kSets / sharers * sharers && row < p.partial_rows;       // (sets that make up no row are idle)
   const float* sums = partial + row * DIM + 4 * lane;
   float4v ahead[kAhead];
 #pragma unroll
