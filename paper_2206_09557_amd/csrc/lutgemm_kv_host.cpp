@@ -32,9 +32,10 @@ AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q
   p.waves = p.row_tiles >= 4 ? 8 : 4;
   // Splits until the device is full, but none so short that its ends cost more than it saves: three blocks a wavefront (one sequence of
   // 3000 positions and 8 key heads of 8 query heads, 8 bits: 10.7 us in 8 splits of four wavefronts, 12.3 in 6 of eight; 600 positions of
-  // 32 heads 9.9 unsplit, 11.2 in two of eight), where blocks are shared two for each set of wavefronts (six sequences of 700 positions,
-  // 77 rows: 15.9 in 6, 17.9 in 2).
-  const int64_t least = p.row_tiles >= 4 ? 2 * (most_tiles / p.row_tiles) : 3 * p.waves;
+  // 32 heads 9.9 unsplit, 11.2 in two of eight), two at up to 32 rows (6000 positions, 20 rows: 12.2 in 24, 15.1 in 15), and where
+  // wavefronts share a block two or, in sets that take blocks in turn, four a split (6000 positions, 100 rows: 17.6 in 38, 25.8 in 8;
+  // 3000 positions, 64 rows, 2 key heads: 15.6 in 24, 18.4 in 11).
+  const int64_t least = p.row_tiles >= 4 ? (p.row_tiles == most_tiles ? 2 : 4) : (p.row_tiles == 2 ? 2 : 3) * p.waves;
   const int64_t room = kComputeUnits * 4 * simd / p.waves;
   int64_t splits = std::max<int64_t>(1, std::min<int64_t>({room / units, blocks / least, kMostSplits}));
   if (p.row_tiles == 1) {

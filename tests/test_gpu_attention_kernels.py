@@ -9,6 +9,7 @@ from oracle import kv_oracle as K
 
 from gpu_util import make_workspace, torch_cuda
 from kv_util import Cache, keys_and_values, stream, up
+import test_gpu_kv_cache
 from test_gpu_attention import _check, _fill, _run, _tree
 
 pytestmark = pytest.mark.gpu
@@ -106,6 +107,11 @@ def test_all_wavefronts_of_a_compute_unit():
             plan = L.lutgemm_plan_attention(c, s, 1, positions)
             found.add((plan[4], plan[2] > 1))
     assert {(8, False), (8, True), (12, False), (12, True)} <= found, found
+
+
+@pytest.mark.parametrize("bits,dim,group", [c for c in CASES if c not in test_gpu_kv_cache.CASES and c[0] != 16])
+def test_every_group_is_written_and_read(bits, dim, group):
+    test_gpu_kv_cache.test_bytes_and_values(bits, dim, group)
 
 
 def test_a_long_read_past_the_caches():
