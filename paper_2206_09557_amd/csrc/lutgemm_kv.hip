@@ -188,15 +188,6 @@ __device__ __forceinline__ Rows rows_of(const KvParams& p, int seq) {
   r.past = max(p.past[seq], 0);
   return r;
 }
-// The block that holds positions 32 * block .. of a sequence for a head; null where there is none.
-__device__ __forceinline__ char* block_at(const KvParams& p, int seq, int block, int head) {
-  const int col = block / p.page_blocks;
-  if (col >= p.table_pages) return nullptr;
-  const int page = p.table[(int64_t)seq * p.table_pages + col];
-  if (page < 0 || page >= p.pages) return nullptr;
-  return p.pool + (((int64_t)page * p.heads + head) * p.page_blocks + (block - col * p.page_blocks)) * p.block_bytes;
-}
-
 // (By value: a bit cast of a vector's element in place takes the vector's first.)
 __device__ __forceinline__ uint32_t bits_of(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
 __device__ __forceinline__ _Float16 half_of(uint32_t bits) { return __builtin_bit_cast(_Float16, (uint16_t)bits); }
@@ -216,22 +207,29 @@ __device__ __forceinline__ Seat seat_of(int lane) {
 
 // The block of this wavefront and its live places.
 struct Span {
-  char* base;                  // of its keys or values; null: there is no page
   int64_t row0;                // row of place 0
   int from, to;                // live places; from >= to: nothing to do
+  int page, in_page;           // page number as the table has it (-1: beyond the table), block in the page
   bool whole;
 };
-__device__ __forceinline__ Span span_of(const KvParams& p, int value) {
+__device__ __forceinline__ Span span_of(const KvParams& p) {
   const Rows rows = rows_of(p, blockIdx.z);
   const int64_t end = (int64_t)rows.past + rows.count, block = rows.past / kBlock + (int64_t)blockIdx.x;
-  Span s = {nullptr, rows.row + block * kBlock - rows.past, 0, 0, false};
+  Span s = {rows.row + block * kBlock - rows.past, 0, 0, -1, 0, false};
   if (block * kBlock >= end || rows.count == 0) return s;
   s.from = (int)max(rows.past - block * kBlock, (int64_t)0);
   s.to = (int)min(end - block * kBlock, (int64_t)kBlock);
-  s.base = block > INT32_MAX ? nullptr : block_at(p, blockIdx.z, (int)block, blockIdx.y);
-  if (s.base && value) s.base += p.value_offset;
   s.whole = s.from == 0 && s.to == kBlock && !p.rows;
+  const int col = (int)min(block, (int64_t)INT32_MAX) / p.page_blocks;
+  s.in_page = (int)(block - (int64_t)col * p.page_blocks);
+  const int page = p.table[(int64_t)blockIdx.z * p.table_pages + min(col, p.table_pages - 1)];
+  s.page = col < p.table_pages ? page : -1;
   return s;
+}
+// Its keys or values; null where there is no page.
+__device__ __forceinline__ char* base_of(const KvParams& p, const Span& s, int value) {
+  if (s.page < 0 || s.page >= p.pages) return nullptr;
+  return p.pool + (((int64_t)s.page * p.heads + blockIdx.y) * p.page_blocks + s.in_page) * p.block_bytes + (value ? p.value_offset : 0);
 }
 
 // What another of the four lanes that hold a unit's runs has: the next, or the one after.
@@ -318,11 +316,11 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
   const _Float16* source = static_cast<const _Float16*>(value ? p.v : p.k);
   const int64_t stride = value ? p.v_stride : p.k_stride;
   if (!source) return;
-  const Span span = span_of(p, value);
-  if (!span.base) return;
+  const Span span = span_of(p);
+  if (span.from >= span.to) return;
   const Seat seat = seat_of(lane);
 
-  u32x4 x[DC][2];
+  u32x4 x[DC][2];                                   // (on their way while the page table is looked up)
   bool live[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -342,6 +340,8 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
     }
   }
 
+  char* base = base_of(p, span, value);
+  if (!base) return;
   // The groups' statistics, run j of group k in ends[2 k + j], which the four lanes of a row then share out: each works out the scales of every
   // fourth, stores them, and gives them to the others (all of it by every lane took 4 of the write's 15 instructions a value at groups of 32).
   constexpr int kGroups = BITS == 16 ? 0 : 2 * (DC / GU), kMine = (kGroups + 3) / 4;
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
       }
     }
     bool bad = false;
-    _Float16* scales = reinterpret_cast<_Float16*>(span.base + kCode);
+    _Float16* scales = reinterpret_cast<_Float16*>(base + kCode);
 #pragma unroll
     for (int m = 0; m < kMine; ++m) {
       const uint32_t e = either(seat.quarter & 2, either(seat.quarter & 1, ends[4 * m + 3], ends[4 * m + 2]), either(seat.quarter & 1, ends[4 * m + 1], ends[4 * m]));
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
             if (seat.quarter < 2) *reinterpret_cast<u32x2*>(to + seat.quarter * 8) = (u32x2){words[j][0], words[j][1]};
         }
       } else {
-        char* to = span.base + (BITS == 16 ? (c * 128 + seat.lane) * 16 : (c * 64 + seat.lane) * 2 * BITS);
+        char* to = base + (BITS == 16 ? (c * 128 + seat.lane) * 16 : (c * 64 + seat.lane) * 2 * BITS);
         if constexpr (BITS == 16) {
           if (live[0]) *reinterpret_cast<u32x4*>(to) = (u32x4){words[0][0], words[0][1], words[0][2], words[0][3]};
           if (live[1]) *reinterpret_cast<u32x4*>(to + 1024) = (u32x4){words[1][0], words[1][1], words[1][2], words[1][3]};
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
             const unsigned char* pair = from + 2 * i * kPitch + (c * 32 + j * 16 + channel) * 2;
             w[i] = *reinterpret_cast<const uint16_t*>(pair) | (uint32_t)*reinterpret_cast<const uint16_t*>(pair + kPitch) << 16;
           }
-          *reinterpret_cast<u32x4*>(span.base + ((c * 2 + j) * 64 + lane) * 16) = w;
+          *reinterpret_cast<u32x4*>(base + ((c * 2 + j) * 64 + lane) * 16) = w;
         }
       } else {
         constexpr int kWords = BITS / 2;
@@ -509,8 +509,8 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
           const unsigned char* b = from + e * kPitch + at;
           w[i] = BITS == 8 ? bytes_of(b[0], b[kPitch], b[2 * kPitch], b[3 * kPitch]) : bytes_of(b[0], b[2 * kPitch], b[kPitch], b[3 * kPitch]);
         }
-        if constexpr (BITS == 8) *reinterpret_cast<u32x4*>(span.base + (c * 64 + lane) * 16) = (u32x4){w[0], w[1], w[2], w[3]};
-        if constexpr (BITS == 4) *reinterpret_cast<u32x2*>(span.base + (c * 64 + lane) * 8) = (u32x2){w[0], w[1]};
+        if constexpr (BITS == 8) *reinterpret_cast<u32x4*>(base + (c * 64 + lane) * 16) = (u32x4){w[0], w[1], w[2], w[3]};
+        if constexpr (BITS == 4) *reinterpret_cast<u32x2*>(base + (c * 64 + lane) * 8) = (u32x2){w[0], w[1]};
       }
     }
   }
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
     const int place = 8 * eight + e, byte = BITS == 4 ? (e & 4) + ((e & 1) << 1 | (e >> 1 & 1)) : e;
     if (all || place < span.from || place >= span.to || (p.rows && p.rows[span.row0 + place] < 0)) continue;
     const unsigned char* from = codes + place * kPitch + channel * (BITS == 16 ? 2 : 1);
-    char* to = span.base + lane * (BITS == 4 ? 8 : 16) + byte * (BITS == 16 ? 2 : 1);
+    char* to = base + lane * (BITS == 4 ? 8 : 16) + byte * (BITS == 16 ? 2 : 1);
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
 #pragma unroll
@@ -558,15 +558,16 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_read_kernel(KvParams p)
   _Float16* target = static_cast<_Float16*>(const_cast<void*>(value ? p.v : p.k));
   const int64_t stride = value ? p.v_stride : p.k_stride;
   if (!target) return;
-  const Span span = span_of(p, value);
+  const Span span = span_of(p);
   if (span.from >= span.to) return;
+  const char* base = base_of(p, span, value);
   unsigned char* half = lds + value * kBytes;
-  if (span.base) {
+  if (base) {
     u32x4 piece[(kBytes / 16 + 63) / 64];
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(piece) / 16); ++i) {
       const int at = i * 64 + lane;
-      if (at < kBytes / 16) piece[i] = reinterpret_cast<const u32x4*>(span.base)[at];
+      if (at < kBytes / 16) piece[i] = reinterpret_cast<const u32x4*>(base)[at];
     }
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(piece) / 16); ++i) {
@@ -584,7 +585,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_read_kernel(KvParams p)
     const int key_lane = 16 * quarter + pair;                                        // of a key's codes
     const int value_lane = 16 * eight + 8 * (quarter & 1), upper = quarter >> 1;     // of the first of eight values' codes
     u32x4 x[2] = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
-    if (span.base) {
+    if (base) {
       if constexpr (BITS == 16) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
