@@ -479,7 +479,8 @@ int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, 
                      how the work is split depends on it: the result is right for longer ones too
      workspace       lutgemm_attention_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any
                      other and shared with products on the same stream if large enough
-   Products and sums are fp32, the weights w are rounded to fp16 before they meet V.  Infinities and NaNs in positions that a row does
+   Products and sums are fp32, the weights w are rounded to fp16 before they meet V (a weight of less than 2^-25 of its row's
+   largest counts for nothing).  Infinities and NaNs in positions that a row does
    not see do not reach it.  Bitwise reproducible.                                        */
 int lutgemm_attention(const void* q, const uint64_t* mask, const lutgemm_kv_cache* cache, const lutgemm_kv_step* step,
                       void* y, int q_heads, int64_t q_stride, int64_t y_stride, float scale, int64_t most_positions,
