@@ -478,7 +478,8 @@ int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, 
      most_positions  of the longest sequence after this step; 0: as many as the table holds.  Only
                      how the work is split depends on it: the result is right for longer ones too
      workspace       lutgemm_attention_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any
-                     other and shared with products on the same stream if large enough
+                     other and shared with products on the same stream if large enough.  It grows neither with the new tokens nor
+                     with most_positions throughout (more of them can mean fewer splits): ask for each that will be used
    Products and sums are fp32, the weights w are rounded to fp16 before they meet V (a weight of less than 2^-25 of its row's
    largest counts for nothing).  Infinities and NaNs in positions that a row does
    not see do not reach it.  Bitwise reproducible.                                        */

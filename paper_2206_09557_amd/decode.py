@@ -49,9 +49,10 @@ class AttentionHalf:
         self.qkv = torch.empty(MOST_ROWS, self.row, dtype=torch.float16, device="cuda")
         self.mixed = torch.empty(MOST_ROWS, heads * head_dim, dtype=torch.float16, device="cuda")
         self.step = L.lutgemm_kv_step(self.first, self.past, self.table, seqs, pages, MOST_ROWS, MOST_ROWS)
-        # one workspace for all of it, of the largest step
-        self.ws_bytes = max([L.lutgemm_workspace_bytes(m, n, q, g, 8, b) for m, n in self.shapes() for b in (1, MOST_ROWS)] +
-                            [L.lutgemm_attention_workspace_bytes(self.cache, self._step(t, t), heads, longest) for t in (1, MOST_ROWS)])
+        # one workspace for all of it: for every number of tokens, as attention's need does not grow with them (where more rows make another
+        # plan there may be fewer splits)
+        self.ws_bytes = max([L.lutgemm_workspace_bytes(m, n, q, g, 8, b) for m, n in self.shapes() for b in range(1, MOST_ROWS + 1)] +
+                            [L.lutgemm_attention_workspace_bytes(self.cache, self._step(t, t), heads, longest) for t in range(1, MOST_ROWS + 1)])
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
         L.lutgemm_workspace_init(self.ws, self.ws_bytes, self._stream())
 
