@@ -412,7 +412,7 @@ __device__ __forceinline__ bool find_place(const Params& p, int block_rows, int 
   w->head = blockIdx.y / p.row_blocks;
   w->row_block = blockIdx.y - w->head * p.row_blocks;
   w->row_first = max(p.first[w->seq], 0);
-  const int count = min(min(p.first[w->seq + 1], p.tokens) - w->row_first, p.most_tokens);   // (at most kMostTokens)
+  const int count = min(min(max(p.first[w->seq + 1], 0), p.tokens) - w->row_first, p.most_tokens);   // (at most kMostTokens)
   w->past = max(p.past[w->seq], 0);
   w->rows = count * p.shared;
   w->row0 = w->row_block * block_rows;

@@ -182,7 +182,7 @@ struct Rows {
 };
 __device__ __forceinline__ Rows rows_of(const KvParams& p, int seq) {
   Rows r;
-  const int lo = max(p.first[seq], 0), hi = min(p.first[seq + 1], p.tokens);
+  const int lo = max(p.first[seq], 0), hi = min(max(p.first[seq + 1], 0), p.tokens);      // (hi - lo fits 32 bits)
   r.row = lo;
   r.count = max(hi - lo, 0);
   r.past = max(p.past[seq], 0);
