@@ -1044,7 +1044,7 @@ __global__ __launch_bounds__(GROUPS_R * PARTS * 64, 2) void lutgemm_attention_sh
     half8v weight[RT];
     find();
     if (!idle) {
-      const int limit = none ? -(1 << 30) : limit_of_rows, place = block * kBlock + 8 * quarter - w.past;
+      const int limit = none ? INT32_MIN : limit_of_rows, place = block * kBlock + 8 * quarter - w.past;
       uint32_t visible[RT];
 #pragma unroll
       for (int t = 0; t < RT; ++t) {

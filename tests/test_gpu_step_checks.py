@@ -65,3 +65,26 @@ def test_rows_that_end_before_they_begin_see_nothing(shared, tiles, end):
     alone = L.lutgemm_kv_step(up(np.array([3, end], np.int32)), step._held[1], step._held[2], 1, 20, 6, 6)
     y = _run(cache, alone, q, None, shared, 0.125, 0, d_y=torch.full((6, shared * 64 + 8), 77.0, dtype=torch.float16, device="cuda"))
     assert (y == 77).all()
+
+
+@pytest.mark.parametrize("past", [(1 << 30) + 5, (1 << 31) - 7])
+@pytest.mark.parametrize("shared,tiles", [(1, 1), (4, 2), (16, 8), (43, 16)])
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_missing_page_of_a_sequence_longer_than_its_table(bits, shared, tiles, past):
+    """A length that no table holds: the rows see all that the table has, and nothing where it names no page."""
+    rng = np.random.default_rng(shared + bits)
+    cache = Cache(1, 20, 32, 1, 64, bits, 0, seed=5)
+    k, v = _fill(cache, rng, [634], [6])[0]
+    table = cache.table.copy()
+    seen = np.ones(640, bool)
+    for page in (0, 7, 8, 19):
+        table[0, page] = -1
+        seen[32 * page:32 * page + 32] = False
+    q = rng.standard_normal((6, shared, 64)).astype(np.float16)
+    step = cache.step([6], [past], table)
+    plan = L.lutgemm_plan_attention(cache.c, step, shared)
+    assert plan[0] == tiles
+    print("case missing page", bits, shared, past, plan, flush=True)
+    y = _run(cache, step, q, None, shared, 0.125, 0)
+    none = np.zeros((6, 1, 64), np.float16)
+    _check(y, *K.attention(q, np.concatenate([k[seen], none]), np.concatenate([v[seen], none]), int(seen.sum()), [0] * 6, 0.125), 64)
