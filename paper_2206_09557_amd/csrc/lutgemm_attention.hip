@@ -70,6 +70,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kJoinThreads = 256, kJoinAhead = 4;      // splits that a thread asks for at once
 constexpr float kSlack = 8.0f;    // how far, in powers of two, a score may pass the kept maximum: weights up to 2^8 in fp16
+// Scores that fp32 holds without fractions.  The weights' multiply-add brings back what rounding took off a maximum like that: from 2^28 on more
+// than fp16's exponents hold.  So these are rounded before the maximum, which is rounded too, is taken off.
+constexpr float kFar = 16777216.0f;
 
 // Partial results that cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
 // that are served from it (what a relaxed atomic of device scope is, but of 16 or 8 bytes).
@@ -356,6 +359,13 @@ __device__ __forceinline__ void block_scores(float4v (&score)[RT][2], const KeyW
   }
 }
 
+// (Not the first half of a multiply-add.)
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  const float c = a * b;
+  return c;
+}
+
 // The weights' turn: of one tile's eight positions a lane, as the next product's operand.  Of a block that not every row sees all of,
 // `visible` has a bit for each position (4 j + i: position 8 quarter + 4 j + i of the block).
 template <int DC, int RT>
@@ -367,22 +377,33 @@ __device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT
   float most = score[0][0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) most = fmaxf(most, score[i >> 2][i & 3]);
-  most *= scale;
-  if (__any(most > s.top[t] + kSlack)) {
+  float factor = scale, base = s.top[t];
+  if (__any(__builtin_fmaf(most, scale, -base) > kSlack)) {             // (as the weights are worked out: none passes 2^kSlack)
     most = max_of_column(most);
-    const float raised = most > s.top[t] + kSlack ? most : s.top[t];     // (a row's own need: others do not change its result)
-    const float shrink = raised == s.top[t] ? 1.0f : __builtin_amdgcn_exp2f(s.top[t] - raised);
-    s.top[t] = raised;
+    const bool own = __builtin_fmaf(most, scale, -base) > kSlack;       // (a row's own need: others do not change its result)
+    const float raised = own ? most * scale : base;
+    const float shrink = raised == base ? 1.0f : __builtin_amdgcn_exp2f(base - raised);
+    s.top[t] = base = raised;
     s.total[t] *= shrink;
 #pragma unroll
     for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= shrink;
+    const bool far = own && fabsf(raised) >= kFar;
+    if (__any(far)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = score[i >> 2][i & 3];
+        score[i >> 2][i & 3] = far ? rounded_product(x, scale) - raised : __builtin_fmaf(x, scale, -raised);
+      }
+      factor = 1.0f;
+      base = 0.0f;
+    }
   }
   half2v w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float2v e;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], scale, -s.top[t]));
+    for (int k = 0; k < 2; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], factor, -base));
     w[i] = __builtin_convertvector(e, half2v);
   }
   half8v weight = join(w[0], w[1], w[2], w[3]);

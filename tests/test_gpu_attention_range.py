@@ -1,0 +1,49 @@
+"""GPU checks of attention where scores or weights leave the ordinary range: scores too large for their differences to be
+told, one score far above a long tail, infinite ones."""
+import numpy as np
+import pytest
+
+import paper_2206_09557_amd as L
+from oracle import kv_oracle as K
+
+from kv_util import Cache, keys_and_values, stream, up
+from test_gpu_attention import _check, _run
+
+pytestmark = pytest.mark.gpu
+
+DIM = 64
+
+
+def _write(cache, k, v):
+    n = len(k)
+    L.lutgemm_kv_write(up(k.reshape(n, -1)), up(v.reshape(n, -1)), None, cache.c, cache.step([n], [0]), DIM, DIM, stream())
+
+
+def _scores(rng, scores):
+    """Keys whose first channel is `scores`, the rest zero; values as usual."""
+    k = np.zeros((len(scores), 1, DIM), np.float16)
+    k[:, 0, 0] = scores
+    return k, keys_and_values(rng, (len(scores), 1, DIM))
+
+
+@pytest.mark.parametrize("tokens,shared,tiles", [(2, 5, 1), (4, 5, 2), (10, 5, 4), (40, 5, 16)])
+@pytest.mark.parametrize("order", ["rising", "falling", "shuffled"])
+def test_scores_that_differ_by_more_than_any_weight(tokens, shared, tiles, order):
+    """Up to 5e9, where fp32 counts in hundreds: the largest takes all, and its value comes out as it is."""
+    rng = np.random.default_rng(tokens)
+    n = 700 + tokens
+    at = np.linspace(-60000, 60000, n)
+    k, v = _scores(rng, {"rising": at, "falling": at[::-1], "shuffled": rng.permutation(at)}[order])
+    cache = Cache(1, 30, 64, 1, DIM, 16, 0)
+    _write(cache, k, v)
+    q = np.zeros((tokens, shared, DIM), np.float16)
+    q[..., 0] = np.linspace(30000, 60000, tokens * shared).reshape(tokens, shared)
+    q[0, 0, 0] = -60000
+    step = cache.step([tokens], [700])
+    plan = L.lutgemm_plan_attention(cache.c, step, shared)
+    assert plan[0] == tiles
+    print("case large", tokens, shared, order, plan, flush=True)
+    y = _run(cache, step, q, None, shared, 1.0, 0).reshape(tokens * shared, DIM)
+    for r in range(tokens * shared):
+        seen = k[:701 + r // shared, 0, 0].astype(np.float64) * float(q[r // shared, r % shared, 0])
+        np.testing.assert_array_equal(y[r], v[int(seen.argmax()), 0])
