@@ -480,8 +480,8 @@ int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, 
      workspace       lutgemm_attention_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any
                      other and shared with products on the same stream if large enough.  It grows neither with the new tokens nor
                      with most_positions throughout (more of them can mean fewer splits): ask for each that will be used
-   Products and sums are fp32, the weights w are rounded to fp16 before they meet V (a weight of less than 2^-25 of its row's
-   largest counts for nothing).  Infinities and NaNs in positions that a row does
+   Products and sums are fp32, the weights w are rounded to fp16 before they meet V (by 2^-11 of themselves, or 2^-32 of
+   their row's largest where that is more).  Infinities and NaNs in positions that a row does
    not see do not reach it.  Bitwise reproducible.                                        */
 int lutgemm_attention(const void* q, const uint64_t* mask, const lutgemm_kv_cache* cache, const lutgemm_kv_step* step,
                       void* y, int q_heads, int64_t q_stride, int64_t y_stride, float scale, int64_t most_positions,

@@ -8,7 +8,7 @@
 // so that a lane owns one row (its column) and eight positions of it, the softmax needs no exchange
 // between lanes but the maximum's, and its weights are the second product's operand as they stand: the cache's layout
 // deals the positions to the lanes so that they are (place 8 a + 4 j + b is row 4 a + b of the j-th tile of S^T).
-// The maximum that the weights are relative to is only raised where a score passes it by 2^8, which is seldom;
+// What the weights are relative to is only raised where a score passes it by 2^15, which is seldom;
 // the sum of the weights is one more product, of a tile of ones, so it adds what the other products add.
 //
 // At the end the wavefronts' sums meet in LDS, and where the positions are split the splits' sums meet in memory: of up to 16 rows the
@@ -69,7 +69,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kJoinThreads = 256, kJoinAhead = 4;      // splits that a thread asks for at once
-constexpr float kSlack = 8.0f;    // how far, in powers of two, a score may pass the kept maximum: weights up to 2^8 in fp16
+// Weights are fp16 where they meet the values, from 2^-14 (2^-25, with fewer bits) to 2^15.  What they are relative to is put kLift below a
+// score that raises it, and raised again where a score passes it by kSlack, all in powers of two: the row's largest is worth 2^7 to 2^15, and a
+// weight is off by 2^-32 of it at most where it is not by 2^-11 of itself.  (Relative to the score itself a weight would vanish at 2^-25 of the
+// largest, and some ten thousand of those together are 2^-11 of a result.)
+constexpr float kLift = 7.0f, kSlack = 15.0f;
 // Scores that fp32 holds without fractions.  The weights' multiply-add brings back what rounding took off a maximum like that: from 2^28 on more
 // than fp16's exponents hold.  So these are rounded before the maximum, which is rounded too, is taken off.
 constexpr float kFar = 16777216.0f;
@@ -381,7 +385,7 @@ __device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT
   if (__any(__builtin_fmaf(most, scale, -base) > kSlack)) {             // (as the weights are worked out: none passes 2^kSlack)
     most = max_of_column(most);
     const bool own = __builtin_fmaf(most, scale, -base) > kSlack;       // (a row's own need: others do not change its result)
-    const float raised = own ? most * scale : base;
+    const float raised = own ? rounded_product(most, scale) - kLift : base;
     const float shrink = raised == base ? 1.0f : __builtin_amdgcn_exp2f(base - raised);
     s.top[t] = base = raised;
     s.total[t] *= shrink;

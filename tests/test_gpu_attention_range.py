@@ -47,3 +47,30 @@ def test_scores_that_differ_by_more_than_any_weight(tokens, shared, tiles, order
     for r in range(tokens * shared):
         seen = k[:701 + r // shared, 0, 0].astype(np.float64) * float(q[r // shared, r % shared, 0])
         np.testing.assert_array_equal(y[r], v[int(seen.argmax()), 0])
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("tokens,shared,past,hint", [(1, 1, 4000, 32), (1, 4, 30000, 0), (3, 8, 9000, 0), (20, 5, 5000, 0), (20, 5, 300, 0)])
+def test_one_high_score_over_a_long_tail(bits, tokens, shared, past, hint):
+    """The first position's score stands above all others by up to 2^30; its value is zero, so that the result is the tail's share alone.
+    A weight is rounded to fp16, by 2^-32 of its row's largest at most, beside what every weight may be off."""
+    rng = np.random.default_rng(past)
+    n = past + tokens
+    k, v = _scores(rng, rng.uniform(-1, 0, n))
+    k[0, 0, 0] = 20
+    v[0] = 0
+    v[1:] = np.abs(v[1:])
+    cache = Cache(1, -(-n // 64), 64, 1, DIM, bits, 0)
+    _write(cache, k, v)
+    k, v = cache.rounded(k), cache.rounded(v)
+    q = np.zeros((tokens, shared, DIM), np.float16)
+    q[..., 0] = np.linspace(1.0, 0.55, tokens * shared).reshape(tokens, shared)
+    step = cache.step([tokens], [past])
+    print("case tail", bits, tokens, shared, past, L.lutgemm_plan_attention(cache.c, step, shared, hint), flush=True)
+    y = _run(cache, step, q, None, shared, 1.0, hint).astype(np.float64)
+    ref, mass, reach = K.attention(q, k, v, past, None, 1.0)
+    score = (DIM + 8) * 2.0 ** -24 * reach * 2 + 2.0 ** -20          # as in the other tests of attention
+    bound = 2.0 ** -11 * np.abs(ref) + (2.0 ** -10 + 2 * score) * mass + 2.0 ** -24 + 2.0 ** -32 * np.abs(v.astype(np.float64)).sum(0)
+    err = np.abs(y - ref)
+    worst = (err / bound).max()
+    assert worst <= 1
