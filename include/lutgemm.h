@@ -471,7 +471,7 @@ int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, 
    with the keys and values of head h / (q_heads / heads).  Token t of sequence s sees every position before past[s], and
    of the new ones position past[s] + j where bit j of mask[t] is set (a token that sees itself has its
    own bit set; bits beyond the sequence's tokens count for nothing).  mask NULL: each new token sees itself and those before it.  A
-   row that sees nothing is zero.  Up to 64 new tokens a sequence; a longer prompt is taken in chunks.
+   row that sees nothing, or nothing but scores of -inf, is zero.  Up to 64 new tokens a sequence; a longer prompt is taken in chunks.
      q, y            fp16 rows of q_stride / y_stride, heads one after the other; 16-byte aligned, strides
                      multiples of 8.  y must not overlap q
      mask            uint64 [tokens] or NULL

@@ -74,6 +74,7 @@ constexpr int kJoinThreads = 256, kJoinAhead = 4;      // splits that a thread a
 // weight is off by 2^-32 of it at most where it is not by 2^-11 of itself.  (Relative to the score itself a weight would vanish at 2^-25 of the
 // largest, and some ten thousand of those together are 2^-11 of a result.)
 constexpr float kLift = 7.0f, kSlack = 15.0f;
+constexpr float kNothing = -3.402823466e38f;      // what weights are relative to before a row has seen a score: finite, so that one of -inf weighs nothing
 // Scores that fp32 holds without fractions.  The weights' multiply-add brings back what rounding took off a maximum like that: from 2^28 on more
 // than fp16's exponents hold.  So these are rounded before the maximum, which is rounded too, is taken off.
 constexpr float kFar = 16777216.0f;
@@ -321,11 +322,8 @@ __device__ __forceinline__ int walk_page(const Walk<STEP>& w) {
   return w.col <= w.last_col && w.entry >= 0 && w.entry < w.pages ? w.entry : -1;
 }
 
-// Factor of a part's sums where parts meet: its top is at most `raised`.  A part that saw nothing has none; a NaN stays one.
-__device__ __forceinline__ float part_factor(float top, float raised, float total) {
-  if (top == -__builtin_inff()) return total == total ? 0.0f : total;
-  return __builtin_amdgcn_exp2f(top - raised);
-}
+// Factor of a part's sums where parts meet: its top is at most `raised`.  (A part that saw nothing has sums of zero; a NaN stays one.)
+__device__ __forceinline__ float part_factor(float top, float raised) { return __builtin_amdgcn_exp2f(top - raised); }
 // Row / query heads of a key head.  (row + 1/2) / shared is at least 1/2 / shared away from a whole number: 3e-5 at least, where the
 // product is off by 64 * 2^-23 at most.
 __device__ __forceinline__ int token_of(const Params& p, int row) { return (int)(((float)row + 0.5f) * p.inverse_shared); }
@@ -411,7 +409,7 @@ __device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT
     w[i] = __builtin_convertvector(e, half2v);
   }
   half8v weight = join(w[0], w[1], w[2], w[3]);
-  if (!whole) {                                  // (where a row has seen nothing yet its weights are no numbers)
+  if (!whole) {                                  // (with a scale of zero those that are not seen are no numbers)
     u32x4 m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) m[i] = (visible >> (2 * i) & 1u ? 0x0000ffffu : 0u) | (visible >> (2 * i + 1) & 1u ? 0xffff0000u : 0u);
@@ -455,7 +453,7 @@ template <int DC, int RT>
 __device__ __forceinline__ void clear_sums(Sums<DC, RT>& s) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    s.top[t] = -__builtin_inff();
+    s.top[t] = kNothing;
     s.total[t] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int u = 0; u < 2 * DC; ++u) s.out[t][u] = (float4v){0.0f, 0.0f, 0.0f, 0.0f};
@@ -587,12 +585,12 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
   static_assert(kRows * kLanes <= kThreads, "");
   if ((int)threadIdx.x < kRows * kLanes) {
     const int row = threadIdx.x / kLanes, k = threadIdx.x % kLanes;
-    float2v end = {-__builtin_inff(), 0.0f};
+    float2v end = {kNothing, 0.0f};
     if (k < PARTS) end = ends[k * kRows + row];
     float raised = end[0];
 #pragma unroll
     for (int d = kLanes / 2; d >= 1; d >>= 1) raised = fmaxf(raised, __shfl_xor(raised, d, kLanes));
-    const float factor = part_factor(end[0], raised, end[1]);
+    const float factor = part_factor(end[0], raised);
     float total = factor * end[1];
 #pragma unroll
     for (int d = kLanes / 2; d >= 1; d >>= 1) total += __shfl_xor(total, d, kLanes);
@@ -663,7 +661,7 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
     __syncthreads();
 #pragma unroll 1
     for (int row = threadIdx.x >> 4; row < live_rows; row += kThreads / 16) {      // sixteen lanes a row
-      float raised = -__builtin_inff(), sum = 0.0f;
+      float raised = kNothing, sum = 0.0f;
 #pragma unroll 1
       for (int i = column; i < w.active; i += 16) raised = fmaxf(raised, split_ends[row * w.active + i][0]);
 #pragma unroll
@@ -671,7 +669,7 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
 #pragma unroll 1
       for (int i = column; i < w.active; i += 16) {
         const float2v end = split_ends[row * w.active + i];
-        const float factor = part_factor(end[0], raised, end[1]);
+        const float factor = part_factor(end[0], raised);
         split_ends[row * w.active + i][0] = factor;
         sum += factor * end[1];
       }
@@ -737,11 +735,11 @@ __global__ __launch_bounds__(kJoinThreads, DIM == 64 ? 7 : 8) void lutgemm_atten
   float4v a = {0.0f, 0.0f, 0.0f, 0.0f};
   float total = 0.0f;
   if (live) {
-    float raised = -__builtin_inff();
+    float raised = kNothing;
     for (int i = 0; i < w.active; ++i) raised = fmaxf(raised, ends[slot][i][0]);
     auto add = [&](float4v v, int split) {
       const float2v end = ends[slot][split];
-      const float factor = part_factor(end[0], raised, end[1]);
+      const float factor = part_factor(end[0], raised);
       total += factor * end[1];
       a += v * factor;
     };

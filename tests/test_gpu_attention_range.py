@@ -74,3 +74,36 @@ def test_one_high_score_over_a_long_tail(bits, tokens, shared, past, hint):
     err = np.abs(y - ref)
     worst = (err / bound).max()
     assert worst <= 1
+
+
+@pytest.mark.parametrize("tokens,shared,tiles", [(2, 5, 1), (4, 5, 2), (10, 5, 4), (40, 5, 16)])
+@pytest.mark.parametrize("pages,first,last", [(8, 0, 256), (8, 64, 100), (60, 0, 350)])
+def test_keys_that_are_infinitely_far(tokens, shared, tiles, pages, first, last):
+    """Scores of -inf count for nothing, whole blocks of them before any other score included; with none but those a row is zero.  One
+    of +inf or NaN makes a row NaN."""
+    rng = np.random.default_rng(last)
+    past = 350
+    cache = Cache(1, pages, 64, 1, DIM, 16, 0)
+    k, v = (keys_and_values(rng, (past + tokens, 1, DIM)) for _ in range(2))
+    k[first:last, 0, 0] = -np.inf
+    _write(cache, k, v)
+    q = rng.standard_normal((tokens, shared, DIM)).astype(np.float16)
+    q[..., 0] = np.abs(q[..., 0]) + np.float16(0.5)
+    q[-1, 0, 0], q[-1, 1, 0] = -1.0, 0.0
+    step = cache.step([tokens], [past])
+    plan = L.lutgemm_plan_attention(cache.c, step, shared)
+    assert plan[0] == tiles
+    print("case infinite", tokens, shared, pages, first, last, plan, flush=True)
+    y = _run(cache, step, q, None, shared, DIM ** -0.5, 0)
+    seen = np.r_[0:first, last:past + tokens]
+    odd = np.zeros((tokens, shared), bool)
+    odd[-1, :2] = True
+    np.testing.assert_array_equal(np.isnan(y), np.repeat(odd[..., None], DIM, 2))
+    ref, mass, reach = K.attention(q, k[seen], v[seen], past - (last - first), None, DIM ** -0.5)
+    _check(y[~odd], ref[~odd], mass[~odd], reach, DIM)
+    # none but those
+    mask = np.zeros(tokens, np.uint64)
+    k[:past, 0, 0] = -np.inf
+    _write(cache, k[:past], v[:past])
+    y = _run(cache, step, q, mask, shared, DIM ** -0.5, 0)
+    assert (y[~odd] == 0).all() and np.isnan(y[odd]).all()
