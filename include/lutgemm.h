@@ -471,7 +471,8 @@ int lutgemm_kv_read(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, 
    with the keys and values of head h / (q_heads / heads).  Token t of sequence s sees every position before past[s], and
    of the new ones position past[s] + j where bit j of mask[t] is set (a token that sees itself has its
    own bit set; bits beyond the sequence's tokens count for nothing).  mask NULL: each new token sees itself and those before it.  A
-   row that sees nothing, or nothing but scores of -inf, is zero.  Up to 64 new tokens a sequence; a longer prompt is taken in chunks.
+   row that sees nothing, or nothing but scores of -inf, is zero.  Up to 64 new tokens a sequence; a longer prompt is taken in
+   chunks.  Up to 65535 sequences, 2^14 query heads and tables of 2^30 positions (table_pages * page_tokens).
      q, y            fp16 rows of q_stride / y_stride, heads one after the other; 16-byte aligned, strides
                      multiples of 8.  y must not overlap q
      mask            uint64 [tokens] or NULL
@@ -491,7 +492,8 @@ size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lu
 
 /* HOST.  How lutgemm_attention splits such a call: out[0] tiles of 16 rows (token, query head) of a workgroup, out[1]
    workgroups along the rows of a key head, out[2] along the positions, out[3] positions of each
-   of these, out[4] wavefronts of a workgroup.                                            */
+   of these, out[4] wavefronts of a workgroup.  It refuses the sizes that the call refuses; the bytes of a workspace are 0 for
+   them.                                                                                  */
 int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,
                            int64_t most_positions, int* out);
 

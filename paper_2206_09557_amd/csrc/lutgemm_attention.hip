@@ -1182,20 +1182,17 @@ extern "C" int lutgemm_attention(const void* q, const uint64_t* mask, const lutg
   int rc = check_cache(cache);
   if (rc == LUTGEMM_OK) rc = check_step(step);
   if (rc != LUTGEMM_OK) return rc;
-  if (!q || !y || !workspace || q_heads < 1 || q_heads % cache->heads != 0 || most_positions < 0) return LUTGEMM_EINVAL;
+  if (!q || !y || !workspace) return LUTGEMM_EINVAL;
   if ((((uintptr_t)q | (uintptr_t)y | (uintptr_t)workspace) & 15) != 0 || ((uintptr_t)mask & 7) != 0) return LUTGEMM_EINVAL;
+  AttentionPlan plan;
+  rc = check_attention(cache, step, q_heads, most_positions, &plan);
+  if (rc != LUTGEMM_OK) return rc;
   const int64_t row = (int64_t)q_heads * cache->head_dim;
   if (q_stride < row || y_stride < row || q_stride % 8 != 0 || y_stride % 8 != 0) return LUTGEMM_EINVAL;
-  if (step->most_tokens > kMostTokens || q_heads > 1 << 14) return LUTGEMM_EUNSUPPORTED;
-  const int64_t held = (int64_t)step->table_pages * cache->page_tokens;
-  if (held > (int64_t)1 << 30) return LUTGEMM_EUNSUPPORTED;
-  if (most_positions == 0 || most_positions > held) most_positions = held;
   const int group = group_of(cache->head_dim, cache->bits, cache->group);
-  const AttentionPlan plan = plan_attention(cache->heads, cache->head_dim, cache->bits, group, q_heads, step->seqs, step->most_tokens, most_positions);
   if (workspace_bytes < 32768 + 4 * (size_t)attention_partial_floats(plan, cache->heads, cache->head_dim, q_heads, step->seqs, step->most_tokens))
     return LUTGEMM_EWORKSPACE;
   if (step->tokens == 0 || step->most_tokens == 0) return LUTGEMM_OK;
-  if ((int64_t)cache->heads * plan.row_blocks > 65535) return LUTGEMM_EUNSUPPORTED;
   Params p = {};
   p.q = static_cast<const _Float16*>(q);
   p.mask = mask;

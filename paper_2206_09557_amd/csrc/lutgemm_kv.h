@@ -13,6 +13,11 @@ namespace lutgemm_kv_detail {
 constexpr int kBlock = 32;        // positions of a block, channels of a unit
 constexpr int kMostSplits = 128;  // of the positions
 constexpr int kMostTokens = 64;   // new tokens of a sequence that attention takes: one bit each in a mask word
+constexpr int kMostSeqs = 65535;  // a grid's third side
+// Of attention: query heads (a grid's second side has heads * row_blocks of AttentionPlan, with 128 rows and more to a block where there are
+// several: 12288 at most), positions of a table (so that any two are less than 2^31 apart).
+constexpr int kMostQueryHeads = 1 << 14;
+constexpr int64_t kMostHeld = (int64_t)1 << 30;
 
 // Bytes of one block's keys (or values): codes, then scales.
 inline int code_bytes(int head_dim, int bits) { return kBlock * head_dim * bits / 8; }
@@ -46,7 +51,7 @@ inline int check_step(const lutgemm_kv_step* s) {
   if (!s || !s->first || !s->past || !s->table) return LUTGEMM_EINVAL;
   if ((((uintptr_t)s->first | (uintptr_t)s->past | (uintptr_t)s->table) & 3) != 0) return LUTGEMM_EINVAL;
   if (s->seqs < 1 || s->table_pages < 1 || s->tokens < 0 || s->most_tokens < 0) return LUTGEMM_EINVAL;
-  if (s->seqs > 65535) return LUTGEMM_EUNSUPPORTED;
+  if (s->seqs > kMostSeqs) return LUTGEMM_EUNSUPPORTED;
   return LUTGEMM_OK;
 }
 
@@ -75,6 +80,7 @@ struct AttentionPlan {
   int waves;        // wavefronts of a workgroup
 };
 AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q_heads, int seqs, int most_tokens, int64_t most_positions);
+int check_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, AttentionPlan* plan);
 // Floats of the partial results behind the workspace's counters (0: nothing is split).
 int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens);
 

@@ -65,26 +65,23 @@ int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim
   return (int64_t)seqs * heads * p.row_blocks * p.splits * rows * (head_dim + 2);
 }
 
-}  // namespace lutgemm_kv_detail
-
-using namespace lutgemm_kv_detail;
-
-namespace {
-
-// LUTGEMM_OK and the plan of a call's shape.
-int plan_of(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, AttentionPlan* plan) {
-  if (!cache || !step || step->seqs < 1 || step->table_pages < 1 || step->most_tokens < 0 || q_heads < 1 || most_positions < 0) return LUTGEMM_EINVAL;
+// What the sizes of a call must be, for the call itself and for what is asked about it before; the plan of one that is offered.
+int check_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, AttentionPlan* plan) {
+  if (!cache || !step || step->seqs < 1 || step->table_pages < 1 || step->tokens < 0 || step->most_tokens < 0 || q_heads < 1 || most_positions < 0) return LUTGEMM_EINVAL;
   const int rc = check_shape(cache->pages, cache->page_tokens, cache->heads, cache->head_dim, cache->bits, cache->group);
   if (rc != LUTGEMM_OK) return rc;
   if (q_heads % cache->heads != 0) return LUTGEMM_EINVAL;
-  if (step->seqs > 65535 || step->most_tokens > kMostTokens || q_heads > 1 << 14) return LUTGEMM_EUNSUPPORTED;
+  if (step->seqs > kMostSeqs || step->most_tokens > kMostTokens || q_heads > kMostQueryHeads) return LUTGEMM_EUNSUPPORTED;
   const int64_t held = (int64_t)step->table_pages * cache->page_tokens;
+  if (held > kMostHeld) return LUTGEMM_EUNSUPPORTED;
   if (most_positions == 0 || most_positions > held) most_positions = held;
   *plan = plan_attention(cache->heads, cache->head_dim, cache->bits, group_of(cache->head_dim, cache->bits, cache->group), q_heads, step->seqs, step->most_tokens, most_positions);
   return LUTGEMM_OK;
 }
 
-}  // namespace
+}  // namespace lutgemm_kv_detail
+
+using namespace lutgemm_kv_detail;
 
 extern "C" {
 
@@ -95,14 +92,14 @@ size_t lutgemm_kv_pool_bytes(int64_t pages, int page_tokens, int heads, int head
 
 size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions) {
   AttentionPlan p;
-  if (plan_of(cache, step, q_heads, most_positions, &p) != LUTGEMM_OK) return 0;
+  if (check_attention(cache, step, q_heads, most_positions, &p) != LUTGEMM_OK) return 0;
   return 32768 + 4 * (size_t)attention_partial_floats(p, cache->heads, cache->head_dim, q_heads, step->seqs, step->most_tokens);
 }
 
 int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, int* out) {
   AttentionPlan p;
   if (!out) return LUTGEMM_EINVAL;
-  const int rc = plan_of(cache, step, q_heads, most_positions, &p);
+  const int rc = check_attention(cache, step, q_heads, most_positions, &p);
   if (rc != LUTGEMM_OK) return rc;
   const int v[5] = {p.row_tiles, p.row_blocks, p.splits, p.chunk, p.waves};
   std::copy(v, v + 5, out);
