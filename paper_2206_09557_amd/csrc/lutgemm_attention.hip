@@ -542,7 +542,7 @@ __device__ __forceinline__ half8v finite_only(half8v v) {
 // A split's partial results: sums [partial_rows][dim], then a top and a total for each row.
 __device__ __forceinline__ float* partial_of(const Params& p, const Place& w, int split, int dim) {
   const int64_t unit = ((int64_t)w.seq * p.heads + w.head) * p.row_blocks + w.row_block;
-  return p.partial + (unit * p.splits + split) * p.partial_rows * (dim + 2);
+  return p.partial + (unit * p.splits + split) * split_floats(p.partial_rows, dim);
 }
 
 // The kernel's arguments once more, from memory: what only its end needs would else take up scalar registers through its loops.
@@ -609,8 +609,8 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
   }
   __syncthreads();
   float* mine = partial_of(p, w, blockIdx.x, kDim);
-  const int64_t split_floats = (int64_t)p.partial_rows * (kDim + 2);
-  const Buffer through = buffer_of(mine, split_floats);
+  const int64_t next = split_floats(p.partial_rows, kDim);                       // from a split's to the next one's
+  const Buffer through = buffer_of(mine, next);
 #pragma unroll 1
   for (int i = threadIdx.x; i < live_rows * kFours; i += kThreads) {              // a thread takes four channels
     const int row = i / kFours, d = i % kFours * 4;
@@ -635,7 +635,7 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
     const bool adds = *last != 0u;
     __syncthreads();
     if (!adds) return;
-    const Buffer all = buffer_of(partial_of(p, w, 0, kDim), p.splits * split_floats);
+    const Buffer all = buffer_of(partial_of(p, w, 0, kDim), p.splits * next);
     float2v* split_ends = reinterpret_cast<float2v*>(lds);        // [live_rows][active]: top and total, then factor and total
     float* row_total = lds + 2 * kRows * kMostSplits;             // [kRows]
     float* shares = row_total + kRows;                            // [kThreads][4]
@@ -650,13 +650,13 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
     auto load_ahead = [&](int i, int split) {
       const int at = min(i, items - 1) * 4;                       // row * kDim + d
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) ahead[k] = load4(all, min(split + k * sharers, w.active - 1) * (int)split_floats + at);
+      for (int k = 0; k < kAhead; ++k) ahead[k] = load4(all, min(split + k * sharers, w.active - 1) * (int)next + at);
     };
     load_ahead(place, share);
 #pragma unroll 1
     for (int i = threadIdx.x; i < live_rows * w.active; i += kThreads) {
       const int split = i / live_rows, row = i - split * live_rows;
-      split_ends[row * w.active + split] = load2(all, split * (int)split_floats + p.partial_rows * kDim + 2 * row);
+      split_ends[row * w.active + split] = load2(all, split * (int)next + p.partial_rows * kDim + 2 * row);
     }
     __syncthreads();
 #pragma unroll 1
@@ -719,7 +719,7 @@ __global__ __launch_bounds__(kJoinThreads, DIM == 64 ? 7 : 8) void lutgemm_atten
   w.head = blockIdx.y / p.row_blocks;
   w.row_block = blockIdx.y - w.head * p.row_blocks;
   const float* partial = partial_of(p, w, 0, DIM);
-  const int64_t next = (int64_t)p.partial_rows * (DIM + 2);
+  const int64_t next = split_floats(p.partial_rows, DIM);
   const bool held = set < kSets / sharers * sharers && row < p.partial_rows;       // (sets that make up no row are idle)
   const float* sums = partial + row * DIM + 4 * lane;
   float4v ahead[kAhead];

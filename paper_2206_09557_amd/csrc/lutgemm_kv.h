@@ -81,6 +81,8 @@ struct AttentionPlan {
 };
 AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q_heads, int seqs, int most_tokens, int64_t most_positions);
 int check_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads, int64_t most_positions, AttentionPlan* plan);
+// Floats of a split's partial results: sums, a top and a total for each row; the next split's begin on 16 bytes again.
+constexpr int64_t split_floats(int rows, int head_dim) { return ((int64_t)rows * (head_dim + 2) + 3) / 4 * 4; }
 // Floats of the partial results behind the workspace's counters (0: nothing is split).
 int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens);
 

@@ -62,7 +62,7 @@ AttentionPlan plan_attention(int heads, int head_dim, int bits, int group, int q
 int64_t attention_partial_floats(const AttentionPlan& p, int heads, int head_dim, int q_heads, int seqs, int most_tokens) {
   if (p.splits == 1) return 0;
   const int64_t rows = std::min<int64_t>(16 * p.row_tiles, (int64_t)std::min(most_tokens, kMostTokens) * (q_heads / heads));
-  return (int64_t)seqs * heads * p.row_blocks * p.splits * rows * (head_dim + 2);
+  return (int64_t)seqs * heads * p.row_blocks * p.splits * split_floats((int)rows, head_dim);
 }
 
 // What the sizes of a call must be, for the call itself and for what is asked about it before; the plan of one that is offered.

@@ -51,3 +51,15 @@ def test_any_sizes():
         assert called == (L.LUTGEMM_EWORKSPACE if asked is None else asked), sizes
         if plan:
             assert heads * plan[1] <= 65535 and plan[2] <= 128 and nbytes >= 32768, (sizes, plan)      # sides of a grid
+
+
+@pytest.mark.parametrize("most,shared,dim,rows", [(1, 1, 64, 1), (1, 3, 96, 3), (3, 5, 128, 15), (17, 1, 128, 17), (13, 3, 64, 39), (31, 1, 256, 31), (5, 5, 192, 25)])
+def test_partial_results_begin_on_16_bytes(most, shared, dim, rows):
+    """Of every split: `rows` sums of `dim` floats, which are moved 16 bytes at a time, and two floats a row."""
+    c = L.lutgemm_kv_cache(A, 4, 64, 2, dim, 8, 0)
+    s = L.lutgemm_kv_step(A, A, A, 1, 1 << 11, most, most)
+    plan = L.lutgemm_plan_attention(c, s, 2 * shared)
+    assert plan[1] == 1 and plan[2] > 1
+    nbytes = L.lutgemm_attention_workspace_bytes(c, s, 2 * shared) - 32768
+    each = nbytes // (2 * plan[2])
+    assert nbytes == each * 2 * plan[2] and each % 16 == 0 and 0 <= each - 4 * rows * (dim + 2) < 16
