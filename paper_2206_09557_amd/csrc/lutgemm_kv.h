@@ -39,6 +39,8 @@ inline int check_shape(int64_t pages, int page_tokens, int heads, int head_dim, 
   if (head_dim % g != 0) return LUTGEMM_EINVAL;
   if (g % kBlock != 0) return LUTGEMM_EUNSUPPORTED;
   if (pages > INT32_MAX || page_tokens > 1 << 20 || heads > 1 << 12) return LUTGEMM_EUNSUPPORTED;
+  int64_t bytes;                  // of the pool: an offset in it has to fit (a page alone is 2^42 bytes at most)
+  if (__builtin_mul_overflow(pages, (int64_t)heads * (page_tokens / kBlock) * block_bytes(head_dim, bits, g), &bytes)) return LUTGEMM_EUNSUPPORTED;
   return LUTGEMM_OK;
 }
 

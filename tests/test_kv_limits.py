@@ -63,3 +63,15 @@ def test_partial_results_begin_on_16_bytes(most, shared, dim, rows):
     nbytes = L.lutgemm_attention_workspace_bytes(c, s, 2 * shared) - 32768
     each = nbytes // (2 * plan[2])
     assert nbytes == each * 2 * plan[2] and each % 16 == 0 and 0 <= each - 4 * rows * (dim + 2) < 16
+
+
+def test_pools_beyond_any_offset():
+    """2^73 bytes: the product of the sizes leaves 64 bits, and none of its low bits is a size."""
+    for pages, page, heads, dim, bits in [((1 << 31) - 1, 1 << 20, 1 << 12, 256, 16), (1 << 22, 1 << 20, 1 << 12, 128, 16), ((1 << 31) - 1, 1 << 20, 4000, 192, 4)]:
+        assert L.lutgemm_kv_pool_bytes(pages, page, heads, dim, bits) == 0
+        c, s = L.lutgemm_kv_cache(A, pages, page, heads, dim, bits), L.lutgemm_kv_step(A, A, A, 1, 1, 1, 1)
+        row = heads * dim
+        assert _code(L.lutgemm_kv_write, A, A, None, c, s, row, row) == L.LUTGEMM_EUNSUPPORTED
+        assert _code(L.lutgemm_kv_read, c, s, A, A, row, row) == L.LUTGEMM_EUNSUPPORTED
+        assert _code(L.lutgemm_attention, A, None, c, s, A, heads, row, row, 1.0, 0, A, 1 << 40) == L.LUTGEMM_EUNSUPPORTED
+    assert L.lutgemm_kv_pool_bytes(1 << 20, 1 << 20, 1 << 12, 256, 16) == 1 << 62
