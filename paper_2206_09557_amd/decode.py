@@ -71,10 +71,14 @@ class AttentionHalf:
     def place(self, counts, depths=None, mask=None):
         """counts[s] tokens of sequence s come next; depths: of a tree's tokens below their sequence's last (0 at its roots), mask:
         which of their sequence's new tokens each sees, as bits.  Without them the tokens follow one another."""
-        if len(counts) != self.seqs or sum(counts) < 1 or sum(counts) > MOST_ROWS:
+        if len(counts) != self.seqs or min(counts) < 0 or sum(counts) < 1 or sum(counts) > MOST_ROWS:
             raise ValueError(f"a step has counts of {self.seqs} sequences and 1 to {MOST_ROWS} tokens")
         if any(n + c > self.longest for n, c in zip(self.lengths, counts)):
             raise ValueError(f"a sequence would be longer than {self.longest}")
+        if depths is not None and [len(d) for d in depths] != list(counts):
+            raise ValueError("a step has a depth for every token, by sequences")
+        if mask is not None and len(mask) != sum(counts):
+            raise ValueError("a step has a mask word for every token")
         self.counts = list(counts)
         self._set(self.first, np.concatenate([[0], np.cumsum(counts)]), np.int32)
         self._set(self.past, self.lengths, np.int32)
@@ -111,6 +115,8 @@ class AttentionHalf:
         if accepted is None:
             kept = self.counts
         else:
+            if len(accepted) != self.seqs or any(list(a) != sorted(set(a) & set(range(c))) for a, c in zip(accepted, self.counts)):
+                raise ValueError("of each sequence some of the step's tokens are kept, in ascending order")
             kept = [len(a) for a in accepted]
             if any(list(a) != list(range(len(a))) for a in accepted):
                 # the accepted tokens' keys and values, still in the product's rows, over the first of the drafted ones

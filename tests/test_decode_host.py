@@ -39,3 +39,28 @@ def test_no_step_needs_more_workspace_than_there_is(on_host, hidden, heads, kv_h
         for most in range(1, tokens + 1):
             step = half._step(tokens, most)
             assert 0 < L.lutgemm_attention_workspace_bytes(half.cache, step, heads, longest) <= half.ws_bytes, (tokens, most)
+
+
+@pytest.mark.parametrize("counts,depths,mask", [
+    ([1], None, None), ([2, -1], None, None), ([0, 0], None, None), ([20, 13], None, None), ([80, 1], None, None),
+    ([2, 1], [[0, 1]], None), ([2, 1], [[0, 1], [0, 1]], None), ([2, 1], [[0], [0, 1]], None), ([2, 1], None, [1, 3]), ([2, 1], None, [1, 3, 1, 1])])
+def test_steps_that_are_refused(on_host, counts, depths, mask):
+    half = _half(512, 8, 2, 64, 2, 80, 16)
+    with pytest.raises(ValueError):
+        half.place(counts, depths, mask)
+    half.place([2, 1], [[0, 0], [0]], [1, 2, 1])
+    assert half.step.tokens == 3 and half.mask[:3].tolist() == [1, 2, 1] and half.positions[:3].tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("accepted", [[[0]], [[0], [0], []], [[3], [0]], [[0], [2]], [[-1], []], [[1, 0], []], [[1, 1], []], [[0, 40], []]])
+def test_tokens_that_cannot_be_kept(on_host, monkeypatch, accepted):
+    """Rows that the step does not have are not read, another sequence's are not taken."""
+    written = []
+    monkeypatch.setattr(L.lutgemm, "lutgemm_kv_write", lambda *args: written.append(args))
+    half = _half(512, 8, 2, 64, 2, 80, 16)
+    half.place([3, 2])
+    with pytest.raises(ValueError):
+        half.keep(accepted)
+    assert half.lengths == [0, 0] and not written
+    half.keep([[1, 2], [0]])
+    assert half.lengths == [2, 1] and len(written) == 1 and half.rows[:3].tolist() == [1, 2, 3] and half.first.tolist() == [0, 2, 3]
