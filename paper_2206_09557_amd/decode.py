@@ -23,11 +23,14 @@ MOST_ROWS = 32      # vectors of one product
 class AttentionHalf:
     """One layer: packed weights (bits, alpha, z on the device), its cache, buffers for steps of up to 32 tokens.
 
+    Rotary positions: `turns` (lutgemm_rope_frequencies of rot_dim), on the first rot_dim channels of a head (0: all), neighbours or halves
+    paired, times `amplitude` (the one that goes with stretched frequencies).
+
     `place` says where the next step's tokens stand, `run` launches the step (and may be captured), `keep` advances the
     lengths by all of the step's tokens, or by those of a drafted tree that were accepted."""
 
     def __init__(self, qkv, out, hidden, heads, kv_heads, head_dim, seqs, longest, q=3, g=128, kv_bits=8, kv_group=0, page=64,
-                 turns=None):
+                 turns=None, rot_dim=0, neighbours=False, amplitude=1.0):
         import torch
         self.torch, self.weights, self.hidden, self.heads, self.kv_heads, self.dim = torch, (qkv, out), hidden, heads, kv_heads, head_dim
         self.q, self.g, self.seqs = q, g, seqs
@@ -38,7 +41,11 @@ class AttentionHalf:
         self.cache = L.lutgemm_kv_cache(self.pool, seqs * pages, page, kv_heads, head_dim, kv_bits, kv_group)
         self.table = torch.arange(seqs * pages, dtype=torch.int32, device="cuda").view(seqs, pages)
         self.longest = longest
-        turns = L.lutgemm_rope_frequencies(head_dim) if turns is None else turns
+        self.rot_dim, self.amplitude = rot_dim or head_dim, float(amplitude)
+        self.rope_flags = L.LUTGEMM_Y_F16 | (L.LUTGEMM_ROPE_NEIGHBOURS if neighbours else 0)
+        turns = L.lutgemm_rope_frequencies(self.rot_dim) if turns is None else turns
+        if len(turns) * 2 != self.rot_dim:
+            raise ValueError(f"{self.rot_dim} channels are turned by {self.rot_dim // 2} frequencies, not {len(turns)}")
         self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
         self.lengths = [0] * seqs
         self.past = torch.zeros(seqs, dtype=torch.int32, device="cuda")
@@ -102,8 +109,8 @@ class AttentionHalf:
         (m, n), (hidden, mixed) = self.shapes()
         queries = self.heads * self.dim
         self._product(self.weights[0], x, self.qkv, m, n, tokens)
-        L.lutgemm_rope(self.qkv, self.qkv, self.positions, self.turns, tokens, self.heads + self.kv_heads, self.dim, self.dim, self.row,
-                       self.row, 1.0, L.LUTGEMM_Y_F16, stream)
+        L.lutgemm_rope(self.qkv, self.qkv, self.positions, self.turns, tokens, self.heads + self.kv_heads, self.dim, self.rot_dim,
+                       self.row, self.row, self.amplitude, self.rope_flags, stream)
         keys, values = self.qkv[:, queries:], self.qkv[:, queries + self.kv_heads * self.dim:]
         L.lutgemm_kv_write(keys, values, None, self.cache, self.step, self.row, self.row, stream)
         L.lutgemm_attention(self.qkv, self.mask if self.masked else None, self.cache, self.step, self.mixed, self.heads, self.row, mixed,

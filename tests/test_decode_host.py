@@ -64,3 +64,11 @@ def test_tokens_that_cannot_be_kept(on_host, monkeypatch, accepted):
     assert half.lengths == [0, 0] and not written
     half.keep([[1, 2], [0]])
     assert half.lengths == [2, 1] and len(written) == 1 and half.rows[:3].tolist() == [1, 2, 3] and half.first.tolist() == [0, 2, 3]
+
+
+@pytest.mark.parametrize("turned,rot_dim", [(64, 32), (32, 0), (32, 64)])
+def test_frequencies_of_other_channels_are_refused(on_host, turned, rot_dim):
+    with pytest.raises(ValueError):
+        _half(512, 8, 2, 64, 2, 80, 16, turns=L.lutgemm_rope_frequencies(turned), rot_dim=rot_dim)
+    half = _half(512, 8, 2, 64, 2, 80, 16, turns=L.lutgemm_rope_frequencies(turned), rot_dim=turned)
+    assert len(half.turns) == turned // 2
