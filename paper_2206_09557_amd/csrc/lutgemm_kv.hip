@@ -32,7 +32,6 @@ struct RopeParams {
   int tokens, heads, head_dim, rot_dim;
   int pair_runs;       // runs of kRun pairs in rot_dim
   int heads_a_thread;
-  int whole;           // nothing is left to copy: y is x
   float amplitude;
   float sign;          // of the angle
 };
@@ -173,7 +172,7 @@ struct KvParams {
   int64_t k_stride, v_stride;
   int64_t pages;
   int block_bytes, value_offset;       // of a block; of its value half
-  int tokens, seqs, table_pages, page_blocks, heads;
+  int tokens, table_pages, page_blocks, heads;
 };
 
 // Where the tokens of a sequence are, checked against what the host said.
@@ -693,7 +692,6 @@ int move_rows(bool write, const void* k, const void* v, const int32_t* rows, con
   if ((!k && !v) || !aligned16(k) || !aligned16(v) || ((uintptr_t)rows & 3) != 0) return LUTGEMM_EINVAL;
   const int64_t row = (int64_t)cache->heads * cache->head_dim;
   if ((k && (k_stride < row || k_stride % 8 != 0)) || (v && (v_stride < row || v_stride % 8 != 0))) return LUTGEMM_EINVAL;
-  if (cache->heads > 65535) return LUTGEMM_EUNSUPPORTED;
   if (step->tokens == 0 || step->most_tokens == 0) return LUTGEMM_OK;
   const int group = group_of(cache->head_dim, cache->bits, cache->group);
   KvParams p = {};
@@ -710,7 +708,6 @@ int move_rows(bool write, const void* k, const void* v, const int32_t* rows, con
   p.block_bytes = block_bytes(cache->head_dim, cache->bits, group);
   p.value_offset = p.block_bytes / 2;
   p.tokens = step->tokens;
-  p.seqs = step->seqs;
   p.table_pages = step->table_pages;
   p.page_blocks = cache->page_tokens / kBlock;
   p.heads = cache->heads;
