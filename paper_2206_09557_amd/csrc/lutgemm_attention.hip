@@ -76,7 +76,7 @@ constexpr int kJoinThreads = 256, kJoinAhead = 4;      // splits that a thread a
 constexpr float kLift = 7.0f, kSlack = 15.0f;
 constexpr float kNothing = -3.402823466e38f;      // what weights are relative to before a row has seen a score: finite, so that one of -inf weighs nothing
 // Scores that fp32 holds without fractions.  The weights' multiply-add brings back what rounding took off a maximum like that: from 2^28 on more
-// than fp16's exponents hold.  So these are rounded before the maximum, which is rounded too, is taken off.
+// than fp16's exponents hold.  So where a row has one the tile's are rounded before the maximum, which is rounded too, is taken off.
 constexpr float kFar = 16777216.0f;
 
 // Partial results that cross workgroups inside one kernel: stores that are written through to the device's point of coherence and loads
@@ -379,25 +379,20 @@ __device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT
   float most = score[0][0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) most = fmaxf(most, score[i >> 2][i & 3]);
-  float factor = scale, base = s.top[t];
-  if (__any(__builtin_fmaf(most, scale, -base) > kSlack)) {             // (as the weights are worked out: none passes 2^kSlack)
+  float factor = scale;
+  if (__any(__builtin_fmaf(most, scale, -s.top[t]) > kSlack)) {         // (as the weights are worked out: none passes 2^kSlack)
     most = max_of_column(most);
-    const bool own = __builtin_fmaf(most, scale, -base) > kSlack;       // (a row's own need: others do not change its result)
-    const float raised = own ? rounded_product(most, scale) - kLift : base;
-    const float shrink = raised == base ? 1.0f : __builtin_amdgcn_exp2f(base - raised);
-    s.top[t] = base = raised;
+    const bool own = __builtin_fmaf(most, scale, -s.top[t]) > kSlack;   // (a row's own need: others do not change its result)
+    const float raised = own ? rounded_product(most, scale) - kLift : s.top[t];
+    const float shrink = raised == s.top[t] ? 1.0f : __builtin_amdgcn_exp2f(s.top[t] - raised);
+    s.top[t] = raised;
     s.total[t] *= shrink;
 #pragma unroll
     for (int u = 0; u < 2 * DC; ++u) s.out[t][u] *= shrink;
-    const bool far = own && fabsf(raised) >= kFar;
-    if (__any(far)) {
+    if (__builtin_expect(__any(own && fabsf(raised) >= kFar), 0)) {     // (but for this rounding of the tile's scores, within their own)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = score[i >> 2][i & 3];
-        score[i >> 2][i & 3] = far ? rounded_product(x, scale) - raised : __builtin_fmaf(x, scale, -raised);
-      }
+      for (int i = 0; i < 8; ++i) score[i >> 2][i & 3] = rounded_product(score[i >> 2][i & 3], scale);
       factor = 1.0f;
-      base = 0.0f;
     }
   }
   half2v w[4];
@@ -405,7 +400,7 @@ __device__ __forceinline__ half8v block_weights(float4v (&score)[2], Sums<DC, RT
   for (int i = 0; i < 4; ++i) {
     float2v e;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], factor, -base));
+    for (int k = 0; k < 2; ++k) e[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i >> 1][(2 * i + k) & 3], factor, -s.top[t]));
     w[i] = __builtin_convertvector(e, half2v);
   }
   half8v weight = join(w[0], w[1], w[2], w[3]);
