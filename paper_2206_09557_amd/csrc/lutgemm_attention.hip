@@ -9,12 +9,15 @@
 // between lanes but the maximum's, and its weights are the second product's operand as they stand: the cache's layout
 // deals the positions to the lanes so that they are (place 8 a + 4 j + b is row 4 a + b of the j-th tile of S^T).
 // What the weights are relative to is only raised where a score passes it by 2^15, which is seldom;
-// the sum of the weights is one more product, of a tile of ones, so it adds what the other products add.
+// the sum of the weights is one more product, of a tile of ones, so it adds what the other products add.  Weights are fp16 there, because the
+// values are and matrix instructions take operands of one type; twice as many of them (a weight in two parts) would be what more bits cost.
+// The rounding is 0.25 to 0.3 x 10^-3 of a result's norm together with the result's own, which alone is 0.21 x 10^-3.
 //
 // At the end the wavefronts' sums meet in LDS, and where the positions are split the splits' sums meet in memory: of up to 16 rows the
 // last workgroup to arrive adds them (the hand-off is the one of finish_row_range in lutgemm_device.hip: write-through
-// stores, a wait for them, a barrier, a relaxed counter), of more rows a second small kernel.  Both add in the order of
-// the splits.  131072 positions of one sequence in 32 splits: meeting in LDS, handing off and adding take 8 us of 40.
+// stores, a wait for them, a barrier, a relaxed counter), of more rows a second small kernel.  Both
+// add in an order that the numbers of rows and splits decide (every 2nd, 4th, ... split by itself, then those sums), not the one in which
+// workgroups arrive.  131072 positions of one sequence in 32 splits: meeting in LDS, handing off and adding take 8 us of 40.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -697,7 +700,7 @@ __device__ __forceinline__ void end_workgroup(const Params& p, const Place& w, f
   }
 }
 
-// The splits' sums meet, in their order.  DIM / 4 lanes take a row, four channels each; `sharers` such sets share a row's splits where
+// The splits' sums meet.  DIM / 4 lanes take a row, four channels each; `sharers` such sets share a row's splits, every sharers-th each, where
 // there are many.  blockIdx as in the kernels before, .x counting rows.  Nothing here is work: what it takes is
 // a trip to memory, so all of it is asked for at once, before the sequence's length says how many splits there are, by as many wavefronts as
 // there is room for (16384 rows of 128 channels in 4 splits: 10 us; with eight splits a thread in flight, two wavefronts a SIMD, 19).
@@ -825,7 +828,7 @@ __device__ __forceinline__ Memory block_address(const Blocks& b, int page, int i
 // Few rows: every wavefront takes all of them, and blocks of its own, from memory straight into registers.  Two blocks are on
 // their way while one is worked on: a set's keys are asked for when the set's last ones have met the queries, its values
 // when those have been added.  Bound by the stream of codes where it is long (16 sequences of 64 heads, up to 4000 positions at 8 bits:
-// 654 MB in 113 us, 5.8 TB/s where a read-only kernel has 6.9), else by what begins and ends it: the chain lengths, page, codes,
+// 654 MB in 112 us, 5.8 TB/s where a read-only kernel has 6.9), else by what begins and ends it: the chain lengths, page, codes,
 // and the sums (331 positions of 40 heads at 16 bits 6.2 us, of which an empty kernel takes 2).
 // BITS of a code, DC units of 32 channels to a head, GU of them to a scale, RT tiles of 16 rows.
 template <int BITS, int DC, int GU, int RT, int WAVES>

@@ -1,5 +1,5 @@
 // Rotary positions, and the key/value cache as it is written and read back: include/lutgemm.h has the formulas and the
-// layout.  All three move data, so what bounds them is HBM (the write's 15 vector instructions a value come near it), and for a few
+// layout.  All three move data, so what bounds them is HBM (the write's 14 vector instructions a value come near it), and for a few
 // tokens the launch and two trips to memory, one after the other.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -98,7 +98,7 @@ __device__ __forceinline__ void store_run(T* p, const Run<T, N>& r) {
 // A thread owns a run of PAIRS pairs (threadIdx.x) of one token for some heads, so that the angles, which no table holds, are worked
 // out once for them: 64-bit position * frequency, one sine and cosine.  Runs behind the pairs' copy
 // what is not turned, 2 PAIRS channels each.  PAST: more is written than the caches hold till it is read, so it goes past them (75 MB
-// read and as many written 25.6 us, 5.9 TB/s, against 31.9; small outputs stay, for the next kernel).
+// read and as many written 24.6 to 26.5 us, 5.7 to 6.1 TB/s, against 31.9; small outputs stay, for the next kernel).
 template <typename T, int PAIRS, bool NEIGHBOURS, bool PAST>
 __global__ __launch_bounds__(256) void lutgemm_rope_kernel(RopeParams p) {
   const int token = blockIdx.x * blockDim.z + threadIdx.z;
@@ -304,8 +304,8 @@ constexpr int kKvThreads = 128;          // two wavefronts: keys and values
 // Writes the block of 32 positions that blockIdx.x counts from the one with the sequence's first new position, for one
 // head.  Values are transposed on the way, through LDS; whole units leave together, 16 bytes a lane.  Of a block that holds others'
 // positions too only the live places' codes are stored, to the byte.
-// 4096 tokens of 64 heads of 128 channels, rows that are parts of a product's: 4 bits in groups of 32, 176 MB, 41 us, 4.3 TB/s (a copy
-// reaches 4.7), the vector units four fifths busy; one token of each of 16 sequences 5 us.
+// 4096 tokens of 64 heads of 128 channels, rows that are parts of a product's: 4 bits in groups of 32, 176 MB, 41 us, 4.3 TB/s
+// (a copy of 75 MB that goes past the caches: 6.3), the vector units three quarters busy; one token of each of 16 sequences 6 us.
 template <int BITS, int DC, int GU>
 __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p) {
   constexpr int kCode = kBlock * DC * 4 * BITS;
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(kKvThreads) void lutgemm_kv_write_kernel(KvParams p
   char* base = base_of(p, span, value);
   if (!base) return;
   // The groups' statistics, run j of group k in ends[2 k + j], which the four lanes of a row then share out: each works out the scales of every
-  // fourth, stores them, and gives them to the others (all of it by every lane took 4 of the write's 15 instructions a value at groups of 32).
+  // fourth, stores them, and gives them to the others (all of it by every lane is 15.3 vector instructions a value where this is 13.6, 4 bits in groups of 32).
   constexpr int kGroups = BITS == 16 ? 0 : 2 * (DC / GU), kMine = (kGroups + 3) / 4;
   Group mine[kMine > 0 ? kMine : 1];
   if constexpr (BITS != 16) {
