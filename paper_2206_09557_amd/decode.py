@@ -122,10 +122,11 @@ class AttentionHalf:
         if accepted is None:
             kept = self.counts
         else:
-            if len(accepted) != self.seqs or any(list(a) != sorted(set(a) & set(range(c))) for a, c in zip(accepted, self.counts)):
+            accepted = [[int(t) for t in a] for a in accepted]
+            if len(accepted) != self.seqs or any(a != sorted(set(a) & set(range(c))) for a, c in zip(accepted, self.counts)):
                 raise ValueError("of each sequence some of the step's tokens are kept, in ascending order")
             kept = [len(a) for a in accepted]
-            if any(list(a) != list(range(len(a))) for a in accepted):
+            if any(a != list(range(len(a))) for a in accepted):
                 # the accepted tokens' keys and values, still in the product's rows, over the first of the drafted ones
                 begins = np.concatenate([[0], np.cumsum(self.counts)])
                 rows = np.concatenate([np.asarray(a, dtype=np.int64) + b for a, b in zip(accepted, begins)])

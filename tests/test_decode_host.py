@@ -72,3 +72,14 @@ def test_frequencies_of_other_channels_are_refused(on_host, turned, rot_dim):
         _half(512, 8, 2, 64, 2, 80, 16, turns=L.lutgemm_rope_frequencies(turned), rot_dim=rot_dim)
     half = _half(512, 8, 2, 64, 2, 80, 16, turns=L.lutgemm_rope_frequencies(turned), rot_dim=turned)
     assert len(half.turns) == turned // 2
+
+
+def test_kept_tokens_in_any_container(on_host, monkeypatch):
+    import numpy as np
+    import torch
+    monkeypatch.setattr(L.lutgemm, "lutgemm_kv_write", lambda *args: None)
+    for accepted in ([np.array([1, 2]), np.array([0])], (torch.tensor([1, 2]), torch.tensor([0])), ((1, 2), range(1))):
+        half = _half(512, 8, 2, 64, 2, 80, 16)
+        half.place(np.array([3, 2]))
+        half.keep(accepted)
+        assert half.lengths == [2, 1] and half.rows[:3].tolist() == [1, 2, 3]
