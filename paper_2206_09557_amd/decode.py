@@ -106,6 +106,9 @@ class AttentionHalf:
     def run(self, x, y):
         """x, y: fp16 [tokens][hidden], contiguous.  Five calls on the current stream; nothing is allocated."""
         tokens, stream = self.step.tokens, self._stream()
+        for rows in (x, y):
+            if rows.shape != (tokens, self.hidden) or rows.dtype != self.torch.float16 or not rows.is_contiguous():
+                raise ValueError(f"a step of {tokens} tokens takes and gives contiguous fp16 rows [{tokens}][{self.hidden}]")
         (m, n), (hidden, mixed) = self.shapes()
         queries = self.heads * self.dim
         self._product(self.weights[0], x, self.qkv, m, n, tokens)

@@ -83,3 +83,17 @@ def test_kept_tokens_in_any_container(on_host, monkeypatch):
         half.place(np.array([3, 2]))
         half.keep(accepted)
         assert half.lengths == [2, 1] and half.rows[:3].tolist() == [1, 2, 3]
+
+
+def test_rows_that_a_step_cannot_take(on_host, monkeypatch):
+    """Too few, too many, of another type, not one after the other: refused before anything is launched."""
+    import torch
+    half = _half(512, 8, 2, 64, 2, 80, 16)
+    monkeypatch.setattr(half, "_product", lambda *args: pytest.fail("launched"))
+    half.place([2, 1])
+    good = torch.empty(3, 512, dtype=torch.float16)
+    for bad in (good[:2], good[:, :256], good.float(), torch.empty(512, 3, dtype=torch.float16).t(), torch.empty(3, 1024, dtype=torch.float16)[:, ::2],
+                torch.empty(1, 3, 512, dtype=torch.float16)):
+        for x, y in ((bad, good), (good, bad)):
+            with pytest.raises(ValueError):
+                half.run(x, y)
