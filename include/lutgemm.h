@@ -497,6 +497,97 @@ size_t lutgemm_attention_workspace_bytes(const lutgemm_kv_cache* cache, const lu
 int lutgemm_plan_attention(const lutgemm_kv_cache* cache, const lutgemm_kv_step* step, int q_heads,
                            int64_t most_positions, int* out);
 
+/* =======================================================================================
+ * What surrounds the products and attention of a serving step: where its tokens stand, the norm in front of
+ * a product, low-rank adapters beside it.
+ * ======================================================================================= */
+
+/* Who has which pages of a cache, in DEVICE memory, kept by the three calls below.  `table` is a step's (lutgemm_kv_step); entries
+   beyond a sequence's pages are -1. */
+typedef struct lutgemm_kv_pages {
+  int32_t* free;     /* [pages]: the first *count are the pages that nobody has, the next one to be taken last */
+  int32_t* count;    /* [1] */
+  int32_t* owned;    /* [seqs]: sequence s has the pages table[s][0 .. owned[s] - 1] */
+  int32_t* table;    /* [seqs][table_pages] */
+  int64_t pages;     /* of the pool */
+  int page_tokens, seqs, table_pages;
+} lutgemm_kv_pages;
+
+/* DEVICE.  Nobody has a page; page 0 is taken first. */
+int lutgemm_kv_pages_init(const lutgemm_kv_pages* pages, void* hip_stream);
+
+/* DEVICE.  Places a step's tokens: fresh[s] of sequence s at positions past[s], past[s] + 1, ... (both int32 [seqs]), with
+   pages for all of them.  Sequences are served in order.  One with fresh[s] <= 0 takes no part; nor does one whose
+   past[s] is negative, that brings more than most_tokens or whose positions the table does not hold.  The first one for which the
+   `tokens` rows or the free pages that are left do not suffice waits, and all behind it do: they take no part, and keep
+   what they have.  (first[s + 1] == first[s] tells.)
+     first      int32 [seqs + 1]: rows first[s] .. first[s + 1] - 1 are sequence s's
+     positions  int32 [tokens]: of every row (lutgemm_rope); 0 behind the last sequence's.  May be NULL, as the next two
+     owner      int32 [tokens]: the row's sequence (lutgemm_adapt); -1 behind the last
+     slots      int64 [tokens]: page * page_tokens + place in the page of the row's position; -1 behind the last
+   past, fresh, first and the pages' table make a lutgemm_kv_step of `tokens` rows: its sizes are the host's, so a
+   captured graph places, writes and attends whatever lengths it finds.  past is not advanced.
+   Up to 65535 sequences and tables of 2^30 positions.                                    */
+int lutgemm_kv_place(const lutgemm_kv_pages* pages, const int32_t* past, const int32_t* fresh, int tokens, int most_tokens,
+                     int32_t* first, int32_t* positions, int32_t* owner, int64_t* slots, void* hip_stream);
+
+/* DEVICE.  Gives back what lengths[s] positions (int32 [seqs]) do not need of sequence s's pages: after drafted tokens were refused, or
+   all of them (0) at its end.  A negative length leaves a sequence as it is.  What one call of lutgemm_kv_place took comes back in the
+   order in which it was taken.                                                           */
+int lutgemm_kv_trim(const lutgemm_kv_pages* pages, const int32_t* lengths, void* hip_stream);
+
+/* `flags` of lutgemm_rms_norm, beside LUTGEMM_Y_F16 / LUTGEMM_Y_F32, which name the type of x: what a product gives. */
+enum { LUTGEMM_NORM_STREAM_F32 = 8 /* residual and sum are fp32, else fp16 */ };
+
+/* DEVICE.  The residual's addition and a root-mean-square norm, for every token t and channel c < n:
+     s = x[t][c] + residual[t][c],   sum[t][c] = s,   y[t][c] = s * weight[c] / sqrt(mean over c of s^2 + eps)
+   in fp32 from the sum before its rounding (squares are added in 64 bits), one rounding to fp16.  With scales not NULL y is 8 bits,
+   by the rule of the cache's but with an fp32 scale: for every `group` channels (a multiple of 32 that divides n; 0: the whole row, whatever n)
+     scales[t][g] = max|y| / 127,    y = rint(y / scale) in -127..127 (int8; the quotient within 2^-23 of itself)
+   A group with an infinity or a NaN has a NaN for its scale, one whose values are all below 2^-100 zero; codes are 0 in both.
+     residual   NULL: nothing is added                sum      NULL: not kept
+     weight     fp16 [n], NULL: ones                  scales   fp32 [tokens][n / group], without gaps
+   Row t of x begins at t * x_stride, of residual and sum at t * stream_stride, of y at t * y_stride; strides are at least n, up to 2^28.
+   sum may be residual, or x where the types agree; y may be x or residual where types and strides do.  Else outputs overlap neither
+   inputs nor one another (LUTGEMM_EINVAL; parts of the same rows side by side are apart).  n up to 32768, tokens up to 2^21, eps > 0.
+   Any alignment that the types have; rows of 16-byte multiples are faster.  A row with an infinity or a NaN is none of the others'
+   business.  Bitwise reproducible.                                                       */
+int lutgemm_rms_norm(const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales, int tokens, int n,
+                     int group, int64_t x_stride, int64_t stream_stride, int64_t y_stride, float eps, unsigned flags,
+                     void* hip_stream);
+
+/* Low-rank adapters beside an m x n product: A_a [r][n] and B_a [m][r], r = ranks[a], for a = 0 .. count - 1, in stores of one
+   rank for all (a multiple of 8, up to 256); what the stores hold beyond an adapter's rank counts for nothing.     */
+typedef struct lutgemm_adapters {
+  const void* down;       /* DEVICE, fp16 [count][rank][n], 16-byte aligned: A */
+  const void* up;         /* DEVICE, fp16 [count][m][rank], 16-byte aligned: B */
+  const int32_t* ranks;   /* DEVICE [count] (0 .. rank), or NULL: all of them `rank` */
+  const float* scales;    /* DEVICE [count], or NULL: all of them 1 */
+  int64_t m, n;           /* n a multiple of 8; both up to 2^20 */
+  int count, rank;        /* up to 1024 and 256 */
+} lutgemm_adapters;
+
+/* DEVICE.  y[t] = base[t] + scales[a] * B_a (A_a x[t]) for every token t, a its adapter:
+     of, owner    owner NULL: of is int32 [tokens], the adapter of each.  Else of is int32 [seqs], the adapter of each sequence, and
+                  owner int32 [tokens], the sequence of each token (lutgemm_kv_place).  An adapter outside 0..count-1 or a sequence outside
+                  0..seqs-1 is none: y[t] = base[t]
+     x            fp16 rows of x_stride: the product's input; 16-byte aligned, stride a multiple of 8
+     base, y      fp16 or fp32 (LUTGEMM_Y_F16 / LUTGEMM_Y_F32) rows of base_stride and y_stride: the product's output.  y may be base
+                  (with the same stride), else must not overlap it.  Any alignment that the type has; 16-byte aligned rows are faster
+     workspace    lutgemm_adapt_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any other and shared with
+                  products on the same stream if large enough
+   Sums are fp32, and A_a x[t] is kept to 22 bits of its largest element.  An adapter's weights are read once for up to 16 of its tokens (32 or 64 where the
+   tokens are many).  Tokens with adapters of their own do not see those of others, nor one another's infinities and NaNs (which may
+   be NaN where the exact result is an infinity).  Up to 65536 tokens.  Bitwise reproducible.  */
+int lutgemm_adapt(const void* x, const void* base, const lutgemm_adapters* adapters, const int32_t* of, const int32_t* owner,
+                  void* y, int tokens, int seqs, int64_t x_stride, int64_t base_stride, int64_t y_stride, unsigned flags,
+                  void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t lutgemm_adapt_workspace_bytes(const lutgemm_adapters* adapters, int tokens);
+
+/* HOST.  How lutgemm_adapt splits such a call: out[0] tokens of a tile (of one adapter), out[1] tiles at most, out[2] parts of the n
+   columns, out[3] columns of each, out[4] rows of m of a workgroup.  It refuses the sizes that the call refuses.  */
+int lutgemm_plan_adapt(const lutgemm_adapters* adapters, int tokens, int* out);
+
 /* Human-readable name of an error code (static storage).                                */
 const char* lutgemm_strerror(int code);
 

@@ -14,9 +14,10 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "liblutgemm.so")
-HOST_SOURCES = ("lutgemm_host.cpp", "lutgemm_kv_host.cpp")
+HOST_SOURCES = ("lutgemm_host.cpp", "lutgemm_kv_host.cpp", "lutgemm_step_host.cpp")
 # device sources and the kernel families of each (LUT_PART = 0, 1, ...)
-DEVICE_SOURCES = {"lutgemm_device.hip": 20, "lutgemm_kv.hip": 1, "lutgemm_attention.hip": 15}
+DEVICE_SOURCES = {"lutgemm_device.hip": 20, "lutgemm_kv.hip": 1, "lutgemm_attention.hip": 15, "lutgemm_place.hip": 1, "lutgemm_norm.hip": 4,
+                  "lutgemm_adapt.hip": 1}
 BINDING = os.path.join(PKG, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))   # of this Python alone
 BINDING_SOURCE = os.path.join(PKG, "csrc", "lutgemm_binding.cpp")
 

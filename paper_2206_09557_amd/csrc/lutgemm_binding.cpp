@@ -27,10 +27,18 @@ typedef int (*ReadFn)(const void*, const void*, void*, void*, int64_t, int64_t, 
 typedef int (*AttentionFn)(const void*, const void*, const void*, const void*, void*, int, int64_t, int64_t, float, int64_t, void*, size_t,
                            void*);
 
-// Products of layers, then the attention half of a step; either set can be loaded without the other.
-enum Which { kGemv, kGemm, kMfma, kDequant, kStatic, kGroup, kProducts, kRope = kProducts, kKvWrite, kKvRead, kAttention, kCount };
+typedef int (*PlaceFn)(const void*, const void*, const void*, int, int, void*, void*, void*, void*, void*);
+typedef int (*TrimFn)(const void*, const void*, void*);
+typedef int (*NormFn)(const void*, const void*, const void*, void*, void*, void*, int, int, int, int64_t, int64_t, int64_t, float, unsigned,
+                      void*);
+typedef int (*AdaptFn)(const void*, const void*, const void*, const void*, const void*, void*, int, int, int64_t, int64_t, int64_t, unsigned,
+                       void*, size_t, void*);
+
+// Products of layers, the attention half of a step, what surrounds both; each set can be loaded without the others.
+enum Which { kGemv, kGemm, kMfma, kDequant, kStatic, kGroup, kProducts, kRope = kProducts, kKvWrite, kKvRead, kAttention, kPlace, kTrim, kNorm, kAdapt, kCount };
 const char* const kNames[kCount] = {"lutgemm_gemv", "lutgemm_gemm", "lutgemm_gemm_mfma", "lutgemm_gemm_dequant_mfma", "lutgemm_gemv_static",
-                                    "lutgemm_gemv_group", "lutgemm_rope", "lutgemm_kv_write", "lutgemm_kv_read", "lutgemm_attention"};
+                                    "lutgemm_gemv_group", "lutgemm_rope", "lutgemm_kv_write", "lutgemm_kv_read", "lutgemm_attention", "lutgemm_kv_place",
+                                    "lutgemm_kv_trim", "lutgemm_rms_norm", "lutgemm_adapt"};
 
 void* g_function[kCount];        // of the loaded library, null until then
 PyObject* g_ctypes[kCount];      // lutgemm.py's functions
@@ -247,11 +255,66 @@ PyObject* attention(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) 
   return result(w, code);
 }
 
+// Arguments in the order of `kinds`: p an address, i an int, l an int64, f a float, u flags, z a number of bytes; then stream=0.
+struct Parsed {
+  void* p[8];
+  int i[3];
+  int64_t l[3], flags, bytes;
+  float f;
+  void* stream;
+};
+bool parse(const char* kinds, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames, Parsed* out) {
+  if (kwnames && PyTuple_GET_SIZE(kwnames) != 0) return false;
+  int p = 0, i = 0, l = 0;
+  Py_ssize_t at = 0;
+  for (; kinds[at]; ++at) {
+    if (at >= nargs) return false;
+    PyObject* o = args[at];
+    bool ok = true;
+    switch (kinds[at]) {
+      case 'p': ok = address(o, &out->p[p++]); break;
+      case 'i': ok = c_int(o, &out->i[i++]); break;
+      case 'l': ok = integer(o, INT64_MIN, INT64_MAX, &out->l[l++]); break;
+      case 'f': ok = real(o, &out->f); break;
+      case 'u': ok = integer(o, 0, UINT_MAX, &out->flags); break;
+      default: ok = integer(o, 0, INT64_MAX, &out->bytes); break;
+    }
+    if (!ok) return false;
+  }
+  out->stream = nullptr;
+  if (nargs == at) return true;
+  return nargs == at + 1 && PyLong_CheckExact(args[at]) && address(args[at], &out->stream);
+}
+
+// pages, past, fresh, tokens, most_tokens, first, positions, owner, slots; pages, lengths; x, residual, weight, sum, y, scales, tokens, n, group,
+// x_stride, stream_stride, y_stride, eps, flags; x, base, adapters, of, owner, y, tokens, seqs, x_stride, base_stride, y_stride, flags,
+// workspace, workspace_bytes; each with stream=0
+PyObject* step_call(Which w, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+  static const char* const kKinds[] = {"pppiipppp", "pp", "ppppppiiilllfu", "ppppppiilllupz"};
+  Parsed a;
+  if (!g_function[w] || !parse(kKinds[w - kPlace], args, nargs, kwnames, &a)) return by_ctypes(w, args, nargs, kwnames);
+  int code;
+  Py_BEGIN_ALLOW_THREADS
+  if (w == kPlace)
+    code = reinterpret_cast<PlaceFn>(g_function[w])(a.p[0], a.p[1], a.p[2], a.i[0], a.i[1], a.p[3], a.p[4], a.p[5], a.p[6], a.stream);
+  else if (w == kTrim)
+    code = reinterpret_cast<TrimFn>(g_function[w])(a.p[0], a.p[1], a.stream);
+  else if (w == kNorm)
+    code = reinterpret_cast<NormFn>(g_function[w])(a.p[0], a.p[1], a.p[2], a.p[3], a.p[4], a.p[5], a.i[0], a.i[1], a.i[2], a.l[0], a.l[1], a.l[2],
+                                                   a.f, (unsigned)a.flags, a.stream);
+  else
+    code = reinterpret_cast<AdaptFn>(g_function[w])(a.p[0], a.p[1], a.p[2], a.p[3], a.p[4], a.p[5], a.i[0], a.i[1], a.l[0], a.l[1], a.l[2],
+                                                    (unsigned)a.flags, a.p[6], (size_t)a.bytes, a.stream);
+  Py_END_ALLOW_THREADS
+  return result(w, code);
+}
+
 template <Which W>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
   if (W == kRope) return rope(args, nargs, kwnames);
   if (W == kKvWrite || W == kKvRead) return kv_rows(W, args, nargs, kwnames);
   if (W == kAttention) return attention(args, nargs, kwnames);
+  if (W >= kPlace) return step_call(W, args, nargs, kwnames);
   return W == kGroup ? group(args, nargs, kwnames) : one_layer(W, args, nargs, kwnames);
 }
 
@@ -304,6 +367,10 @@ PyMethodDef g_methods[] = {
     ENTRY("lutgemm_kv_write", kKvWrite, "k, v, rows, cache, step, k_stride, v_stride, stream=0"),
     ENTRY("lutgemm_kv_read", kKvRead, "cache, step, k, v, k_stride, v_stride, stream=0"),
     ENTRY("lutgemm_attention", kAttention, "q, mask, cache, step, y, q_heads, q_stride, y_stride, scale, most_positions, workspace, workspace_bytes, stream=0"),
+    ENTRY("lutgemm_kv_place", kPlace, "pages, past, fresh, tokens, most_tokens, first, positions, owner, slots, stream=0"),
+    ENTRY("lutgemm_kv_trim", kTrim, "pages, lengths, stream=0"),
+    ENTRY("lutgemm_rms_norm", kNorm, "x, residual, weight, sum, y, scales, tokens, n, group, x_stride, stream_stride, y_stride, eps, flags, stream=0"),
+    ENTRY("lutgemm_adapt", kAdapt, "x, base, adapters, of, owner, y, tokens, seqs, x_stride, base_stride, y_stride, flags, workspace, workspace_bytes, stream=0"),
     {"set_up", set_up, METH_VARARGS, nullptr},
     {"load", load, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,298 @@
+// The residual's addition and the root-mean-square norm in front of a product: include/lutgemm.h has the formulas.
+//
+// A workgroup owns a row and holds it in registers between the two things that are done with it, so that every value
+// is read once: s = x + r, the sum of squares (in 64 bits: squares of fp32 values leave 32), then s * inv * w.
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include "lutgemm_step.h"
+
+#ifndef LUT_PART
+#error "compiled once per part, -DLUT_PART=0 .. 3: x in fp16 or fp32 (1), the residual stream in fp16 or fp32 (2)"
+#endif
+
+namespace lutgemm_norm_parts {
+
+struct Params {
+  const void* x;
+  const void* residual;        // null: nothing is added
+  const _Float16* weight;      // null: ones
+  void* sum;                   // null: not kept
+  void* y;
+  float* scales;               // null: y is fp16
+  int64_t x_stride, stream_stride, y_stride;
+  int n, group, groups;
+  float eps, inverse_n;
+};
+
+typedef const void* (*Family)(int threads, int runs, bool wide, bool bytes);
+const void* family0(int threads, int runs, bool wide, bool bytes);
+const void* family1(int threads, int runs, bool wide, bool bytes);
+const void* family2(int threads, int runs, bool wide, bool bytes);
+const void* family3(int threads, int runs, bool wide, bool bytes);
+
+}  // namespace lutgemm_norm_parts
+
+namespace {
+
+using lutgemm_norm_parts::Params;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kRun = 8;      // channels that a thread has next to each other
+
+// Eight values from memory, 16 bytes at a time.
+template <typename T>
+__device__ __forceinline__ void load_wide(const T* p, float* v) {
+  T t[kRun];
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(t) / 16; ++i) reinterpret_cast<u32x4*>(t)[i] = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+  for (int e = 0; e < kRun; ++e) v[e] = (float)t[e];
+}
+template <typename T>
+__device__ __forceinline__ void store_wide(T* p, const float* v) {
+  T t[kRun];
+#pragma unroll
+  for (int e = 0; e < kRun; ++e) t[e] = (T)v[e];
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(t) / 16; ++i) reinterpret_cast<u32x4*>(p)[i] = reinterpret_cast<const u32x4*>(t)[i];
+}
+
+// WIDE: a thread's runs are eight channels next to each other, 16 bytes at a time; else rows begin anywhere and have any length: a
+// wavefront's lanes take channels next to each other.
+template <typename X, typename S, bool BYTES, bool WIDE, int THREADS, int RUNS>
+__global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
+  constexpr int kWaves = THREADS / 64;
+  extern __shared__ uint32_t tops[];               // of every group: the largest |y|, as bits
+  __shared__ double squares[kWaves];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const X* x = static_cast<const X*>(p.x) + row * p.x_stride;
+  const S* r = static_cast<const S*>(p.residual) + row * p.stream_stride;
+  S* sum = static_cast<S*>(p.sum) + row * p.stream_stride;
+
+  auto channel = [&](int run, int e) { return WIDE ? (run * THREADS + tid) * kRun + e : (run * kRun + e) * THREADS + tid; };
+  float v[RUNS][kRun], w[RUNS][kRun];
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k) {
+#pragma unroll
+    for (int e = 0; e < kRun; ++e) v[k][e] = 0.0f, w[k][e] = 1.0f;
+    if (WIDE) {
+      const int c = channel(k, 0);
+      if (c < p.n) {
+        load_wide(x + c, v[k]);
+        if (p.weight) load_wide(p.weight + c, w[k]);
+        if (p.residual) {
+          float t[kRun];
+          load_wide(r + c, t);
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) v[k][e] += t[e];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kRun; ++e) {
+        const int c = channel(k, e);
+        if (c < p.n) {
+          v[k][e] = (float)x[c];
+          if (p.weight) w[k][e] = (float)p.weight[c];
+          if (p.residual) v[k][e] += (float)r[c];
+        }
+      }
+    }
+  }
+  if (BYTES) {
+    for (int g = tid; g < p.groups; g += THREADS) tops[g] = 0;
+  }
+  double square = 0.0;
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k) {
+#pragma unroll
+    for (int e = 0; e < kRun; ++e) square = fma((double)v[k][e], (double)v[k][e], square);
+    if (p.sum) {
+      if (WIDE) {
+        if (channel(k, 0) < p.n) store_wide(sum + channel(k, 0), v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kRun; ++e)
+          if (channel(k, e) < p.n) sum[channel(k, e)] = (S)v[k][e];
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) square += __shfl_xor(square, d);
+  if ((tid & 63) == 0) squares[tid >> 6] = square;
+  __syncthreads();
+  double total = 0.0;
+#pragma unroll
+  for (int k = 0; k < kWaves; ++k) total += squares[k];
+  const float inv = (float)(1.0 / sqrt(total / (double)p.n + (double)p.eps));
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k) {
+#pragma unroll
+    for (int e = 0; e < kRun; ++e) v[k][e] = v[k][e] * inv * w[k][e];
+  }
+
+  if constexpr (!BYTES) {
+    _Float16* y = static_cast<_Float16*>(p.y) + row * p.y_stride;
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) {
+      if (WIDE) {
+        if (channel(k, 0) < p.n) store_wide(y + channel(k, 0), v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kRun; ++e)
+          if (channel(k, e) < p.n) y[channel(k, e)] = (_Float16)v[k][e];
+      }
+    }
+  } else {
+    int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) {
+      if (WIDE) {
+        uint32_t top = 0;                          // (as bits: infinities and NaNs come out on top)
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));       // of 32 channels, which are of one group
+        if ((tid & 3) == 0 && channel(k, 0) < p.n) atomicMax(&tops[channel(k, 0) / p.group], top);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kRun; ++e)
+          if (channel(k, e) < p.n) atomicMax(&tops[channel(k, e) / p.group], __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
+      }
+    }
+    __syncthreads();
+    for (int g = tid; g < p.groups; g += THREADS) {
+      const float top = __builtin_bit_cast(float, tops[g]);
+      p.scales[row * p.groups + g] = !(top < __builtin_inff()) ? __builtin_nanf("") : (top < 0x1p-100f ? 0.0f : top / 127.0f);
+    }
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) {
+      // (a group's codes: none where it has an infinity or a NaN, or nothing that is a number's worth)
+      auto code = [&](float value, uint32_t bits) {
+        const float top = __builtin_bit_cast(float, bits);
+        const float per = top < __builtin_inff() && !(top < 0x1p-100f) ? 127.0f / top : 0.0f;
+        return per == 0.0f ? 0 : (int)rintf(value * per);
+      };
+      if (WIDE) {
+        const int c = channel(k, 0);
+        if (c < p.n) {
+          const uint32_t bits = tops[c / p.group];
+          uint32_t word[2] = {0, 0};
+#pragma unroll
+          for (int e = 0; e < kRun; ++e) word[e / 4] |= ((uint32_t)code(v[k][e], bits) & 0xffu) << (8 * (e % 4));
+          *reinterpret_cast<u32x2*>(y + c) = (u32x2){word[0], word[1]};
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < kRun; ++e)
+          if (channel(k, e) < p.n) y[channel(k, e)] = (int8_t)code(v[k][e], tops[channel(k, e) / p.group]);
+      }
+    }
+  }
+}
+
+template <typename X, typename S, bool BYTES, bool WIDE>
+const void* pick(int threads, int runs) {
+#define CASE(t, r) \
+  if (threads == t && runs == r) return reinterpret_cast<const void*>(lutgemm_rms_norm_kernel<X, S, BYTES, WIDE, t, r>);
+  CASE(64, 1) CASE(64, 4) CASE(256, 2) CASE(256, 4) CASE(1024, 2) CASE(1024, 4)
+#undef CASE
+  return nullptr;
+}
+template <typename X, typename S>
+const void* pick(int threads, int runs, bool wide, bool bytes) {
+  return wide ? (bytes ? pick<X, S, true, true>(threads, runs) : pick<X, S, false, true>(threads, runs))
+              : (bytes ? pick<X, S, true, false>(threads, runs) : pick<X, S, false, false>(threads, runs));
+}
+
+}  // namespace
+
+namespace lutgemm_norm_parts {
+#if LUT_PART == 0
+const void* family0(int threads, int runs, bool wide, bool bytes) { return pick<_Float16, _Float16>(threads, runs, wide, bytes); }
+#elif LUT_PART == 1
+const void* family1(int threads, int runs, bool wide, bool bytes) { return pick<float, _Float16>(threads, runs, wide, bytes); }
+#elif LUT_PART == 2
+const void* family2(int threads, int runs, bool wide, bool bytes) { return pick<_Float16, float>(threads, runs, wide, bytes); }
+#else
+const void* family3(int threads, int runs, bool wide, bool bytes) { return pick<float, float>(threads, runs, wide, bytes); }
+#endif
+}  // namespace lutgemm_norm_parts
+
+#if LUT_PART == 0
+namespace {
+// The bytes from the first row's first value to the last row's last.
+struct Range {
+  uintptr_t from, to;
+};
+Range range_of(const void* p, int64_t rows, int64_t stride, int64_t n, int64_t size) {
+  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * stride + n) * size)};
+}
+// Whether a kernel that reads a row of `in` before it writes that row of `out` may be given both: the same rows of the same type, or
+// no byte in common (parts of one matrix's rows next to each other among them).
+bool apart(const void* in, int64_t in_stride, int64_t in_size, const void* out, int64_t out_stride, int64_t out_size, int64_t rows, int64_t n) {
+  const Range a = range_of(in, rows, in_stride, n, in_size), b = range_of(out, rows, out_stride, n, out_size);
+  if (a.to <= b.from || b.to <= a.from) return true;
+  if (in_stride * in_size != out_stride * out_size) return rows == 1 && in == out && in_size == out_size;
+  if (in == out) return in_size == out_size;
+  // Rows of one pitch: where a row of one begins within a row of the other.
+  const uintptr_t pitch = (uintptr_t)(in_stride * in_size);
+  const uintptr_t behind = a.from < b.from ? (b.from - a.from) % pitch : (pitch - (a.from - b.from) % pitch) % pitch;
+  return behind >= (uintptr_t)(n * in_size) && behind + (uintptr_t)(n * out_size) <= pitch;
+}
+}  // namespace
+
+extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales, int tokens, int n,
+                                int group, int64_t x_stride, int64_t stream_stride, int64_t y_stride, float eps, unsigned flags, void* hip_stream) {
+  using namespace lutgemm_norm_parts;
+  if (!x || !y || tokens < 0 || n < 1 || x_stride < n || y_stride < n || !(eps > 0.0f) || !(eps < __builtin_inff())) return LUTGEMM_EINVAL;
+  if (group < 0 || (!scales && group != 0)) return LUTGEMM_EINVAL;
+  if ((residual || sum) && stream_stride < n) return LUTGEMM_EINVAL;
+  if ((flags & ~(unsigned)(LUTGEMM_Y_F32 | LUTGEMM_NORM_STREAM_F32)) != 0) return LUTGEMM_EUNSUPPORTED;
+  const int64_t xs = flags & LUTGEMM_Y_F32 ? 4 : 2, ss = flags & LUTGEMM_NORM_STREAM_F32 ? 4 : 2, ys = scales ? 1 : 2;
+  if ((uintptr_t)x % xs != 0 || ((uintptr_t)residual | (uintptr_t)sum) % ss != 0 || (uintptr_t)y % ys != 0 || (uintptr_t)weight % 2 != 0 ||
+      (uintptr_t)scales % 4 != 0)
+    return LUTGEMM_EINVAL;
+  if (scales && group != 0 && n % group != 0) return LUTGEMM_EINVAL;
+  if (n > 32768 || tokens > 1 << 21 || (scales && group % 32 != 0)) return LUTGEMM_EUNSUPPORTED;   // (a grid has less than 2^32 threads)
+  if (tokens == 0) return LUTGEMM_OK;
+  const int64_t most_stride = (int64_t)1 << 28;          // (so that offsets in bytes stay within 64 bits)
+  if (x_stride > most_stride || y_stride > most_stride || ((residual || sum) && stream_stride > most_stride)) return LUTGEMM_EUNSUPPORTED;
+  if (!apart(x, x_stride, xs, y, y_stride, ys, tokens, n) || (residual && !apart(residual, stream_stride, ss, y, y_stride, ys, tokens, n)) ||
+      (sum && (!apart(x, x_stride, xs, sum, stream_stride, ss, tokens, n) || sum == y || !apart(sum, stream_stride, ss, y, y_stride, ys, tokens, n))) ||
+      (sum && residual && !apart(residual, stream_stride, ss, sum, stream_stride, ss, tokens, n)))
+    return LUTGEMM_EINVAL;
+  Params p = {};
+  p.x = x;
+  p.residual = residual;
+  p.weight = static_cast<const _Float16*>(weight);
+  p.sum = sum;
+  p.y = y;
+  p.scales = scales;
+  p.x_stride = x_stride;
+  p.stream_stride = stream_stride;
+  p.y_stride = y_stride;
+  p.n = n;
+  p.group = group == 0 ? n : group;
+  p.groups = n / p.group;
+  p.eps = eps;
+  auto rows16 = [&](const void* a, int64_t stride, int64_t size) { return ((uintptr_t)a | (uintptr_t)(stride * size)) % 16 == 0; };
+  const bool bytes = scales != nullptr;
+  const bool wide = n % (bytes ? 32 : 8) == 0 && rows16(x, x_stride, xs) && (!residual || rows16(residual, stream_stride, ss)) &&
+                    (!sum || rows16(sum, stream_stride, ss)) && (uintptr_t)weight % 16 == 0 &&
+                    (bytes ? ((uintptr_t)y | (uintptr_t)y_stride) % 8 == 0 : rows16(y, y_stride, 2));
+  const int units = (n + 7) / 8;
+  const int threads = units <= 256 ? 64 : (units <= 1024 ? 256 : 1024);
+  const int runs = threads == 64 ? (units <= 64 ? 1 : 4) : (units <= 2 * threads ? 2 : 4);
+  static const Family families[4] = {family0, family1, family2, family3};
+  const void* kern = families[(xs == 4 ? 1 : 0) + (ss == 4 ? 2 : 0)](threads, runs, wide, bytes);
+  void* args[] = {&p};
+  if (hipLaunchKernel(kern, dim3(tokens), dim3(threads), args, bytes ? 4 * (size_t)p.groups : 0, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    return LUTGEMM_EHIP;
+  return LUTGEMM_OK;
+}
+#endif

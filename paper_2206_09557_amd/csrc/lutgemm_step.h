@@ -1,0 +1,38 @@
+// What surrounds the products and attention of a step: sizes and plans that the kernels and the host helpers share.
+#ifndef LUTGEMM_STEP_H
+#define LUTGEMM_STEP_H
+
+#include <cstddef>
+#include <cstdint>
+
+#include "lutgemm.h"
+
+namespace lutgemm_step_detail {
+
+constexpr int64_t kCounterBytes = 32768;   // of a workspace, which products keep their arrival counters in
+
+// ---- low-rank adapters ----
+constexpr int kMostAdapters = 1024;
+constexpr int kMostRank = 256;
+constexpr int kMostAdapted = 1 << 16;      // tokens of a call
+constexpr int kFewTokens = 64;             // as many as a wavefront groups by itself
+constexpr int kRankBlock = 64;             // ranks of a workgroup of the first product
+
+struct AdaptPlan {
+  int tile;        // tokens of a workgroup: 16, 32 or 64
+  int tiles;       // of one adapter each: as many as there can be
+  int parts;       // of the n columns, in the first product
+  int part;        // columns of one: a multiple of 128
+  int rows;        // of the m rows that a workgroup of the second product has: a multiple of 256
+};
+AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens);
+int check_adapters(const lutgemm_adapters* a, int tokens);
+
+// The workspace behind the counters: tiles' table and the tokens by adapter (where there are more tokens than a wavefront groups), then
+// the first product's sums, [part][tile][token of the tile][rank].
+inline int64_t adapt_table_ints(const AdaptPlan& p, int tokens) { return tokens <= kFewTokens ? 0 : 4 + 4 * (int64_t)p.tiles + (tokens + 3) / 4 * 4; }
+inline int64_t adapt_part_floats(const AdaptPlan& p, int rank) { return (int64_t)p.tiles * p.tile * rank; }
+
+}  // namespace lutgemm_step_detail
+
+#endif

@@ -22,6 +22,7 @@ LUTGEMM_Q_GREEDY, LUTGEMM_Q_GREEDY_MEAN_OFFSET, LUTGEMM_Q_UNIFORM_RTN, LUTGEMM_Q
 LUTGEMM_Y_F16, LUTGEMM_Y_F32, LUTGEMM_ALPHA_SHARED, LUTGEMM_PATH_AUTO = 0, 1, 2, 4
 LUTGEMM_ROPE_NEIGHBOURS, LUTGEMM_ROPE_TRANSPOSE = 8, 16
 LUTGEMM_ROPE_PLAIN, LUTGEMM_ROPE_LINEAR, LUTGEMM_ROPE_BASE, LUTGEMM_ROPE_PARTS = 0, 1, 2, 3
+LUTGEMM_NORM_STREAM_F32 = 8
 LUTGEMM_KERNEL_GEMV, LUTGEMM_KERNEL_PAIR, LUTGEMM_KERNEL_QUAD, LUTGEMM_KERNEL_FP4, LUTGEMM_KERNEL_FP16 = 1, 2, 4, 16, 32
 
 _c = ctypes
@@ -75,6 +76,16 @@ _SIGNATURES = {
                                      _c.c_int64, _c.c_float, _c.c_int64, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
     "lutgemm_attention_workspace_bytes": (_c.c_size_t, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int64]),
     "lutgemm_plan_attention": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int64, _c.c_void_p]),
+    "lutgemm_kv_pages_init": (_c.c_int, [_c.c_void_p, _c.c_void_p]),
+    "lutgemm_kv_place": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int, _c.c_void_p, _c.c_void_p, _c.c_void_p,
+                                    _c.c_void_p, _c.c_void_p]),
+    "lutgemm_kv_trim": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p]),
+    "lutgemm_rms_norm": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int,
+                                    _c.c_int, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_float, _c.c_uint, _c.c_void_p]),
+    "lutgemm_adapt": (_c.c_int, [_c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int, _c.c_int,
+                                 _c.c_int64, _c.c_int64, _c.c_int64, _c.c_uint, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "lutgemm_adapt_workspace_bytes": (_c.c_size_t, [_c.c_void_p, _c.c_int]),
+    "lutgemm_plan_adapt": (_c.c_int, [_c.c_void_p, _c.c_int, _c.c_void_p]),
     "lutgemm_strerror": (_c.c_char_p, [_c.c_int]),
 }
 EXPORTS = tuple(_SIGNATURES)
@@ -111,7 +122,7 @@ def lib():
         _lib = handle
         if _binding is not None:
             _binding.load({name: ctypes.cast(getattr(handle, name), ctypes.c_void_p).value
-                           for name in _DEVICE_CALLS + _CACHE_CALLS if hasattr(handle, name)})
+                           for name in _DEVICE_CALLS + _CACHE_CALLS + _STEP_CALLS if hasattr(handle, name)})
     return _lib
 
 
@@ -382,6 +393,70 @@ def lutgemm_plan_attention(cache, step, q_heads, most_positions=0):
     return tuple(out)
 
 
+# ---- what surrounds the products and attention of a step -------------------------------
+class lutgemm_kv_pages(ctypes.Structure):
+    """Who has which pages of a cache: see the header.  Holds on to what it was given."""
+    _fields_ = [("free", _c.c_void_p), ("count", _c.c_void_p), ("owned", _c.c_void_p), ("table", _c.c_void_p), ("pages", _c.c_int64),
+                ("page_tokens", _c.c_int), ("seqs", _c.c_int), ("table_pages", _c.c_int)]
+
+    def __init__(self, free, count, owned, table, pages, page_tokens, seqs, table_pages):
+        super().__init__(_addr(free), _addr(count), _addr(owned), _addr(table), pages, page_tokens, seqs, table_pages)
+        self._held = (free, count, owned, table)
+        self._address = ctypes.addressof(self)
+
+    def data_ptr(self):
+        return self._address
+
+
+class lutgemm_adapters(ctypes.Structure):
+    """Low-rank adapters beside a product: see the header.  Holds on to what it was given."""
+    _fields_ = [("down", _c.c_void_p), ("up", _c.c_void_p), ("ranks", _c.c_void_p), ("scales", _c.c_void_p), ("m", _c.c_int64),
+                ("n", _c.c_int64), ("count", _c.c_int), ("rank", _c.c_int)]
+
+    def __init__(self, down, up, ranks, scales, m, n, count, rank):
+        super().__init__(_addr(down), _addr(up), _addr(ranks), _addr(scales), m, n, count, rank)
+        self._held = (down, up, ranks, scales)
+        self._address = ctypes.addressof(self)
+
+    def data_ptr(self):
+        return self._address
+
+
+def lutgemm_kv_pages_init(pages, stream=0):
+    _check(lib().lutgemm_kv_pages_init(_addr(pages), stream or None), "lutgemm_kv_pages_init")
+
+
+def lutgemm_kv_place(pages, past, fresh, tokens, most_tokens, first, positions, owner, slots, stream=0):
+    _check(lib().lutgemm_kv_place(_addr(pages), _addr(past), _addr(fresh), tokens, most_tokens, _addr(first), _addr(positions),
+                                  _addr(owner), _addr(slots), stream or None), "lutgemm_kv_place")
+
+
+def lutgemm_kv_trim(pages, lengths, stream=0):
+    _check(lib().lutgemm_kv_trim(_addr(pages), _addr(lengths), stream or None), "lutgemm_kv_trim")
+
+
+def lutgemm_rms_norm(x, residual, weight, sum, y, scales, tokens, n, group, x_stride, stream_stride, y_stride, eps, flags, stream=0):
+    _check(lib().lutgemm_rms_norm(_addr(x), _addr(residual), _addr(weight), _addr(sum), _addr(y), _addr(scales), tokens, n, group,
+                                  x_stride, stream_stride, y_stride, eps, flags, stream or None), "lutgemm_rms_norm")
+
+
+def lutgemm_adapt_workspace_bytes(adapters, tokens):
+    return lib().lutgemm_adapt_workspace_bytes(_addr(adapters), tokens)
+
+
+def lutgemm_adapt(x, base, adapters, of, owner, y, tokens, seqs, x_stride, base_stride, y_stride, flags, workspace, workspace_bytes,
+                  stream=0):
+    _check(lib().lutgemm_adapt(_addr(x), _addr(base), _addr(adapters), _addr(of), _addr(owner), _addr(y), tokens, seqs, x_stride,
+                               base_stride, y_stride, flags, _addr(workspace), workspace_bytes, stream or None), "lutgemm_adapt")
+
+
+def lutgemm_plan_adapt(adapters, tokens):
+    """(tokens of a tile, tiles at most, parts of the columns, columns of each, rows of a workgroup)"""
+    out = (ctypes.c_int * 5)()
+    _check(lib().lutgemm_plan_adapt(_addr(adapters), tokens, ctypes.addressof(out)), "lutgemm_plan_adapt")
+    return tuple(out)
+
+
 # The calls of a serving loop are bound by this marshalling where the layer is small: csrc/lutgemm_binding.cpp does it
 # for the usual arguments and hands everything else to the functions above.  Where it is not built (when this package
 # is imported to build it, or for want of Python's headers) they are the entry points themselves: the same calls, 1.1 us
@@ -389,12 +464,13 @@ def lutgemm_plan_attention(cache, step, q_heads, most_positions=0):
 _DEVICE_CALLS = ("lutgemm_gemv", "lutgemm_gemm", "lutgemm_gemm_mfma", "lutgemm_gemm_dequant_mfma", "lutgemm_gemv_static",
                  "lutgemm_gemv_group")
 _CACHE_CALLS = ("lutgemm_rope", "lutgemm_kv_write", "lutgemm_kv_read", "lutgemm_attention")
+_STEP_CALLS = ("lutgemm_kv_place", "lutgemm_kv_trim", "lutgemm_rms_norm", "lutgemm_adapt")
 try:
     _binding = importlib.import_module(__package__ + "._binding")
 except ImportError as e:
     if not isinstance(e, ModuleNotFoundError):   # built, but not for this process
         warnings.warn(f"the compiled marshalling of the device calls does not load, ctypes does it: {e}")
 else:
-    _binding.set_up({name: globals()[name] for name in _DEVICE_CALLS + _CACHE_CALLS}, _check)
+    _binding.set_up({name: globals()[name] for name in _DEVICE_CALLS + _CACHE_CALLS + _STEP_CALLS}, _check)
     # (one that was built before a call was added has none for it, till it is built again)
-    globals().update({name: getattr(_binding, name) for name in _DEVICE_CALLS + _CACHE_CALLS if hasattr(_binding, name)})
+    globals().update({name: getattr(_binding, name) for name in _DEVICE_CALLS + _CACHE_CALLS + _STEP_CALLS if hasattr(_binding, name)})
