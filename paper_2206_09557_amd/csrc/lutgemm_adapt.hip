@@ -107,10 +107,18 @@ __global__ __launch_bounds__(kSortThreads) void lutgemm_adapt_sort_kernel(AdaptP
   int32_t* mine = counts + wave * kinds;
   const int each = (p.tokens + kSortThreads - 1) / kSortThreads * 64;      // tokens of a wavefront, next to each other
   for (int turn = 0; turn < 2; ++turn) {
+    constexpr int kAhead = 8;
+    int ahead[kAhead];
     for (int i = 0; i < each; i += 64) {
-      const int token = wave * each + i + lane;
-      const bool live = token < p.tokens;
-      const int a = live ? adapter_of(p, token) : -1;
+      const int token = wave * each + i + lane, k = i / 64 % kAhead;
+      if (k == 0) {                              // (the next runs' are looked up together)
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ahead[u] = token + 64 * u < p.tokens && i + 64 * u < each ? adapter_of(p, token + 64 * u) : -1;
+      }
+      int a = ahead[0];
+#pragma unroll
+      for (int u = 1; u < kAhead; ++u) a = k == u ? ahead[u] : a;
+      const bool live = a >= 0;
       uint64_t same = __ballot(live);
       for (int bit = 1; bit <= p.count; bit *= 2) {
         const uint64_t set = __ballot((a & bit) != 0);
@@ -154,34 +162,44 @@ __global__ __launch_bounds__(kSortThreads) void lutgemm_adapt_sort_kernel(AdaptP
       }
       if (lane == 0) {
         begins[kinds] = tokens;
+        tiles[kinds] = cut;
         p.table[0] = cut;
       }
     }
     __syncthreads();
     for (int a = tid; a < kinds; a += kSortThreads) {
-      const int end = begins[a + 1];
-      int at = begins[a], number = tiles[a];
-      for (int from = at; from < end; from += tile, ++number) {
-        int32_t* entry = p.table + 4 + 4 * number;
-        entry[0] = a;
-        entry[1] = from;
-        entry[2] = min(end - from, tile);
-      }
+      int at = begins[a];
       for (int w = 0; w < kSortWaves; ++w) {
         const int have = counts[w * kinds + a];
         counts[w * kinds + a] = at;
         at += have;
       }
     }
+    for (int i = tid; i < tiles[kinds]; i += kSortThreads) {     // the adapter of a tile: the last whose first tile is not behind it
+      int lo = 0, hi = kinds - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tiles[mid] <= i)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      const int from = begins[lo] + (i - tiles[lo]) * tile;
+      int32_t* entry = p.table + 4 + 4 * i;
+      entry[0] = lo;
+      entry[1] = from;
+      entry[2] = min(begins[lo + 1] - from, tile);
+    }
     __syncthreads();
   }
 }
 
-// H^T of a tile, for a part of the columns and RANKS of its ranks: four wavefronts take a quarter of the part each.
+// H^T of a tile, for a part of the columns and RANKS of its ranks: four wavefronts take a quarter of the part each, AHEAD steps of 32 columns
+// on their way at a time.
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 template <int TILE, int RANKS>
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParams p) {
-  constexpr int NT = TILE / 16, RT = RANKS / 16;
+  constexpr int NT = TILE / 16, RT = RANKS / 16, AHEAD = NT * RT >= 8 ? 2 : 4;
   __shared__ int token[TILE];
   __shared__ __attribute__((aligned(16))) float sums[kWaves][TILE][RANKS + 4];
   const Tile tile = tile_of<TILE>(p, blockIdx.y, false, token);
@@ -200,23 +218,31 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParam
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < RT; ++j) acc[i][j] = (float4v){0, 0, 0, 0};
-  for (int64_t k = begin; k < end; k += 32) {
-    const bool inside = k + eight < end;         // (n is a multiple of 8)
-    const int64_t at = inside ? k + eight : 0;
-    half8v xs[NT], as[RT];
+  for (int64_t k = begin; k < end; k += 32 * AHEAD) {
+    half8v xs[AHEAD][NT], as[AHEAD][RT];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) xs[i] = *reinterpret_cast<const half8v*>(x[i] + at);
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t at = min(k + 32 * u + eight, p.n - 8);        // (n is a multiple of 8)
 #pragma unroll
-    for (int j = 0; j < RT; ++j) as[j] = *reinterpret_cast<const half8v*>(a[j] + at);
-    const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
+      for (int i = 0; i < NT; ++i) xs[u][i] = *reinterpret_cast<const half8v*>(x[i] + at);
 #pragma unroll
-    for (int i = 0; i < NT; ++i) xs[i] = inside ? xs[i] : none;
+      for (int j = 0; j < RT; ++j) as[u][j] = *reinterpret_cast<const half8v*>(a[j] + at);
+    }
 #pragma unroll
-    for (int j = 0; j < RT; ++j) as[j] = inside ? as[j] : none;
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k + 32 * u + 32 > end) {               // columns that there are not, or that are another wavefront's
+        const bool inside = k + 32 * u + eight < end;
+        const half8v none = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+        for (int i = 0; i < NT; ++i) xs[u][i] = inside ? xs[u][i] : none;
 #pragma unroll
-      for (int j = 0; j < RT; ++j) acc[i][j] = mfma(as[j], xs[i], acc[i][j]);
+        for (int j = 0; j < RT; ++j) as[u][j] = inside ? as[u][j] : none;
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) acc[i][j] = mfma(as[u][j], xs[u][i], acc[i][j]);
+    }
   }
 #pragma unroll
   for (int i = 0; i < NT; ++i)
@@ -234,116 +260,189 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParam
   }
 }
 
-// Y^T of a tile, for p.rows rows of m.  A wavefront takes 64 rows at a time as four matrix tiles, dealt so that a lane's results are 16
-// rows of its token next to each other (row 16 g + 4 i + e is row 4 g + e of tile i).
-template <int TILE, typename Y, bool WIDE>
+// The tile's A x, added up over the parts and scaled, as two fp16 numbers of a power of two that brings a token's largest to 2^14 .. 2^15
+// (so that neither overflows, and what is lost is 2^-22 of the largest), [token][rank] in LDS.
+template <int TILE>
+__device__ __forceinline__ void load_h(const AdaptParams& p, const Tile& tile, int steps, float* h, _Float16* high, _Float16* low, int pitch, int* drop) {
+  __shared__ __attribute__((aligned(16))) float4v meet[kThreads];
+  const int tid = threadIdx.x, items = tile.tokens * p.rank / 4;
+  const float scale = p.scales ? p.scales[tile.adapter] : 1.0f;
+  const float* from = p.sums + (int64_t)blockIdx.y * TILE * p.rank;
+  // Where there are few numbers to a part the parts are shared out: sharers are 256 / share threads apart.
+  int share = kThreads;
+  while (share / 2 >= items && share > 1) share /= 2;
+  const int sharers = kThreads / share, mine = tid / share;
+  for (int base = 0; base < items; base += share) {
+    const int i = base + tid % share;
+    float4v s = {0, 0, 0, 0};
+    if (i < items) {
+      for (int k = mine; k < p.parts; k += 4 * sharers) {
+        float4v v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float4v*>(from + min(k + u * sharers, p.parts - 1) * p.part_floats + 4 * (int64_t)i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (k + u * sharers < p.parts) s += v[u];
+      }
+    }
+    if (sharers > 1) {                           // (one turn of the loop)
+      meet[tid] = s;
+      __syncthreads();
+      if (mine != 0) continue;
+      for (int g = 1; g < sharers; ++g) s += meet[g * share + tid];
+    }
+    if (i < items) {
+      const int r = 4 * i % p.rank;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[4 * i + e] = r + e < tile.rank ? s[e] * scale : 0.0f;      // (beyond the rank there may be anything)
+    }
+  }
+  __syncthreads();
+  constexpr int kOf = kThreads / TILE;           // lanes of a token
+  const int t = tid / kOf, part = tid % kOf;
+  float top = 0.0f;
+  if (t < tile.tokens)
+    for (int r = part; r < tile.rank; r += kOf) top = fmaxf(top, fabsf(h[t * p.rank + r]));
+#pragma unroll
+  for (int d = 1; d < kOf; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  // (no power where the largest is an infinity: the result is no number then; or zero)
+  const int lift = top > 0.0f && top < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+  for (int r = part; r < 32 * steps; r += kOf) {
+    const float v = t < tile.tokens && r < tile.rank ? ldexpf(h[t * p.rank + r], lift) : 0.0f;
+    const _Float16 hi = (_Float16)v;
+    high[t * pitch + r] = hi;
+    low[t * pitch + r] = fabsf((float)hi) < __builtin_inff() ? (_Float16)(v - (float)hi) : (_Float16)0.0f;
+  }
+  if (part == 0) drop[t] = -lift;
+  __syncthreads();
+}
+
+// Y^T of a tile, for p.rows rows of m.  A wavefront takes 64 rows at a time as four matrix tiles, dealt so that every 16 bytes of
+// a lane's results are next to those of the three lanes that have the same token.  STEPS: of 32 ranks, whose operands are in registers, the
+// next rows' on their way; 0: any number.
+template <int TILE, typename Y, bool WIDE, int STEPS>
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_up_kernel(AdaptParams p) {
-  constexpr int NT = TILE / 16;
+  constexpr int NT = TILE / 16, HELD = STEPS > 0 ? STEPS : 1, RUN = 16 / sizeof(Y), RUNS = 16 / RUN;   // a lane's 16 rows: RUNS runs of RUN
   extern __shared__ __attribute__((aligned(16))) char shared[];
   __shared__ int token[TILE];
-  __shared__ float back[TILE];                   // what a token's results are multiplied with
+  __shared__ int drop[TILE];                     // the power of two that a token's results are multiplied with
   const Tile tile = tile_of<TILE>(p, blockIdx.y, p.copies, token);
   if (tile.tokens == 0) return;
-  const int steps = (tile.rank + 31) / 32, pitch = 32 * ((p.rank + 31) / 32) + 8;      // (a row's padding keeps rows in different banks)
+  const int steps = STEPS > 0 ? STEPS : (tile.rank + 31) / 32, pitch = 32 * ((p.rank + 31) / 32) + 8;      // (a row's padding keeps rows in different banks)
   float* h = reinterpret_cast<float*>(shared);
   _Float16* high = reinterpret_cast<_Float16*>(h + TILE * p.rank);
   _Float16* low = high + TILE * pitch;
-  if (tile.rank > 0) {
-    const float scale = p.scales ? p.scales[tile.adapter] : 1.0f;
-    const float* from = p.sums + (int64_t)blockIdx.y * TILE * p.rank;
-    for (int i = threadIdx.x; i < tile.tokens * p.rank; i += kThreads) {
-      float s = 0.0f;
-      if (i % p.rank < tile.rank) {
-        s = from[i];
-        for (int k = 1; k < p.parts; ++k) s += from[k * p.part_floats + i];
-        s *= scale;
-      }
-      h[i] = s;
-    }
-    __syncthreads();
-    constexpr int kOf = kThreads / TILE;         // lanes of a token
-    const int t = threadIdx.x / kOf, part = threadIdx.x % kOf;
-    float top = 0.0f;
-    if (t < tile.tokens)
-      for (int r = part; r < tile.rank; r += kOf) top = fmaxf(top, fabsf(h[t * p.rank + r]));
-#pragma unroll
-    for (int d = 1; d < kOf; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    // a power of two that brings the largest to 2^14 .. 2^15; none where it is an infinity (the result is no number then), or zero
-    int lift = 0;
-    if (top > 0.0f && top < __builtin_inff()) lift = 15 - __builtin_amdgcn_frexp_expf(top);
-    for (int r = part; r < 32 * steps; r += kOf) {
-      const float v = t < tile.tokens && r < tile.rank ? ldexpf(h[t * p.rank + r], lift) : 0.0f;
-      const _Float16 hi = (_Float16)v;
-      const float rest = v - (float)hi;
-      high[t * pitch + r] = hi;
-      low[t * pitch + r] = fabsf((float)hi) < __builtin_inff() ? (_Float16)rest : (_Float16)0.0f;
-    }
-    if (part == 0) back[t] = (float)lift;
-    __syncthreads();
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, four = lane >> 4;
   const int64_t last = min((int64_t)(blockIdx.x + 1) * p.rows, p.m);
-  for (int64_t m0 = (int64_t)blockIdx.x * p.rows + 64 * wave; m0 < last; m0 += 64 * kWaves) {
-    const _Float16* b[4];
+  const _Float16* up = p.up + (int64_t)min(tile.adapter, p.count - 1) * p.m * p.rank;
+  // The row of m that lane `col` of matrix tile i reads: row 4 g + e of it is row e % RUN of run 4 (i * 4 + e) / RUN of lane g.
+  const int own = RUN == 4 ? col : 8 * (col >> 2) + (col & 3);
+  auto row_of = [&](int64_t m0, int i) { return min(m0 + own + (RUN == 4 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)), p.m - 1); };
+  u32x4 live[HELD];                              // of the operands: ranks that there are
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = p.up + ((int64_t)min(tile.adapter, p.count - 1) * p.m + min(m0 + 16 * (col >> 2) + 4 * i + (col & 3), p.m - 1)) * p.rank;
+  for (int k = 0; k < HELD; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int left = tile.rank - (32 * k + 8 * four + 2 * e);
+      live[k][e] = left >= 2 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
+    }
+  u32x4 next[HELD][4];
+  auto fetch = [&](int64_t m0, int k0) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) next[k][i] = *reinterpret_cast<const u32x4*>(up + row_of(m0, i) * p.rank + min(32 * (k0 + k) + 8 * four, p.rank - 8));
+  };
+  int64_t m0 = (int64_t)blockIdx.x * p.rows + 64 * wave;
+  if (STEPS > 0 && tile.rank > 0) fetch(m0, 0);
+  if (tile.rank > 0) load_h<TILE>(p, tile, steps, h, high, low, pitch, drop);
+
+  for (; m0 < last; m0 += 64 * kWaves) {
     float4v acc[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[n][i] = (float4v){0, 0, 0, 0};
-    for (int k = 0; k < steps; ++k) {
-      const int r = 32 * k + 8 * four, live = tile.rank - r;      // ranks of this lane's eight that there are
-      half8v bs[4];
+    if (tile.rank > 0) {
+      for (int k0 = 0; k0 < steps; k0 += HELD) {
+        if (STEPS == 0) fetch(m0, k0);
+        half8v bs[HELD][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bs[i] = *reinterpret_cast<const half8v*>(b[i] + min(r, p.rank - 8));
+        for (int k = 0; k < HELD; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) bs[i][e] = e < live ? bs[i][e] : (_Float16)0.0f;
-      }
+          for (int i = 0; i < 4; ++i) {
+            u32x4 mask = live[k];
+            if (STEPS == 0) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const half8v hi = *reinterpret_cast<const half8v*>(high + (16 * n + col) * pitch + r);
-        const half8v lo = *reinterpret_cast<const half8v*>(low + (16 * n + col) * pitch + r);
+              for (int e = 0; e < 4; ++e) {
+                const int left = tile.rank - (32 * k0 + 8 * four + 2 * e);
+                mask[e] = left >= 2 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
+              }
+            }
+            bs[k][i] = __builtin_bit_cast(half8v, next[k][i] & mask);
+          }
+        if (STEPS > 0 && m0 + 64 * kWaves < last) fetch(m0 + 64 * kWaves, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] = mfma(bs[i], hi, mfma(bs[i], lo, acc[n][i]));
+        for (int k = 0; k < HELD; ++k)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const int at = (16 * n + col) * pitch + 32 * (k0 + k) + 8 * four;
+            const half8v hi = *reinterpret_cast<const half8v*>(high + at), lo = *reinterpret_cast<const half8v*>(low + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[n][i] = mfma(bs[k][i], hi, mfma(bs[k][i], lo, acc[n][i]));
+          }
       }
     }
-    const int64_t m = m0 + 16 * four;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int t = 16 * n + col;
-      if (t >= tile.tokens || m >= p.m) continue;
-      const int drop = tile.rank > 0 ? -(int)back[t] : 0;
-      const Y* base = static_cast<const Y*>(p.base) + token[t] * p.base_stride + m;
-      Y* y = static_cast<Y*>(p.y) + token[t] * p.y_stride + m;
-      const int rows = (int)min(p.m - m, (int64_t)16);
-      if (WIDE && rows == 16) {
-        Y v[16];
+      if (t >= tile.tokens) continue;
+      const int power = tile.rank > 0 ? drop[t] : 0;
+      const Y* base = static_cast<const Y*>(p.base) + token[t] * p.base_stride;
+      Y* y = static_cast<Y*>(p.y) + token[t] * p.y_stride;
+      u32x4 held[RUNS];
+      if (WIDE) {
 #pragma unroll
-        for (unsigned i = 0; i < sizeof(v) / 16; ++i) reinterpret_cast<u32x4*>(v)[i] = reinterpret_cast<const u32x4*>(base)[i];
+        for (int c = 0; c < RUNS; ++c) {
+          const int64_t m = m0 + 4 * RUN * c + RUN * four;
+          if (m + RUN <= p.m) held[c] = *reinterpret_cast<const u32x4*>(base + m);
+        }
+      }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = tile.rank > 0 ? (Y)((float)v[e] + ldexpf(acc[n][e / 4][e % 4], drop)) : v[e];
+      for (int c = 0; c < RUNS; ++c) {
+        const int64_t m = m0 + 4 * RUN * c + RUN * four;
+        float d[RUN];
 #pragma unroll
-        for (unsigned i = 0; i < sizeof(v) / 16; ++i) reinterpret_cast<u32x4*>(y)[i] = reinterpret_cast<const u32x4*>(v)[i];
-      } else {
+        for (int e = 0; e < RUN; ++e) d[e] = ldexpf(acc[n][c * (RUN / 4) + e / 4][e % 4], power);
+        if (WIDE && m + RUN <= p.m) {
+          Y v[RUN];
+          *reinterpret_cast<u32x4*>(v) = held[c];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          if (e < rows) y[e] = tile.rank > 0 ? (Y)((float)base[e] + ldexpf(acc[n][e / 4][e % 4], drop)) : base[e];
+          for (int e = 0; e < RUN; ++e) v[e] = tile.rank > 0 ? (Y)((float)v[e] + d[e]) : v[e];
+          *reinterpret_cast<u32x4*>(y + m) = *reinterpret_cast<const u32x4*>(v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < RUN; ++e)
+            if (m + e < p.m) y[m + e] = tile.rank > 0 ? (Y)((float)base[m + e] + d[e]) : base[m + e];
         }
       }
     }
   }
 }
 
-template <int TILE>
-const void* pick_up(bool f32, bool wide) {
-  return f32 ? (wide ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, float, true>) : reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, float, false>))
-             : (wide ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, _Float16, true>) : reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, _Float16, false>));
+template <int TILE, typename Y, bool WIDE>
+const void* pick_up(int rank) {
+  return rank <= 32   ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 1>)
+         : rank <= 64 ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 2>)
+                      : reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 0>);
 }
 template <int TILE>
-const void* pick_down(int rank, int* ranks) {
-  *ranks = rank <= 16 ? 16 : (rank <= 32 ? 32 : 64);
+const void* pick_up(bool f32, bool wide, int rank) {
+  return f32 ? (wide ? pick_up<TILE, float, true>(rank) : pick_up<TILE, float, false>(rank))
+             : (wide ? pick_up<TILE, _Float16, true>(rank) : pick_up<TILE, _Float16, false>(rank));
+}
+template <int TILE>
+const void* pick_down(int rank) {
   return rank <= 16   ? reinterpret_cast<const void*>(lutgemm_adapt_down_kernel<TILE, 16>)
          : rank <= 32 ? reinterpret_cast<const void*>(lutgemm_adapt_down_kernel<TILE, 32>)
                       : reinterpret_cast<const void*>(lutgemm_adapt_down_kernel<TILE, 64>);
@@ -401,17 +500,17 @@ extern "C" int lutgemm_adapt(const void* x, const void* base, const lutgemm_adap
   if (tokens > kFewTokens) {
     int tile = plan.tile;
     void* args[] = {&p, &tile};
-    rc = launch(reinterpret_cast<const void*>(lutgemm_adapt_sort_kernel), dim3(1), kSortThreads, args, 4 * (size_t)((kSortWaves + 2) * (a.count + 1) + 1), hip_stream);
+    rc = launch(reinterpret_cast<const void*>(lutgemm_adapt_sort_kernel), dim3(1), kSortThreads, args, 4 * (size_t)((kSortWaves + 2) * (a.count + 1) + 2), hip_stream);
     if (rc != LUTGEMM_OK) return rc;
   }
   void* args[] = {&p};
-  int ranks;
-  const void* down = pick_down<16>(a.rank, &ranks);
+  const int ranks = a.rank <= 16 ? 16 : (a.rank <= 32 ? 32 : kRankBlock);
+  const void* down = plan.tile == 16 ? pick_down<16>(a.rank) : (plan.tile == 32 ? pick_down<32>(a.rank) : pick_down<64>(a.rank));
   rc = launch(down, dim3(plan.parts, plan.tiles, (a.rank + ranks - 1) / ranks), kThreads, args, 0, hip_stream);
   if (rc != LUTGEMM_OK) return rc;
   const bool wide = (((uintptr_t)base | (uintptr_t)y | (uintptr_t)(base_stride * size) | (uintptr_t)(y_stride * size)) & 15) == 0;
   const int pitch = 32 * ((a.rank + 31) / 32) + 8;
   const size_t lds = (size_t)plan.tile * (4 * a.rank + 4 * pitch);
-  const void* up = pick_up<16>(size == 4, wide);
+  const void* up = plan.tile == 16 ? pick_up<16>(size == 4, wide, a.rank) : (plan.tile == 32 ? pick_up<32>(size == 4, wide, a.rank) : pick_up<64>(size == 4, wide, a.rank));
   return launch(up, dim3((a.m + plan.rows - 1) / plan.rows, plan.tiles), kThreads, args, lds, hip_stream);
 }

@@ -14,17 +14,18 @@ int check_adapters(const lutgemm_adapters* a, int tokens) {
 AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens) {
   AdaptPlan p;
   const int t = std::max(tokens, 1);
-  p.tile = 16;
+  // Tiles as large as the adapters' shares of the tokens are on average.
+  const int64_t share = t / std::min(a->count, t);
+  p.tile = share >= 48 && a->rank <= 128 ? 64 : (share >= 24 ? 32 : 16);
   // Groups by adapter, those without one included: each ends in a tile that may be part empty.
   const int64_t groups = std::min(a->count + 1, t);
-  p.tiles = (int)((t + groups * (p.tile - 1)) / p.tile);
-  p.tiles = std::min(p.tiles, t);
+  p.tiles = (int)(groups + (t - groups) / p.tile);
   const int64_t rank_blocks = (a->rank + kRankBlock - 1) / kRankBlock;
-  const int64_t most = (a->n + 511) / 512;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>({most, (1024 + p.tiles * rank_blocks - 1) / (p.tiles * rank_blocks), 32}));
+  const int64_t most = (a->n + 511) / 512, wanted = p.tile == 16 ? 1024 : 256;
+  int64_t parts = std::max<int64_t>(1, std::min<int64_t>({most, (wanted + p.tiles * rank_blocks - 1) / (p.tiles * rank_blocks), 32}));
   p.part = (int)(((a->n + parts - 1) / parts + 127) / 128 * 128);
   p.parts = (int)((a->n + p.part - 1) / p.part);
-  p.rows = 256;
+  p.rows = (int)(std::max<int64_t>(1, (a->m * p.tiles / 1536 + 255) / 256) * 256);
   return p;
 }
 
