@@ -318,17 +318,18 @@ __device__ __forceinline__ void load_h(const AdaptParams& p, const Tile& tile, i
 }
 
 // Y^T of a tile, for p.rows rows of m.  A wavefront takes 64 rows at a time as four matrix tiles, dealt so that every 16 bytes of
-// a lane's results are next to those of the three lanes that have the same token.  STEPS: of 32 ranks, whose operands are in registers, the
-// next rows' on their way; 0: any number.
+// a lane's results are next to those of the three lanes that have the same token.  STEPS: of 32 ranks, whose operands are in registers; of up to
+// two the next rows' are on their way, as is what the next results are added to.
 template <int TILE, typename Y, bool WIDE, int STEPS>
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_up_kernel(AdaptParams p) {
-  constexpr int NT = TILE / 16, HELD = STEPS > 0 ? STEPS : 1, RUN = 16 / sizeof(Y), RUNS = 16 / RUN;   // a lane's 16 rows: RUNS runs of RUN
+  constexpr int NT = TILE / 16, RUN = 16 / sizeof(Y), RUNS = 16 / RUN;   // a lane's 16 rows: RUNS runs of RUN
+  constexpr bool AHEAD = STEPS <= 2;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   __shared__ int token[TILE];
   __shared__ int drop[TILE];                     // the power of two that a token's results are multiplied with
   const Tile tile = tile_of<TILE>(p, blockIdx.y, p.copies, token);
   if (tile.tokens == 0) return;
-  const int steps = STEPS > 0 ? STEPS : (tile.rank + 31) / 32, pitch = 32 * ((p.rank + 31) / 32) + 8;      // (a row's padding keeps rows in different banks)
+  constexpr int pitch = 32 * STEPS + 8;          // (a row's padding keeps rows in different banks)
   float* h = reinterpret_cast<float*>(shared);
   _Float16* high = reinterpret_cast<_Float16*>(h + TILE * p.rank);
   _Float16* low = high + TILE * pitch;
@@ -337,93 +338,89 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_up_kernel(AdaptParams 
   const _Float16* up = p.up + (int64_t)min(tile.adapter, p.count - 1) * p.m * p.rank;
   // The row of m that lane `col` of matrix tile i reads: row 4 g + e of it is row e % RUN of run 4 (i * 4 + e) / RUN of lane g.
   const int own = RUN == 4 ? col : 8 * (col >> 2) + (col & 3);
-  auto row_of = [&](int64_t m0, int i) { return min(m0 + own + (RUN == 4 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)), p.m - 1); };
-  u32x4 live[HELD];                              // of the operands: ranks that there are
+  u32x4 next[STEPS][4];
+  auto fetch = [&](int64_t m0) {
 #pragma unroll
-  for (int k = 0; k < HELD; ++k)
+    for (int i = 0; i < 4; ++i) {
+      const _Float16* row = up + min(m0 + own + (RUN == 4 ? 16 * i : 32 * (i >> 1) + 4 * (i & 1)), p.m - 1) * p.rank;
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) next[k][i] = *reinterpret_cast<const u32x4*>(row + min(32 * k + 8 * four, p.rank - 8));
+    }
+  };
+  int64_t m0 = (int64_t)blockIdx.x * p.rows + 64 * wave;
+  if (AHEAD) fetch(m0);
+  u32x4 held[RUNS];                              // of base, for the next results
+  auto look = [&](int64_t at, int n) {
+    if (!WIDE || 16 * n + col >= tile.tokens) return;
+    const Y* base = static_cast<const Y*>(p.base) + token[16 * n + col] * p.base_stride;
+#pragma unroll
+    for (int c = 0; c < RUNS; ++c) {
+      const int64_t m = at + 4 * RUN * c + RUN * four;
+      if (m + RUN <= p.m) held[c] = *reinterpret_cast<const u32x4*>(base + m);
+    }
+  };
+  look(m0, 0);
+  if (tile.rank > 0) load_h<TILE>(p, tile, STEPS, h, high, low, pitch, drop);
+  u32x4 live[STEPS];                             // of the operands: ranks that there are
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int left = tile.rank - (32 * k + 8 * four + 2 * e);
       live[k][e] = left >= 2 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
     }
-  u32x4 next[HELD][4];
-  auto fetch = [&](int64_t m0, int k0) {
-#pragma unroll
-    for (int k = 0; k < HELD; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) next[k][i] = *reinterpret_cast<const u32x4*>(up + row_of(m0, i) * p.rank + min(32 * (k0 + k) + 8 * four, p.rank - 8));
-  };
-  int64_t m0 = (int64_t)blockIdx.x * p.rows + 64 * wave;
-  if (STEPS > 0 && tile.rank > 0) fetch(m0, 0);
-  if (tile.rank > 0) load_h<TILE>(p, tile, steps, h, high, low, pitch, drop);
 
   for (; m0 < last; m0 += 64 * kWaves) {
-    float4v acc[NT][4];
+    if (!AHEAD) fetch(m0);
+    half8v bs[STEPS][4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int k = 0; k < STEPS; ++k)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[n][i] = (float4v){0, 0, 0, 0};
-    if (tile.rank > 0) {
-      for (int k0 = 0; k0 < steps; k0 += HELD) {
-        if (STEPS == 0) fetch(m0, k0);
-        half8v bs[HELD][4];
-#pragma unroll
-        for (int k = 0; k < HELD; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            u32x4 mask = live[k];
-            if (STEPS == 0) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int left = tile.rank - (32 * k0 + 8 * four + 2 * e);
-                mask[e] = left >= 2 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
-              }
-            }
-            bs[k][i] = __builtin_bit_cast(half8v, next[k][i] & mask);
-          }
-        if (STEPS > 0 && m0 + 64 * kWaves < last) fetch(m0 + 64 * kWaves, 0);
-#pragma unroll
-        for (int k = 0; k < HELD; ++k)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const int at = (16 * n + col) * pitch + 32 * (k0 + k) + 8 * four;
-            const half8v hi = *reinterpret_cast<const half8v*>(high + at), lo = *reinterpret_cast<const half8v*>(low + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[n][i] = mfma(bs[k][i], hi, mfma(bs[k][i], lo, acc[n][i]));
-          }
-      }
-    }
+      for (int i = 0; i < 4; ++i) bs[k][i] = __builtin_bit_cast(half8v, next[k][i] & live[k]);
+    const bool more = m0 + 64 * kWaves < last;
+    if (AHEAD && more) fetch(m0 + 64 * kWaves);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int t = 16 * n + col;
-      if (t >= tile.tokens) continue;
-      const int power = tile.rank > 0 ? drop[t] : 0;
-      const Y* base = static_cast<const Y*>(p.base) + token[t] * p.base_stride;
-      Y* y = static_cast<Y*>(p.y) + token[t] * p.y_stride;
-      u32x4 held[RUNS];
-      if (WIDE) {
+      u32x4 base[RUNS];
 #pragma unroll
-        for (int c = 0; c < RUNS; ++c) {
-          const int64_t m = m0 + 4 * RUN * c + RUN * four;
-          if (m + RUN <= p.m) held[c] = *reinterpret_cast<const u32x4*>(base + m);
+      for (int c = 0; c < RUNS; ++c) base[c] = held[c];
+      if (n + 1 < NT)
+        look(m0, n + 1);
+      else if (more)
+        look(m0 + 64 * kWaves, 0);
+      float4v acc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] = (float4v){0, 0, 0, 0};
+      if (tile.rank > 0) {
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+          const half8v hi = *reinterpret_cast<const half8v*>(high + t * pitch + 32 * k + 8 * four);
+          const half8v lo = *reinterpret_cast<const half8v*>(low + t * pitch + 32 * k + 8 * four);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = mfma(bs[k][i], hi, mfma(bs[k][i], lo, acc[i]));
         }
       }
+      if (t >= tile.tokens) continue;
+      const int power = tile.rank > 0 ? drop[t] : 0;
+      const Y* from = static_cast<const Y*>(p.base) + token[t] * p.base_stride;
+      Y* y = static_cast<Y*>(p.y) + token[t] * p.y_stride;
 #pragma unroll
       for (int c = 0; c < RUNS; ++c) {
         const int64_t m = m0 + 4 * RUN * c + RUN * four;
         float d[RUN];
 #pragma unroll
-        for (int e = 0; e < RUN; ++e) d[e] = ldexpf(acc[n][c * (RUN / 4) + e / 4][e % 4], power);
+        for (int e = 0; e < RUN; ++e) d[e] = ldexpf(acc[c * (RUN / 4) + e / 4][e % 4], power);
         if (WIDE && m + RUN <= p.m) {
           Y v[RUN];
-          *reinterpret_cast<u32x4*>(v) = held[c];
+          *reinterpret_cast<u32x4*>(v) = base[c];
 #pragma unroll
           for (int e = 0; e < RUN; ++e) v[e] = tile.rank > 0 ? (Y)((float)v[e] + d[e]) : v[e];
           *reinterpret_cast<u32x4*>(y + m) = *reinterpret_cast<const u32x4*>(v);
         } else {
 #pragma unroll
           for (int e = 0; e < RUN; ++e)
-            if (m + e < p.m) y[m + e] = tile.rank > 0 ? (Y)((float)base[m + e] + d[e]) : base[m + e];
+            if (m + e < p.m) y[m + e] = tile.rank > 0 ? (Y)((float)from[m + e] + d[e]) : from[m + e];
         }
       }
     }
@@ -434,7 +431,8 @@ template <int TILE, typename Y, bool WIDE>
 const void* pick_up(int rank) {
   return rank <= 32   ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 1>)
          : rank <= 64 ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 2>)
-                      : reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 0>);
+         : rank <= 128 ? reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<TILE, Y, WIDE, 4>)
+                      : reinterpret_cast<const void*>(lutgemm_adapt_up_kernel<(TILE < 64 ? TILE : 32), Y, WIDE, 8>);
 }
 template <int TILE>
 const void* pick_up(bool f32, bool wide, int rank) {
@@ -509,7 +507,7 @@ extern "C" int lutgemm_adapt(const void* x, const void* base, const lutgemm_adap
   rc = launch(down, dim3(plan.parts, plan.tiles, (a.rank + ranks - 1) / ranks), kThreads, args, 0, hip_stream);
   if (rc != LUTGEMM_OK) return rc;
   const bool wide = (((uintptr_t)base | (uintptr_t)y | (uintptr_t)(base_stride * size) | (uintptr_t)(y_stride * size)) & 15) == 0;
-  const int pitch = 32 * ((a.rank + 31) / 32) + 8;
+  const int pitch = 32 * (a.rank <= 32 ? 1 : (a.rank <= 64 ? 2 : (a.rank <= 128 ? 4 : 8))) + 8;
   const size_t lds = (size_t)plan.tile * (4 * a.rank + 4 * pitch);
   const void* up = plan.tile == 16 ? pick_up<16>(size == 4, wide, a.rank) : (plan.tile == 32 ? pick_up<32>(size == 4, wide, a.rank) : pick_up<64>(size == 4, wide, a.rank));
   return launch(up, dim3((a.m + plan.rows - 1) / plan.rows, plan.tiles), kThreads, args, lds, hip_stream);
