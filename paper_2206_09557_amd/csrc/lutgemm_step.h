@@ -10,6 +10,7 @@
 namespace lutgemm_step_detail {
 
 constexpr int64_t kCounterBytes = 32768;   // of a workspace, which products keep their arrival counters in
+constexpr int64_t kCacheBytes = 32 << 20;   // of the L2 caches
 
 // ---- low-rank adapters ----
 constexpr int kMostAdapters = 1024;
@@ -19,19 +20,24 @@ constexpr int kFewTokens = 64;             // as many as a wavefront groups by i
 constexpr int kRankBlock = 64;             // ranks of a workgroup of the first product
 
 struct AdaptPlan {
-  int tile;        // tokens of a workgroup: 16, 32 or 64
+  int tile;        // tokens of a workgroup of the second product: 16, 32 or 64
   int tiles;       // of one adapter each: as many as there can be
   int parts;       // of the n columns, in the first product
-  int part;        // columns of one: a multiple of 128
+  int part;        // columns of one: a multiple of 256
   int rows;        // of the m rows that a workgroup of the second product has: a multiple of 256
 };
 AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens);
 int check_adapters(const lutgemm_adapters* a, int tokens);
 
-// The workspace behind the counters: tiles' table and the tokens by adapter (where there are more tokens than a wavefront groups), then
-// the first product's sums, [part][tile][token of the tile][rank].
-inline int64_t adapt_table_ints(const AdaptPlan& p, int tokens) { return tokens <= kFewTokens ? 0 : 4 + 4 * (int64_t)p.tiles + (tokens + 3) / 4 * 4; }
+// The workspace behind the counters: tiles' table and their tokens (where there are more tokens than a wavefront groups), then
+// the first product's sums, [part][tile][token of the tile][rank], and for as many tokens [tile] high and low numbers [token][rank] and a power for each token.
+inline int64_t adapt_table_ints(const AdaptPlan& p, int tokens) { return tokens <= kFewTokens ? 0 : 4 + (4 + (int64_t)p.tile) * p.tiles; }
 inline int64_t adapt_part_floats(const AdaptPlan& p, int rank) { return (int64_t)p.tiles * p.tile * rank; }
+inline int64_t adapt_joined_floats(const AdaptPlan& p, int tokens, int rank) {
+  int pad = 32;
+  while (pad < rank) pad *= 2;
+  return tokens <= kFewTokens ? 0 : (int64_t)p.tiles * p.tile * (pad + 1);
+}
 
 }  // namespace lutgemm_step_detail
 

@@ -16,16 +16,22 @@ AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens) {
   const int t = std::max(tokens, 1);
   // Tiles as large as the adapters' shares of the tokens are on average.
   const int64_t share = t / std::min(a->count, t);
-  p.tile = share >= 48 && a->rank <= 128 ? 64 : (share >= 24 ? 32 : 16);
+  p.tile = share >= 48 && a->rank <= 128 ? 64 : (share >= 24 && a->rank <= 128 ? 32 : 16);
   // Groups by adapter, those without one included: each ends in a tile that may be part empty.
   const int64_t groups = std::min(a->count + 1, t);
   p.tiles = (int)(groups + (t - groups) / p.tile);
   const int64_t rank_blocks = (a->rank + kRankBlock - 1) / kRankBlock;
-  const int64_t most = (a->n + 511) / 512, wanted = p.tile == 16 ? 1024 : 256;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>({most, (wanted + p.tiles * rank_blocks - 1) / (p.tiles * rank_blocks), 32}));
-  p.part = (int)(((a->n + parts - 1) / parts + 127) / 128 * 128);
+  // Of the first product as many workgroups as leave none waiting (1024 of them fit the device where a tile and a chunk of the ranks are small,
+  // else 512, but a third fewer is as fast, and leaves fewer parts to add up: 4096 tokens, 5120 columns, rank 64: 18.4 us in five parts, 23.2 in seven).
+  const int64_t chunk = p.tile == 16 && a->rank <= 32 ? 512 : 256, units = p.tiles * rank_blocks;
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(a->n + chunk - 1) / chunk, (chunk == 512 ? 1024 : 352) / units, 32}));
+  p.part = (int)(((a->n + parts - 1) / parts + chunk - 1) / chunk * chunk);
   p.parts = (int)((a->n + p.part - 1) / p.part);
-  p.rows = (int)(std::max<int64_t>(1, (a->m * p.tiles / 1536 + 255) / 256) * 256);
+  // Of the second one, which has 768 or 512 at work, about as many as that: a round more for a few would be as long as the first, and
+  // each begins with 4 us in which it streams nothing (32 adapters of rank 16, 36864 rows: 12.4 us in 768 workgroups, 14.6 in 1152;
+  // 12288 rows of 4096 tokens, rank 64: 48.8 in 469, 54.5 in 804).
+  const int64_t step = p.tile == 16 && a->rank <= 16 ? 512 : 256, pieces = std::max<int64_t>(1, (p.tile == 16 && a->rank <= 32 ? 768 : 512) / p.tiles);
+  p.rows = (int)(std::max<int64_t>(1, ((a->m + pieces - 1) / pieces + step / 2) / step) * step);
   return p;
 }
 
@@ -38,7 +44,7 @@ extern "C" {
 size_t lutgemm_adapt_workspace_bytes(const lutgemm_adapters* adapters, int tokens) {
   if (check_adapters(adapters, tokens) != LUTGEMM_OK) return 0;
   const AdaptPlan p = plan_adapt(adapters, tokens);
-  return (size_t)(kCounterBytes + 4 * (adapt_table_ints(p, tokens) + p.parts * adapt_part_floats(p, adapters->rank)));
+  return (size_t)(kCounterBytes + 4 * (adapt_table_ints(p, tokens) + p.parts * adapt_part_floats(p, adapters->rank) + adapt_joined_floats(p, tokens, adapters->rank)));
 }
 
 int lutgemm_plan_adapt(const lutgemm_adapters* adapters, int tokens, int* out) {

@@ -97,12 +97,14 @@ def test_adapt_refusals():
 def test_a_plan_covers_everything(tokens, count, rank, m, n):
     a = _adapters(m=m, n=n, count=count, rank=rank)
     tile, tiles, parts, part, rows = L.lutgemm_plan_adapt(a, tokens)
-    assert tile in (16, 32, 64) and part % 128 == 0 and rows % 256 == 0
-    assert part * parts >= n > part * (parts - 1)
+    assert tile in (16, 32, 64) and rows % 256 == 0
+    assert part % 256 == 0 and part * parts >= n > part * (parts - 1)
     # the most tiles that an assignment of tokens to adapters (or to none) can need: every group ends in a tile of one token
     groups = min(count + 1, tokens)
     assert tiles == groups + (tokens - groups) // tile
     floats = parts * tiles * tile * rank
-    table = 0 if tokens <= 64 else 4 + 4 * tiles + -(-tokens // 4) * 4
-    assert L.lutgemm_adapt_workspace_bytes(a, tokens) == 32768 + 4 * (table + floats)
+    table = 0 if tokens <= 64 else 4 + (4 + tile) * tiles
+    pad = next(r for r in (32, 64, 128, 256) if r >= rank)
+    joined = 0 if tokens <= 64 else tiles * tile * (pad + 1)
+    assert L.lutgemm_adapt_workspace_bytes(a, tokens) == 32768 + 4 * (table + floats + joined)
     assert tiles <= 65535 and 32768 + 4 * floats < 1 << 40
