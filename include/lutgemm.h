@@ -527,7 +527,7 @@ int lutgemm_kv_pages_init(const lutgemm_kv_pages* pages, void* hip_stream);
      slots      int64 [tokens]: page * page_tokens + place in the page of the row's position; -1 behind the last
    past, fresh, first and the pages' table make a lutgemm_kv_step of `tokens` rows: its sizes are the host's, so a
    captured graph places, writes and attends whatever lengths it finds.  past is not advanced.
-   Up to 65535 sequences and tables of 2^30 positions.                                    */
+   Up to 65535 sequences, tables of 2^30 positions a sequence and 2^30 entries, 2^30 pages and tokens.   */
 int lutgemm_kv_place(const lutgemm_kv_pages* pages, const int32_t* past, const int32_t* fresh, int tokens, int most_tokens,
                      int32_t* first, int32_t* positions, int32_t* owner, int64_t* slots, void* hip_stream);
 

@@ -39,7 +39,6 @@ struct AdaptParams {
   int64_t x_stride, base_stride, y_stride, m, n, part_floats;
   int tokens, seqs, count, rank, tiles, parts, part, rows;
   bool copies;                 // tokens without an adapter are copied
-  bool past;                   // y goes past the caches: there is more of it than they hold
 };
 
 __device__ __forceinline__ float4v mfma(half8v a, half8v b, float4v c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -474,7 +473,7 @@ struct Up {
         for (int e = 0; e < EACH; ++e) {
           const Y* base = static_cast<const Y*>(p.base) + target[min(16 * n + 4 * e + four, tile.tokens - 1)].base;
 #pragma unroll
-          for (int b = 0; b < BLOCKS; ++b) held[n % DEPTH][e][b] = __builtin_nontemporal_load(reinterpret_cast<const Run*>(base + min(at + 64 * b + 4 * col, p.m - 4)));
+          for (int b = 0; b < BLOCKS; ++b) held[n % DEPTH][e][b] = *reinterpret_cast<const Run*>(base + min(at + 64 * b + 4 * col, p.m - 4));
         }
       }
     };
@@ -542,12 +541,7 @@ struct Up {
             const int64_t m = m0 + 64 * b + 4 * col;
             Y* y = static_cast<Y*>(p.y) + to.y + m;
             if constexpr (WIDE) {
-              if (t < tile.tokens && m < p.m) {
-                if (p.past)
-                  __builtin_nontemporal_store(result[e][b], reinterpret_cast<Run*>(y));
-                else
-                  *reinterpret_cast<Run*>(y) = result[e][b];
-              }
+              if (t < tile.tokens && m < p.m) *reinterpret_cast<Run*>(y) = result[e][b];
             } else {
               const Y* base = static_cast<const Y*>(p.base) + to.base + m;
 #pragma unroll
@@ -583,7 +577,7 @@ __global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= 32 && sizeof(Y) ==
         for (int u = 0; u < kTogether; ++u) {
           const Y* base = static_cast<const Y*>(p.base) + token[min(t0 + u, tile.tokens - 1)] * p.base_stride + m;
           if (WIDE)
-            v[u] = __builtin_nontemporal_load(reinterpret_cast<const Run*>(base));
+            v[u] = *reinterpret_cast<const Run*>(base);
           else
             v[u][0] = *base;
         }
@@ -705,7 +699,6 @@ extern "C" int lutgemm_adapt(const void* x, const void* base, const lutgemm_adap
   p.part = plan.part;
   p.rows = plan.rows;
   p.copies = base != y;
-  p.past = tokens * a.m * (int64_t)size > kCacheBytes;
   if (tokens > kFewTokens) {
     int cut = plan.tile;
     void* args[] = {&p, &cut};

@@ -13,6 +13,8 @@ using namespace lutgemm_kv_detail;
 namespace {
 
 constexpr int kThreads = 1024, kEach = 4, kSeqs = kThreads * kEach;
+constexpr int kAtOnce = 2;       // rows, or pages, that a thread works on together
+constexpr int64_t kMostSum = 1 << 30;      // of rows, of pages: two such sums fit 32 bits
 
 struct PlaceParams {
   int32_t* free;
@@ -28,135 +30,176 @@ struct PlaceParams {
   int pages, page_tokens, seqs, table_pages, tokens, most_tokens;
 };
 
-// Sums over the workgroup of what each thread has, before it and of all; both fit 63 bits (65535 sequences, 31 bits each).
+// Sums of rows and of pages.  They stop at a bound just above what can be served (`most`), so that 32 bits hold any of them: below it they are
+// exact, at it somebody waits, and they do not fall.
 struct Pair {
-  int64_t rows, pages;
+  uint32_t rows, pages;
 };
+__device__ __forceinline__ Pair plus(Pair a, Pair b, Pair most) { return {min(a.rows + b.rows, most.rows), min(a.pages + b.pages, most.pages)}; }
+// What a lane before this one has (in its row of 16, or the last of an earlier row), 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ Pair before_it(Pair v) {
+  return {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)v.rows, CTRL, ROWS, 0xf, false), (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v.pages, CTRL, ROWS, 0xf, false)};
+}
+__device__ __forceinline__ Pair row_sums(Pair v, Pair most) {      // over 16 lanes, this one included
+  v = plus(v, before_it<0x111, 0xf>(v), most);
+  v = plus(v, before_it<0x112, 0xf>(v), most);
+  v = plus(v, before_it<0x114, 0xf>(v), most);
+  return plus(v, before_it<0x118, 0xf>(v), most);
+}
+__device__ __forceinline__ Pair of_lane(Pair v, int lane) {
+  return {(uint32_t)__builtin_amdgcn_readlane((int)v.rows, lane), (uint32_t)__builtin_amdgcn_readlane((int)v.pages, lane)};
+}
+// Over the workgroup: of the threads before this one, and of all.
 struct Scan {
   Pair before, all;
 };
-__device__ __forceinline__ Scan scan_of(Pair mine, Pair* sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Pair in = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t r = __shfl_up(in.rows, d), g = __shfl_up(in.pages, d);
-    if (lane >= d) in.rows += r, in.pages += g;
-  }
+__device__ __forceinline__ Scan scan_of(Pair mine, Pair most, Pair* sums) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Pair in = row_sums(mine, most);
+  in = plus(in, before_it<0x142, 0xa>(in), most);          // lane 15 of the row before, to rows 1 and 3
+  in = plus(in, before_it<0x143, 0xc>(in), most);          // lane 31, to rows 2 and 3
   if (lane == 63) sums[wave] = in;
+  const Pair earlier = before_it<0x138, 0xf>(in);          // (the lane before, of any row)
   __syncthreads();
-  Scan s = {{in.rows - mine.rows, in.pages - mine.pages}, {0, 0}};
-#pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    const Pair t = sums[w];
-    if (w < wave) s.before.rows += t.rows, s.before.pages += t.pages;
-    s.all.rows += t.rows, s.all.pages += t.pages;
-  }
+  static_assert(kThreads / 64 == 16, "a row of lanes has the wavefronts' sums");
+  const Pair waves = row_sums(sums[lane & 15], most);
+  const Pair of_waves = of_lane(waves, max(wave - 1, 0));
+  Scan s;
+  s.before = plus(earlier, wave > 0 ? of_waves : Pair{0, 0}, most);
+  s.all = of_lane(waves, 15);
   return s;
 }
 
-// The sequence that item i belongs to: the first whose end is beyond it.
-__device__ __forceinline__ int seq_of(const int32_t* ends, int count, int i) {
-  int lo = 0, hi = count - 1;          // (i is below the last end)
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (ends[mid] > i)
-      hi = mid;
-    else
-      lo = mid + 1;
+// The sequences that N items belong to: the first whose end is beyond each (below the last end).  Their searches go along together, as each is
+// a chain of reads of LDS.
+template <int N>
+__device__ __forceinline__ void seqs_of(const uint32_t* ends, int count, const uint32_t* item, int* seq) {
+#pragma unroll
+  for (int u = 0; u < N; ++u) seq[u] = 0;
+  for (int step = 1 << (31 - __builtin_clz(count)); step > 0; step >>= 1) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int next = seq[u] + step;
+      if (next < count && ends[next - 1] <= item[u]) seq[u] = next;
+    }
   }
-  return lo;
 }
 
-__device__ __forceinline__ int pages_for(int64_t positions, int page_tokens) { return (int)((positions + page_tokens - 1) / page_tokens); }
+__device__ __forceinline__ int pages_for(uint32_t positions, int page_tokens) { return (int)((positions + (uint32_t)page_tokens - 1) / (uint32_t)page_tokens); }
 
 // FILL: writes rows and pages (any number of workgroups, which share them out); KEEP: what the calls keep, `owned` and `count` (one
 // workgroup).  With one workgroup both at once; else a second launch keeps, as others may not have read yet what the first changes.
 template <bool FILL, bool KEEP>
 __global__ __launch_bounds__(kThreads) void lutgemm_kv_place_kernel(PlaceParams p) {
-  __shared__ int32_t ends[kSeqs], page_ends[kSeqs], had[kSeqs];
+  __shared__ uint32_t ends[kSeqs], page_ends[kSeqs];
+  __shared__ int32_t had[kSeqs], held[kSeqs];
   __shared__ Pair sums[kThreads / 64];
   __shared__ Pair stop;                // of all that are served
-  const int tid = threadIdx.x, share = blockIdx.x * kThreads + tid, shares = gridDim.x * kThreads;
-  const int64_t free = min(max(p.count[0], 0), p.pages);
+  __shared__ bool waits;
+  const int tid = threadIdx.x;
+  const uint32_t share = blockIdx.x * kThreads + tid, shares = gridDim.x * kThreads;
+  const uint32_t free = (uint32_t)min(max(p.count[0], 0), p.pages);
+  const Pair most = {(uint32_t)p.tokens + 1, free + 1};
   Pair before = {0, 0};                // of the sequences of earlier turns, served or not
   Pair served = {0, 0};
   bool over = false;                   // somebody waits: nobody behind is served
   for (int base = 0; base < p.seqs; base += kSeqs) {
     const int seqs = min(p.seqs - base, kSeqs);
-    int32_t past[kEach], want[kEach], need[kEach], owned[kEach];
-    Pair mine = {0, 0};
+    int32_t past[kEach], fresh[kEach], owned[kEach];
+    Pair want[kEach], mine = {0, 0};
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int s = base + min(tid * kEach + e, seqs - 1);
       past[e] = p.past[s];
-      want[e] = p.fresh[s];
+      fresh[e] = p.fresh[s];
       owned[e] = min(max(p.owned[s], 0), p.table_pages);
     }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const int64_t end = (int64_t)past[e] + want[e];
-      const bool fits = tid * kEach + e < seqs && past[e] >= 0 && want[e] > 0 && want[e] <= p.most_tokens && end <= (int64_t)p.table_pages * p.page_tokens;
-      want[e] = fits ? want[e] : 0;
-      need[e] = fits ? max(pages_for(end, p.page_tokens) - owned[e], 0) : 0;
-      mine.rows += want[e];
-      mine.pages += need[e];
+      const uint32_t end = (uint32_t)past[e] + (uint32_t)fresh[e];         // (of two that are not negative)
+      const bool fits = tid * kEach + e < seqs && past[e] >= 0 && fresh[e] > 0 && fresh[e] <= p.most_tokens && end <= (uint32_t)(p.table_pages * p.page_tokens);
+      want[e] = {fits ? (uint32_t)fresh[e] : 0u, fits ? (uint32_t)max(pages_for(end, p.page_tokens) - owned[e], 0) : 0u};
+      mine = plus(mine, {min(want[e].rows, most.rows), want[e].pages}, most);
     }
-    if (tid == 0) stop = {-1, 0};
-    const Scan scan = scan_of(mine, sums);               // (a barrier stands in it)
-    Pair at = {before.rows + scan.before.rows, before.pages + scan.before.pages};
+    if (tid == 0) waits = false;
+    const Scan scan = scan_of(mine, most, sums);         // (a barrier stands in it)
+    Pair at = plus(before, scan.before, most);
+    Pair to[kEach];
     bool ok[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const bool was = at.rows <= p.tokens && at.pages <= free;
       const Pair from = at;
-      at.rows += want[e];
-      at.pages += need[e];
-      ok[e] = at.rows <= p.tokens && at.pages <= free;
-      if (was && !ok[e] && !over) stop = from;           // (one thread's, as the sums do not fall)
+      const bool was = at.rows <= (uint32_t)p.tokens && at.pages <= free;
+      at = plus(at, {min(want[e].rows, most.rows), want[e].pages}, most);
+      to[e] = at;
+      ok[e] = at.rows <= (uint32_t)p.tokens && at.pages <= free;
+      if (was && !ok[e] && !over) {                      // (one thread's, as the sums do not fall)
+        stop = from;
+        waits = true;
+      }
     }
-    before.rows += scan.all.rows;
-    before.pages += scan.all.pages;
+    before = plus(before, scan.all, most);
     __syncthreads();
     const Pair start = served;
     if (!over) {
-      over = stop.rows >= 0;
+      over = waits;
       served = over ? stop : before;
     }
-    at = {before.rows - scan.all.rows + scan.before.rows, before.pages - scan.all.pages + scan.before.pages};
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int s = tid * kEach + e;
-      at.rows += want[e];
-      at.pages += need[e];
       if (s >= seqs) break;
-      const int32_t end = (int32_t)(ok[e] ? at.rows : served.rows), page_end = (int32_t)(ok[e] ? at.pages : served.pages);
+      const Pair end = ok[e] ? to[e] : served;
       if (FILL) {
-        ends[s] = end;
-        page_ends[s] = page_end;
+        ends[s] = end.rows;
+        page_ends[s] = end.pages;
         had[s] = owned[e];
-        if (blockIdx.x == 0) p.first[base + s + 1] = end;
+        held[s] = past[e];
+        if (blockIdx.x == 0) p.first[base + s + 1] = (int32_t)end.rows;
       }
-      if (KEEP && ok[e] && need[e] > 0) p.owned[base + s] = owned[e] + need[e];
+      if (KEEP && ok[e] && want[e].pages > 0) p.owned[base + s] = owned[e] + (int32_t)want[e].pages;
     }
     if (FILL) {
       __syncthreads();
-      for (int64_t i = start.pages + share; i < served.pages; i += shares) {
-        const int s = seq_of(page_ends, seqs, (int)i);
-        const int first_page = s == 0 ? (int)start.pages : page_ends[s - 1];
-        p.table[(int64_t)(base + s) * p.table_pages + had[s] + ((int)i - first_page)] = p.free[free - 1 - i];
+      // (the last threads first: they have the fewest rows)
+      for (uint32_t i0 = start.pages + (shares - 1 - share); i0 < served.pages; i0 += kAtOnce * shares) {
+        uint32_t i[kAtOnce];
+        int s[kAtOnce], page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) i[u] = min(i0 + u * shares, served.pages - 1);
+        seqs_of<kAtOnce>(page_ends, seqs, i, s);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) page[u] = p.free[free - 1 - i[u]];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const uint32_t first_page = s[u] == 0 ? start.pages : page_ends[s[u] - 1];
+          if (i0 + u * shares < served.pages) p.table[(int64_t)(base + s[u]) * p.table_pages + had[s[u]] + (int)(i[u] - first_page)] = page[u];
+        }
       }
-      for (int64_t i = start.rows + share; i < served.rows; i += shares) {
-        const int s = seq_of(ends, seqs, (int)i);
-        const int first_row = s == 0 ? (int)start.rows : ends[s - 1], first_page = s == 0 ? (int)start.pages : page_ends[s - 1];
-        const int position = p.past[base + s] + ((int)i - first_row);
-        if (p.positions) p.positions[i] = position;
-        if (p.owner) p.owner[i] = base + s;
-        if (p.slots) {
-          const int col = position / p.page_tokens;
-          // (pages of this step straight from the stack: the table's entries may not be written yet)
-          const int page = col < had[s] ? p.table[(int64_t)(base + s) * p.table_pages + col] : p.free[free - 1 - (first_page + col - had[s])];
-          p.slots[i] = page < 0 || page >= p.pages ? -1 : (int64_t)page * p.page_tokens + position % p.page_tokens;
+      for (uint32_t i0 = start.rows + share; i0 < served.rows; i0 += kAtOnce * shares) {
+        uint32_t i[kAtOnce], position[kAtOnce], col[kAtOnce];
+        int s[kAtOnce], page[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) i[u] = min(i0 + u * shares, served.rows - 1);
+        seqs_of<kAtOnce>(ends, seqs, i, s);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          position[u] = (uint32_t)held[s[u]] + (i[u] - (s[u] == 0 ? start.rows : ends[s[u] - 1]));
+          if (p.slots) {
+            col[u] = position[u] / (uint32_t)p.page_tokens;
+            // (pages of this step straight from the stack: the table's entries may not be written yet)
+            const uint32_t taken = (s[u] == 0 ? start.pages : page_ends[s[u] - 1]) + col[u] - (uint32_t)had[s[u]];
+            const int32_t* at = (int)col[u] < had[s[u]] ? p.table + (int64_t)(base + s[u]) * p.table_pages + col[u] : p.free + (free - 1 - taken);
+            page[u] = *at;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          if (i0 + u * shares >= served.rows) continue;
+          if (p.positions) p.positions[i[u]] = (int32_t)position[u];
+          if (p.owner) p.owner[i[u]] = base + s[u];
+          if (p.slots) p.slots[i[u]] = page[u] < 0 || page[u] >= p.pages ? -1 : (int64_t)page[u] * p.page_tokens + (position[u] - col[u] * (uint32_t)p.page_tokens);
         }
       }
     }
@@ -164,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void lutgemm_kv_place_kernel(PlaceParams 
   }
   if (FILL) {
     if (share == 0) p.first[0] = 0;
-    for (int64_t i = served.rows + share; i < p.tokens; i += shares) {
+    for (uint32_t i = served.rows + share; i < (uint32_t)p.tokens; i += shares) {
       if (p.positions) p.positions[i] = 0;
       if (p.owner) p.owner[i] = -1;
       if (p.slots) p.slots[i] = -1;
@@ -177,14 +220,17 @@ __global__ __launch_bounds__(kThreads) void lutgemm_kv_place_kernel(PlaceParams 
 // step took comes back in the order in which it would be taken again.
 template <bool FILL, bool KEEP>
 __global__ __launch_bounds__(kThreads) void lutgemm_kv_trim_kernel(PlaceParams p) {
-  __shared__ int32_t page_ends[kSeqs], kept[kSeqs];
+  __shared__ uint32_t page_ends[kSeqs];
+  __shared__ int32_t kept[kSeqs];
   __shared__ Pair sums[kThreads / 64];
-  const int tid = threadIdx.x, share = blockIdx.x * kThreads + tid, shares = gridDim.x * kThreads;
-  const int64_t free = min(max(p.count[0], 0), p.pages);
+  const int tid = threadIdx.x;
+  const uint32_t share = blockIdx.x * kThreads + tid, shares = gridDim.x * kThreads;
+  const uint32_t free = (uint32_t)min(max(p.count[0], 0), p.pages);
+  const Pair most = {0, 1u << 31};     // (a table has 2^30 entries at most)
   // The first page's place on the stack needs the sum of all: a turn over the sequences for it where they do not fit one.
-  int64_t back = 0;
+  uint32_t back = 0;
   for (int turn = p.seqs > kSeqs ? 0 : 1; turn < 2; ++turn) {
-    int64_t before = 0;
+    uint32_t before = 0;
     for (int base = 0; base < p.seqs; base += kSeqs) {
       const int seqs = min(p.seqs - base, kSeqs);
       int32_t keep[kEach], give[kEach];
@@ -193,41 +239,55 @@ __global__ __launch_bounds__(kThreads) void lutgemm_kv_trim_kernel(PlaceParams p
       for (int e = 0; e < kEach; ++e) {
         const int s = base + min(tid * kEach + e, seqs - 1);
         const int length = p.past[s], owned = min(max(p.owned[s], 0), p.table_pages);
-        keep[e] = length < 0 ? owned : min(pages_for(length, p.page_tokens), owned);
+        keep[e] = length < 0 ? owned : min(pages_for((uint32_t)length, p.page_tokens), owned);
         give[e] = tid * kEach + e < seqs ? owned - keep[e] : 0;
-        mine.pages += give[e];
+        mine.pages += (uint32_t)give[e];
       }
-      const Scan scan = scan_of(mine, sums);
-      if (turn == 0 || p.seqs <= kSeqs) back = before + scan.all.pages;
+      const Scan scan = scan_of(mine, most, sums);
+      const uint32_t all = scan.all.pages;
+      if (turn == 0 || p.seqs <= kSeqs) back = before + all;
       if (turn == 1) {
-        int64_t at = before + scan.before.pages;
+        uint32_t at = scan.before.pages;
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
           const int s = tid * kEach + e;
-          at += give[e];
+          at += (uint32_t)give[e];
           if (s >= seqs) break;
           if (FILL) {
-            page_ends[s] = (int32_t)(at - before);
+            page_ends[s] = at;
             kept[s] = keep[e];
           }
           if (KEEP && give[e] > 0) p.owned[base + s] = keep[e];
         }
         if (FILL) {
           __syncthreads();
-          for (int64_t i = share; i < scan.all.pages; i += shares) {
-            const int s = seq_of(page_ends, seqs, (int)i);
-            int32_t* entry = p.table + (int64_t)(base + s) * p.table_pages + kept[s] + ((int)i - (s == 0 ? 0 : page_ends[s - 1]));
-            const int64_t place = free + back - 1 - (before + i);
-            if (place < p.pages) p.free[place] = *entry;
-            *entry = -1;
+          for (uint32_t i0 = share; i0 < all; i0 += kAtOnce * shares) {
+            uint32_t i[kAtOnce];
+            int s[kAtOnce], page[kAtOnce];
+            int32_t* entry[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) i[u] = min(i0 + u * shares, all - 1);
+            seqs_of<kAtOnce>(page_ends, seqs, i, s);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+              entry[u] = p.table + (int64_t)(base + s[u]) * p.table_pages + kept[s[u]] + (int)(i[u] - (s[u] == 0 ? 0 : page_ends[s[u] - 1]));
+              page[u] = *entry[u];
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+              if (i0 + u * shares >= all) continue;
+              const int64_t place = (int64_t)free + back - 1 - ((int64_t)before + i[u]);
+              if (place < p.pages) p.free[place] = page[u];
+              *entry[u] = -1;
+            }
           }
         }
       }
-      before += scan.all.pages;
+      before += all;
       __syncthreads();
     }
   }
-  if (KEEP && share == 0) p.count[0] = (int32_t)min(free + back, (int64_t)p.pages);
+  if (KEEP && share == 0) p.count[0] = (int32_t)min((int64_t)free + back, (int64_t)p.pages);
 }
 
 __global__ __launch_bounds__(256) void lutgemm_kv_pages_init_kernel(PlaceParams p) {
@@ -242,8 +302,8 @@ int check_pages(const lutgemm_kv_pages* g) {
   if (!g || !g->free || !g->count || !g->owned || !g->table) return LUTGEMM_EINVAL;
   if ((((uintptr_t)g->free | (uintptr_t)g->count | (uintptr_t)g->owned | (uintptr_t)g->table) & 3) != 0) return LUTGEMM_EINVAL;
   if (g->pages < 1 || g->page_tokens < kBlock || g->page_tokens % kBlock != 0 || g->seqs < 1 || g->table_pages < 1) return LUTGEMM_EINVAL;
-  if (g->pages > INT32_MAX || g->page_tokens > 1 << 20 || g->seqs > kMostSeqs) return LUTGEMM_EUNSUPPORTED;
-  if ((int64_t)g->table_pages * g->page_tokens > kMostHeld) return LUTGEMM_EUNSUPPORTED;
+  if (g->pages > kMostSum || g->page_tokens > 1 << 20 || g->seqs > kMostSeqs) return LUTGEMM_EUNSUPPORTED;
+  if ((int64_t)g->table_pages * g->page_tokens > kMostHeld || (int64_t)g->table_pages * g->seqs > kMostSum) return LUTGEMM_EUNSUPPORTED;
   return LUTGEMM_OK;
 }
 PlaceParams params_of(const lutgemm_kv_pages* g) {
@@ -263,9 +323,9 @@ int launch(const void* kern, int groups, int threads, PlaceParams* p, void* stre
   return hipLaunchKernel(kern, dim3(groups), dim3(threads), args, 0, static_cast<hipStream_t>(stream)) == hipSuccess ? LUTGEMM_OK : LUTGEMM_EHIP;
 }
 
-// Rows (or pages to be moved) that one workgroup does by itself.
-constexpr int64_t kAlone = 16384;
-int groups_for(int64_t items) { return (int)(items <= kAlone ? 1 : (items / 4096 < 256 ? items / 4096 : 256)); }
+// One workgroup where it has few rows (or pages, of which most calls move far fewer than the most that there can be), as the second launch costs
+// more; else as many as have two rows a thread.
+int groups_for(int64_t items, int64_t alone) { return (int)(items <= alone ? 1 : (items / (2 * kThreads) < 256 ? items / (2 * kThreads) : 256)); }
 
 }  // namespace
 
@@ -285,6 +345,7 @@ int lutgemm_kv_place(const lutgemm_kv_pages* pages, const int32_t* past, const i
   if (!past || !fresh || !first || tokens < 0 || most_tokens < 0) return LUTGEMM_EINVAL;
   if ((((uintptr_t)past | (uintptr_t)fresh | (uintptr_t)first | (uintptr_t)positions | (uintptr_t)owner) & 3) != 0 || ((uintptr_t)slots & 7) != 0)
     return LUTGEMM_EINVAL;
+  if (tokens > kMostSum) return LUTGEMM_EUNSUPPORTED;
   PlaceParams p = params_of(pages);
   p.past = past;
   p.fresh = fresh;
@@ -294,7 +355,7 @@ int lutgemm_kv_place(const lutgemm_kv_pages* pages, const int32_t* past, const i
   p.slots = slots;
   p.tokens = tokens;
   p.most_tokens = most_tokens;
-  const int groups = groups_for(tokens);
+  const int groups = groups_for(tokens, 8192);
   if (groups == 1) return launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<true, true>), 1, kThreads, &p, hip_stream);
   const int filled = launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<true, false>), groups, kThreads, &p, hip_stream);
   return filled != LUTGEMM_OK ? filled : launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<false, true>), 1, kThreads, &p, hip_stream);
@@ -307,7 +368,7 @@ int lutgemm_kv_trim(const lutgemm_kv_pages* pages, const int32_t* lengths, void*
   PlaceParams p = params_of(pages);
   p.past = lengths;
   const int64_t items = (int64_t)p.seqs * p.table_pages;
-  const int groups = groups_for(items < p.pages ? items : p.pages);
+  const int groups = groups_for(items < p.pages ? items : p.pages, 32768);
   if (groups == 1) return launch(reinterpret_cast<const void*>(lutgemm_kv_trim_kernel<true, true>), 1, kThreads, &p, hip_stream);
   const int filled = launch(reinterpret_cast<const void*>(lutgemm_kv_trim_kernel<true, false>), groups, kThreads, &p, hip_stream);
   return filled != LUTGEMM_OK ? filled : launch(reinterpret_cast<const void*>(lutgemm_kv_trim_kernel<false, true>), 1, kThreads, &p, hip_stream);

@@ -19,7 +19,7 @@ def _pages(free=A, count=A, owned=A, table=A, pages=8, page_tokens=64, seqs=2, t
 
 BAD_PAGES = [(dict(free=0), E), (dict(count=0), E), (dict(owned=0), E), (dict(table=0), E), (dict(free=A + 2), E), (dict(table=A + 1), E), (dict(pages=0), E),
              (dict(page_tokens=48), E), (dict(page_tokens=0), E), (dict(seqs=0), E), (dict(table_pages=0), E), (dict(pages=1 << 31), U), (dict(seqs=65536), U),
-             (dict(page_tokens=1 << 21), U), (dict(table_pages=(1 << 24) + 1), U)]
+             (dict(page_tokens=1 << 21), U), (dict(table_pages=(1 << 24) + 1), U), (dict(pages=(1 << 30) + 1), U), (dict(seqs=65535, table_pages=1 << 15), U)]
 
 
 @pytest.mark.parametrize("change,want", BAD_PAGES, ids=lambda v: str(v))
@@ -35,6 +35,7 @@ def test_place_and_trim_refusals():
     for change in [dict(pages=None), dict(past=0), dict(fresh=None), dict(first=0), dict(tokens=-1), dict(most=-1), dict(past=A + 2), dict(fresh=A + 1), dict(first=A + 2),
                    dict(positions=A + 2), dict(owner=A + 3), dict(slots=A + 4)]:
         assert _refused(L.lutgemm_kv_place, *{**good, **change}.values()) == E, change
+    assert _refused(L.lutgemm_kv_place, *{**good, "tokens": (1 << 30) + 1}.values()) == U
     assert _refused(L.lutgemm_kv_trim, None, A) == E and _refused(L.lutgemm_kv_trim, _pages(), 0) == E and _refused(L.lutgemm_kv_trim, _pages(), A + 2) == E
 
 
