@@ -1,7 +1,9 @@
 // The residual's addition and the root-mean-square norm in front of a product: include/lutgemm.h has the formulas.
 //
 // A workgroup owns a row and holds it in registers between the two things that are done with it, so that every value
-// is read once: s = x + r, the sum of squares (in 64 bits: squares of fp32 values leave 32), then s * inv * w.
+// is read once: s = x + r, the sum of squares (in 64 bits: squares of fp32 values leave 32), then s * inv * w.  What bounds it is
+// HBM: 4096 rows of 12288 channels, 403 MB, 68.7 us, 5.9 TB/s (a copy past the caches: 6.3); of few rows the launch and one chain of
+// load, sum and store (3.4 us for one).  The next row on its way during a row's sum (512 workgroups that stay) was no faster: 75 to 79 us.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -22,7 +24,8 @@ struct Params {
   float* scales;               // null: y is fp16
   int64_t x_stride, stream_stride, y_stride;
   int n, group, groups;
-  float eps, inverse_n;
+  float eps;
+  bool past;                   // outputs go past the caches: there is more of them than they hold
 };
 
 typedef const void* (*Family)(int threads, int runs, bool wide, bool bytes);
@@ -42,22 +45,28 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kRun = 8;      // channels that a thread has next to each other
 
-// Eight values from memory, 16 bytes at a time.
+// Eight values as they are in memory, 16 bytes at a time.
 template <typename T>
-__device__ __forceinline__ void load_wide(const T* p, float* v) {
-  T t[kRun];
+struct Eight {
+  u32x4 part[sizeof(T) * kRun / 16];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (unsigned i = 0; i < sizeof(t) / 16; ++i) reinterpret_cast<u32x4*>(t)[i] = reinterpret_cast<const u32x4*>(p)[i];
-#pragma unroll
-  for (int e = 0; e < kRun; ++e) v[e] = (float)t[e];
-}
+    for (unsigned i = 0; i < sizeof(part) / 16; ++i) part[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ float value(int e) const { return (float)reinterpret_cast<const T*>(part)[e]; }
+};
 template <typename T>
-__device__ __forceinline__ void store_wide(T* p, const float* v) {
+__device__ __forceinline__ void store_wide(T* p, const float* v, bool past) {
   T t[kRun];
 #pragma unroll
   for (int e = 0; e < kRun; ++e) t[e] = (T)v[e];
 #pragma unroll
-  for (unsigned i = 0; i < sizeof(t) / 16; ++i) reinterpret_cast<u32x4*>(p)[i] = reinterpret_cast<const u32x4*>(t)[i];
+  for (unsigned i = 0; i < sizeof(t) / 16; ++i) {
+    if (past)
+      __builtin_nontemporal_store(reinterpret_cast<const u32x4*>(t)[i], reinterpret_cast<u32x4*>(p) + i);
+    else
+      reinterpret_cast<u32x4*>(p)[i] = reinterpret_cast<const u32x4*>(t)[i];
+  }
 }
 
 // WIDE: a thread's runs are eight channels next to each other, 16 bytes at a time; else rows begin anywhere and have any length: a
@@ -68,38 +77,47 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
   extern __shared__ uint32_t tops[];               // of every group: the largest |y|, as bits
   __shared__ double squares[kWaves];
   const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const X* x = static_cast<const X*>(p.x) + row * p.x_stride;
-  const S* r = static_cast<const S*>(p.residual) + row * p.stream_stride;
-  S* sum = static_cast<S*>(p.sum) + row * p.stream_stride;
+  auto channel = [&](int run, int e) { return (uint32_t)(WIDE ? (run * THREADS + tid) * kRun + e : (run * kRun + e) * THREADS + tid); };
+  // (Loads have no branches: beyond the row's end they repeat its last eight channels.)
+  auto place = [&](int run) { return min(channel(run, 0), (uint32_t)(p.n - kRun)); };
 
-  auto channel = [&](int run, int e) { return WIDE ? (run * THREADS + tid) * kRun + e : (run * kRun + e) * THREADS + tid; };
-  float v[RUNS][kRun], w[RUNS][kRun];
+  Eight<_Float16> w[RUNS];
+  if constexpr (WIDE) {
+    if (p.weight) {
+#pragma unroll
+      for (int k = 0; k < RUNS; ++k) w[k].load(p.weight + place(k));
+    }
+  }
+  Eight<X> x[RUNS];
+  Eight<S> r[RUNS];
+  const int64_t row = blockIdx.x;
+  if (WIDE) {
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) x[k].load(static_cast<const X*>(p.x) + row * p.x_stride + place(k));
+    if (p.residual) {
+#pragma unroll
+      for (int k = 0; k < RUNS; ++k) r[k].load(static_cast<const S*>(p.residual) + row * p.stream_stride + place(k));
+    }
+  }
+  float v[RUNS][kRun];
 #pragma unroll
   for (int k = 0; k < RUNS; ++k) {
-#pragma unroll
-    for (int e = 0; e < kRun; ++e) v[k][e] = 0.0f, w[k][e] = 1.0f;
-    if (WIDE) {
-      const int c = channel(k, 0);
-      if (c < p.n) {
-        load_wide(x + c, v[k]);
-        if (p.weight) load_wide(p.weight + c, w[k]);
-        if (p.residual) {
-          float t[kRun];
-          load_wide(r + c, t);
-#pragma unroll
-          for (int e = 0; e < kRun; ++e) v[k][e] += t[e];
-        }
-      }
-    } else {
+    if constexpr (WIDE) {
+      const bool inside = channel(k, 0) < (uint32_t)p.n;
 #pragma unroll
       for (int e = 0; e < kRun; ++e) {
-        const int c = channel(k, e);
-        if (c < p.n) {
-          v[k][e] = (float)x[c];
-          if (p.weight) w[k][e] = (float)p.weight[c];
-          if (p.residual) v[k][e] += (float)r[c];
-        }
+        v[k][e] = x[k].value(e);
+        if (p.residual) v[k][e] += r[k].value(e);
+        v[k][e] = inside ? v[k][e] : 0.0f;
+      }
+    } else {
+      const X* at = static_cast<const X*>(p.x) + row * p.x_stride;
+      const S* stream = static_cast<const S*>(p.residual) + row * p.stream_stride;
+#pragma unroll
+      for (int e = 0; e < kRun; ++e) {
+        const uint32_t c = channel(k, e);
+        v[k][e] = c < (uint32_t)p.n ? (float)at[c] : 0.0f;
+        if (p.residual && c < (uint32_t)p.n) v[k][e] += (float)stream[c];
       }
     }
   }
@@ -108,16 +126,19 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
   }
   double square = 0.0;
 #pragma unroll
-  for (int k = 0; k < RUNS; ++k) {
+  for (int k = 0; k < RUNS; ++k)
 #pragma unroll
     for (int e = 0; e < kRun; ++e) square = fma((double)v[k][e], (double)v[k][e], square);
-    if (p.sum) {
+  if (p.sum) {
+    S* sum = static_cast<S*>(p.sum) + row * p.stream_stride;
+#pragma unroll
+    for (int k = 0; k < RUNS; ++k) {
       if (WIDE) {
-        if (channel(k, 0) < p.n) store_wide(sum + channel(k, 0), v[k]);
+        if (channel(k, 0) < (uint32_t)p.n) store_wide(sum + channel(k, 0), v[k], p.past);
       } else {
 #pragma unroll
         for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < p.n) sum[channel(k, e)] = (S)v[k][e];
+          if (channel(k, e) < (uint32_t)p.n) sum[channel(k, e)] = (S)v[k][e];
       }
     }
   }
@@ -132,7 +153,11 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
 #pragma unroll
   for (int k = 0; k < RUNS; ++k) {
 #pragma unroll
-    for (int e = 0; e < kRun; ++e) v[k][e] = v[k][e] * inv * w[k][e];
+    for (int e = 0; e < kRun; ++e) {
+      float weight = 1.0f;
+      if (p.weight) weight = WIDE ? w[k].value(e) : (channel(k, e) < (uint32_t)p.n ? (float)p.weight[channel(k, e)] : 1.0f);
+      v[k][e] = v[k][e] * inv * weight;
+    }
   }
 
   if constexpr (!BYTES) {
@@ -140,11 +165,11 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
 #pragma unroll
     for (int k = 0; k < RUNS; ++k) {
       if (WIDE) {
-        if (channel(k, 0) < p.n) store_wide(y + channel(k, 0), v[k]);
+        if (channel(k, 0) < (uint32_t)p.n) store_wide(y + channel(k, 0), v[k], p.past);
       } else {
 #pragma unroll
         for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < p.n) y[channel(k, e)] = (_Float16)v[k][e];
+          if (channel(k, e) < (uint32_t)p.n) y[channel(k, e)] = (_Float16)v[k][e];
       }
     }
   } else {
@@ -157,11 +182,11 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
         for (int e = 0; e < kRun; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
         top = max(top, (uint32_t)__shfl_xor((int)top, 1));
         top = max(top, (uint32_t)__shfl_xor((int)top, 2));       // of 32 channels, which are of one group
-        if ((tid & 3) == 0 && channel(k, 0) < p.n) atomicMax(&tops[channel(k, 0) / p.group], top);
+        if ((tid & 3) == 0 && channel(k, 0) < (uint32_t)p.n) atomicMax(&tops[channel(k, 0) / (uint32_t)p.group], top);
       } else {
 #pragma unroll
         for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < p.n) atomicMax(&tops[channel(k, e) / p.group], __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
+          if (channel(k, e) < (uint32_t)p.n) atomicMax(&tops[channel(k, e) / (uint32_t)p.group], __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
       }
     }
     __syncthreads();
@@ -172,24 +197,24 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
 #pragma unroll
     for (int k = 0; k < RUNS; ++k) {
       // (a group's codes: none where it has an infinity or a NaN, or nothing that is a number's worth)
-      auto code = [&](float value, uint32_t bits) {
+      auto per = [&](uint32_t bits) {
         const float top = __builtin_bit_cast(float, bits);
-        const float per = top < __builtin_inff() && !(top < 0x1p-100f) ? 127.0f / top : 0.0f;
-        return per == 0.0f ? 0 : (int)rintf(value * per);
+        return top < __builtin_inff() && !(top < 0x1p-100f) ? 127.0f / top : 0.0f;
       };
+      auto code = [&](float value, float per) { return per == 0.0f ? 0 : (int)rintf(value * per); };
       if (WIDE) {
-        const int c = channel(k, 0);
-        if (c < p.n) {
-          const uint32_t bits = tops[c / p.group];
+        const uint32_t c = channel(k, 0);
+        if (c < (uint32_t)p.n) {
+          const float steps = per(tops[c / (uint32_t)p.group]);
           uint32_t word[2] = {0, 0};
 #pragma unroll
-          for (int e = 0; e < kRun; ++e) word[e / 4] |= ((uint32_t)code(v[k][e], bits) & 0xffu) << (8 * (e % 4));
+          for (int e = 0; e < kRun; ++e) word[e / 4] |= ((uint32_t)code(v[k][e], steps) & 0xffu) << (8 * (e % 4));
           *reinterpret_cast<u32x2*>(y + c) = (u32x2){word[0], word[1]};
         }
       } else {
 #pragma unroll
         for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < p.n) y[channel(k, e)] = (int8_t)code(v[k][e], tops[channel(k, e) / p.group]);
+          if (channel(k, e) < (uint32_t)p.n) y[channel(k, e)] = (int8_t)code(v[k][e], per(tops[channel(k, e) / (uint32_t)p.group]));
       }
     }
   }
@@ -199,7 +224,7 @@ template <typename X, typename S, bool BYTES, bool WIDE>
 const void* pick(int threads, int runs) {
 #define CASE(t, r) \
   if (threads == t && runs == r) return reinterpret_cast<const void*>(lutgemm_rms_norm_kernel<X, S, BYTES, WIDE, t, r>);
-  CASE(64, 1) CASE(64, 4) CASE(256, 2) CASE(256, 4) CASE(1024, 2) CASE(1024, 4)
+  CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 1) CASE(256, 2) CASE(256, 3) CASE(256, 4) CASE(512, 3) CASE(512, 4) CASE(1024, 1) CASE(1024, 2) CASE(1024, 3) CASE(1024, 4)
 #undef CASE
   return nullptr;
 }
@@ -249,6 +274,7 @@ bool apart(const void* in, int64_t in_stride, int64_t in_size, const void* out, 
 extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales, int tokens, int n,
                                 int group, int64_t x_stride, int64_t stream_stride, int64_t y_stride, float eps, unsigned flags, void* hip_stream) {
   using namespace lutgemm_norm_parts;
+  using namespace lutgemm_step_detail;
   if (!x || !y || tokens < 0 || n < 1 || x_stride < n || y_stride < n || !(eps > 0.0f) || !(eps < __builtin_inff())) return LUTGEMM_EINVAL;
   if (group < 0 || (!scales && group != 0)) return LUTGEMM_EINVAL;
   if ((residual || sum) && stream_stride < n) return LUTGEMM_EINVAL;
@@ -286,8 +312,14 @@ extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void*
                     (!sum || rows16(sum, stream_stride, ss)) && (uintptr_t)weight % 16 == 0 &&
                     (bytes ? ((uintptr_t)y | (uintptr_t)y_stride) % 8 == 0 : rows16(y, y_stride, 2));
   const int units = (n + 7) / 8;
-  const int threads = units <= 256 ? 64 : (units <= 1024 ? 256 : 1024);
-  const int runs = threads == 64 ? (units <= 64 ? 1 : 4) : (units <= 2 * threads ? 2 : 4);
+  // Threads enough for four runs each; more where there are few rows and much to do for a value, one by one or to 8 bits (77 rows of
+  // 5003 channels 5.6 us with 1024 threads, 9.7 with 256; 509 of 8192 to 8 bits 10.1 and 11.5).
+  const bool spread = tokens <= 1024 && (!wide || bytes);
+  const int threads = spread ? (units <= 64 ? 64 : (units <= 256 ? 256 : 1024)) : (units <= 256 ? 64 : (units <= 1024 ? 256 : (units <= 2048 ? 512 : 1024)));
+  int runs = (units + threads - 1) / threads;
+  if (threads == 64 && runs == 3) runs = 4;
+  // (4096 rows, fp16: 5120 channels 25.3 us so and 30.8 by way of the caches, 12288 68.7 and 70.9)
+  p.past = (int64_t)tokens * n * ((sum ? ss : 0) + ys) > kCacheBytes;
   static const Family families[4] = {family0, family1, family2, family3};
   const void* kern = families[(xs == 4 ? 1 : 0) + (ss == 4 ? 2 : 0)](threads, runs, wide, bytes);
   void* args[] = {&p};

@@ -10,6 +10,7 @@
 namespace lutgemm_step_detail {
 
 constexpr int64_t kCounterBytes = 32768;   // of a workspace, which products keep their arrival counters in
+constexpr int64_t kCacheBytes = 32 << 20;   // of the L2 caches
 
 // ---- low-rank adapters ----
 constexpr int kMostAdapters = 1024;
