@@ -1,10 +1,10 @@
-"""The attention half of a decoder layer over a quantised cache: query/key/value product, rotary positions, cache, attention,
-output product, all calls of this library.
+"""The attention half of a decoder layer over a quantised cache: norm, query/key/value product, rotary positions, cache, attention,
+output product, low-rank adapters beside both products, all calls of this library.
 
-    python -m paper_2206_09557_amd.decode [--seqs 4 --prompt 200 --steps 64 --kv-bits 8]
+    python -m paper_2206_09557_amd.decode [--seqs 4 --prompt 200 --steps 64 --kv-bits 8 --adapters 3 --rank 16]
 
-fills the cache with prompts, decodes from a captured graph whose lengths advance on the device, then has a tree of drafted
-tokens looked at in one step and its accepted branch kept, and prints what a step takes and how far a token decoded by
+fills the cache with prompts, decodes from a captured graph whose tokens are placed and whose pages are taken on the device, then has a
+tree of drafted tokens looked at in one step and its accepted branch kept, and prints what a step takes and how far a token decoded by
 itself is from the same token in a chunk of its prompt.
 """
 from __future__ import annotations
@@ -26,28 +26,53 @@ class AttentionHalf:
     Rotary positions: `turns` (lutgemm_rope_frequencies of rot_dim), on the first rot_dim channels of a head (0: all), neighbours or halves
     paired, times `amplitude` (the one that goes with stretched frequencies).
 
+    norm: fp16 weights [hidden] of a root-mean-square norm in front of the first product, which `run` then takes after adding its
+    x to a residual stream.  adapters: lutgemm_adapters beside the first and the second product (either may be None);
+    `adapter_of` (int32 [seqs] on the device, -1: none) says whose sequences they are.  pages: of a pool that the sequences share, who take
+    them as they grow; 0: each has its own for `longest` positions.
+
     `place` says where the next step's tokens stand, `run` launches the step (and may be captured), `keep` advances the
-    lengths by all of the step's tokens, or by those of a drafted tree that were accepted."""
+    lengths by all of the step's tokens, or by those of a drafted tree that were accepted.  `advance` is a step of one token of every
+    sequence with all of that on the device, for a graph to replay; `advanced` tells the host afterwards how many were."""
 
     def __init__(self, qkv, out, hidden, heads, kv_heads, head_dim, seqs, longest, q=3, g=128, kv_bits=8, kv_group=0, page=64,
-                 turns=None, rot_dim=0, neighbours=False, amplitude=1.0):
+                 turns=None, rot_dim=0, neighbours=False, amplitude=1.0, norm=None, eps=1e-5, adapters=(None, None), pages=0):
         import torch
         self.torch, self.weights, self.hidden, self.heads, self.kv_heads, self.dim = torch, (qkv, out), hidden, heads, kv_heads, head_dim
         self.q, self.g, self.seqs = q, g, seqs
         self.row = (heads + 2 * kv_heads) * head_dim
-        pages = -(-(longest + MOST_ROWS) // page)
-        self.pool = torch.empty(L.lutgemm_kv_pool_bytes(seqs * pages, page, kv_heads, head_dim, kv_bits, kv_group), dtype=torch.uint8,
+        width = -(-(longest + MOST_ROWS) // page)
+        held = pages or seqs * width
+        self.pool = torch.empty(L.lutgemm_kv_pool_bytes(held, page, kv_heads, head_dim, kv_bits, kv_group), dtype=torch.uint8,
                                 device="cuda")
-        self.cache = L.lutgemm_kv_cache(self.pool, seqs * pages, page, kv_heads, head_dim, kv_bits, kv_group)
-        self.table = torch.arange(seqs * pages, dtype=torch.int32, device="cuda").view(seqs, pages)
+        self.cache = L.lutgemm_kv_cache(self.pool, held, page, kv_heads, head_dim, kv_bits, kv_group)
+        self.page, self.shared = page, bool(pages)
+        if self.shared:
+            self.table = torch.empty(seqs, width, dtype=torch.int32, device="cuda")
+            self.free, self.free_count, self.owned = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (pages, 1, seqs))
+            self.pages = L.lutgemm_kv_pages(self.free, self.free_count, self.owned, self.table, pages, page, seqs, width)
+            L.lutgemm_kv_pages_init(self.pages, self._stream())
+            self.taken, self.left = [0] * seqs, pages          # the host's count of them
+            self.fresh = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+        else:
+            self.table = torch.arange(seqs * width, dtype=torch.int32, device="cuda").view(seqs, width)
         self.longest = longest
+        self.norm, self.eps, self.adapters = norm, float(eps), tuple(adapters)
+        for a, (m, n) in zip(self.adapters, self.shapes()):
+            if a is not None and (a.m, a.n) != (m, n):
+                raise ValueError(f"adapters beside a {m} x {n} product are not {a.m} x {a.n}")
+        if norm is not None and (norm.shape != (hidden,) or norm.dtype != torch.float16 or not norm.is_contiguous()):
+            raise ValueError(f"a norm has {hidden} fp16 weights")
+        self.owner = torch.zeros(MOST_ROWS, dtype=torch.int32, device="cuda")
+        self.adapter_of = torch.zeros(seqs, dtype=torch.int32, device="cuda") - 1
+        self.normed = torch.empty(MOST_ROWS, hidden, dtype=torch.float16, device="cuda")
         self.rot_dim, self.amplitude = rot_dim or head_dim, float(amplitude)
         self.rope_flags = L.LUTGEMM_Y_F16 | (L.LUTGEMM_ROPE_NEIGHBOURS if neighbours else 0)
         turns = L.lutgemm_rope_frequencies(self.rot_dim) if turns is None else turns
         if len(turns) * 2 != self.rot_dim:
             raise ValueError(f"{self.rot_dim} channels are turned by {self.rot_dim // 2} frequencies, not {len(turns)}")
         self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
-        self.lengths = [0] * seqs
+        self.lengths, self.counts = [0] * seqs, None
         self.past = torch.zeros(seqs, dtype=torch.int32, device="cuda")
         self.first = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
         self.positions = torch.zeros(MOST_ROWS, dtype=torch.int32, device="cuda")
@@ -55,11 +80,12 @@ class AttentionHalf:
         self.rows = torch.zeros(MOST_ROWS, dtype=torch.int32, device="cuda")
         self.qkv = torch.empty(MOST_ROWS, self.row, dtype=torch.float16, device="cuda")
         self.mixed = torch.empty(MOST_ROWS, heads * head_dim, dtype=torch.float16, device="cuda")
-        self.step = L.lutgemm_kv_step(self.first, self.past, self.table, seqs, pages, MOST_ROWS, MOST_ROWS)
+        self.step = L.lutgemm_kv_step(self.first, self.past, self.table, seqs, width, MOST_ROWS, MOST_ROWS)
         # one workspace for all of it: for every number of tokens, as attention's need does not grow with them (where more rows make another
         # plan there may be fewer splits)
         self.ws_bytes = max([L.lutgemm_workspace_bytes(m, n, q, g, 8, b) for m, n in self.shapes() for b in range(1, MOST_ROWS + 1)] +
-                            [L.lutgemm_attention_workspace_bytes(self.cache, self._step(t, t), heads, longest) for t in range(1, MOST_ROWS + 1)])
+                            [L.lutgemm_attention_workspace_bytes(self.cache, self._step(t, t), heads, longest) for t in range(1, MOST_ROWS + 1)] +
+                            [L.lutgemm_adapt_workspace_bytes(a, t) for a in self.adapters if a is not None for t in range(1, MOST_ROWS + 1)])
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device="cuda")
         L.lutgemm_workspace_init(self.ws, self.ws_bytes, self._stream())
 
@@ -86,6 +112,11 @@ class AttentionHalf:
             raise ValueError("a step has a depth for every token, by sequences")
         if mask is not None and len(mask) != sum(counts):
             raise ValueError("a step has a mask word for every token")
+        needed = [0] * self.seqs
+        if self.shared:
+            needed = [max(0, -(-(n + c) // self.page) - t) if c else 0 for n, c, t in zip(self.lengths, counts, self.taken)]
+            if sum(needed) > self.left:
+                raise ValueError(f"a step needs {sum(needed)} pages more, of {self.left} that are free")
         self.counts = list(counts)
         self._set(self.first, np.concatenate([[0], np.cumsum(counts)]), np.int32)
         self._set(self.past, self.lengths, np.int32)
@@ -94,7 +125,13 @@ class AttentionHalf:
         self.masked = mask is not None
         if self.masked:
             self._set(self.mask, np.array(mask, dtype=np.uint64).view(np.int64), np.int64)
+        self._set(self.owner, np.repeat(np.arange(self.seqs), counts), np.int32)
         self.step = self._step(sum(counts), max(counts))
+        if self.shared:
+            self._set(self.fresh, counts, np.int32)
+            L.lutgemm_kv_place(self.pages, self.past, self.fresh, sum(counts), max(counts), self.first, None, None, None, self._stream())
+            self.taken = [t + n for t, n in zip(self.taken, needed)]
+            self.left -= sum(needed)
 
     def _product(self, weights, x, y, m, n, batch):
         bits, alpha, z = weights
@@ -103,15 +140,30 @@ class AttentionHalf:
         else:
             L.lutgemm_gemm(x, bits, alpha, z, y, self.q, self.g, 8, m, n, batch, L.LUTGEMM_Y_F16, self.ws, self.ws_bytes, self._stream())
 
-    def run(self, x, y):
-        """x, y: fp16 [tokens][hidden], contiguous.  Five calls on the current stream; nothing is allocated."""
+    def _adapt(self, adapters, x, y, tokens):
+        if adapters is not None:
+            L.lutgemm_adapt(x, y, adapters, self.adapter_of, self.owner, y, tokens, self.seqs, adapters.n, adapters.m, adapters.m, L.LUTGEMM_Y_F16, self.ws,
+                            self.ws_bytes, self._stream())
+
+    def run(self, x, y, residual=None):
+        """x, y: fp16 [tokens][hidden], contiguous.  residual (with a norm): the stream's rows, fp16 or fp32, to which x is added before its
+        norm.  Five to eight calls on the current stream; nothing is allocated."""
         tokens, stream = self.step.tokens, self._stream()
         for rows in (x, y):
             if rows.shape != (tokens, self.hidden) or rows.dtype != self.torch.float16 or not rows.is_contiguous():
                 raise ValueError(f"a step of {tokens} tokens takes and gives contiguous fp16 rows [{tokens}][{self.hidden}]")
+        if residual is not None and (self.norm is None or residual.shape != (tokens, self.hidden) or not residual.is_contiguous() or
+                                     residual.dtype not in (self.torch.float16, self.torch.float32)):
+            raise ValueError(f"a residual stream of {tokens} tokens is contiguous fp16 or fp32 rows [{tokens}][{self.hidden}], and a norm's")
         (m, n), (hidden, mixed) = self.shapes()
         queries = self.heads * self.dim
+        if self.norm is not None:
+            wide = residual is not None and residual.dtype == self.torch.float32
+            L.lutgemm_rms_norm(x, residual, self.norm, residual, self.normed, None, tokens, hidden, 0, hidden, hidden, hidden, self.eps,
+                               L.LUTGEMM_Y_F16 | (L.LUTGEMM_NORM_STREAM_F32 if wide else 0), stream)
+            x = self.normed
         self._product(self.weights[0], x, self.qkv, m, n, tokens)
+        self._adapt(self.adapters[0], x, self.qkv, tokens)
         L.lutgemm_rope(self.qkv, self.qkv, self.positions, self.turns, tokens, self.heads + self.kv_heads, self.dim, self.rot_dim,
                        self.row, self.row, self.amplitude, self.rope_flags, stream)
         keys, values = self.qkv[:, queries:], self.qkv[:, queries + self.kv_heads * self.dim:]
@@ -119,9 +171,36 @@ class AttentionHalf:
         L.lutgemm_attention(self.qkv, self.mask if self.masked else None, self.cache, self.step, self.mixed, self.heads, self.row, mixed,
                             1.0 / math.sqrt(self.dim), self.longest, self.ws, self.ws_bytes, stream)
         self._product(self.weights[1], self.mixed, y, hidden, mixed, tokens)
+        self._adapt(self.adapters[1], self.mixed, y, tokens)
+
+    def advance(self, x, y, residual=None):
+        """One token of every sequence, x [seqs][hidden]: placed, run, and its lengths advanced, all on the device, so that a captured call can be
+        replayed, as long as no sequence grows beyond `longest`.  A sequence that finds no page (and those behind it) waits: its rows of y and
+        residual mean nothing, its length stays.  The host learns of it by `advanced`."""
+        if not self.shared:
+            raise ValueError("sequences that advance on the device share their pages")
+        if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
+            raise ValueError(f"up to {MOST_ROWS} sequences advance, up to a length of {self.longest}")
+        self.masked, self.counts = False, None
+        self.step = self._step(self.seqs, 1)
+        self.fresh.fill_(1)
+        L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, 1, self.first, self.positions, self.owner, None, self._stream())
+        self.run(x, y, residual)
+        self.past.add_(self.first[1:] - self.first[:-1])
+
+    def advanced(self):
+        """What the device has made of the lengths since the last `place` or `advanced`; waits for it."""
+        self.lengths = self.past.tolist()
+        self.taken = self.owned.tolist()
+        self.left = int(self.free_count)
+        if max(self.lengths) > self.longest:
+            raise ValueError(f"a sequence has grown beyond {self.longest}")
+        return self.lengths
 
     def keep(self, accepted=None):
         """The step's tokens become the past; accepted: of each sequence which of its tokens (ascending) do, next to each other."""
+        if self.counts is None:
+            raise ValueError("steps that `place` has placed are kept")
         if accepted is None:
             kept = self.counts
         else:
@@ -139,6 +218,22 @@ class AttentionHalf:
                 keys, values = self.qkv[:, queries:], self.qkv[:, queries + self.kv_heads * self.dim:]
                 L.lutgemm_kv_write(keys, values, self.rows, self.cache, self._step(sum(kept), max(kept)), self.row, self.row, self._stream())
         self.lengths = [n + k for n, k in zip(self.lengths, kept)]
+        if self.shared:
+            self._set(self.past, self.lengths, np.int32)
+            self._trim(self.lengths)
+
+    def _trim(self, lengths):
+        L.lutgemm_kv_trim(self.pages, self.past, self._stream())
+        back = [max(0, t - -(-n // self.page)) for t, n in zip(self.taken, lengths)]
+        self.taken = [t - b for t, b in zip(self.taken, back)]
+        self.left += sum(back)
+
+    def end(self, seq):
+        """Sequence `seq` is over: its pages are free, and the next tokens are a new one's first."""
+        self.lengths[seq] = 0
+        if self.shared:
+            self._set(self.past, self.lengths, np.int32)
+            self._trim(self.lengths)
 
     def fill(self, x, y):
         """A prompt of every sequence, x [seqs][length][hidden], in chunks; y: their outputs."""
@@ -164,6 +259,15 @@ def random_layer(hidden, heads, kv_heads, head_dim, q=3, g=128, seed=0):
     return packed
 
 
+def random_adapters(m, n, count, rank, seed=0):
+    """Low-rank adapters beside an m x n product, of about a tenth of its outputs."""
+    import torch
+    rng = np.random.default_rng(seed)
+    down = torch.from_numpy((rng.standard_normal((count, rank, n)) / math.sqrt(n)).astype(np.float16)).cuda()
+    up = torch.from_numpy((0.1 * rng.standard_normal((count, m, rank)) / math.sqrt(rank)).astype(np.float16)).cuda()
+    return L.lutgemm_adapters(down, up, None, None, m, n, count, rank)
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description="decode with one layer's attention half")
     ap.add_argument("--hidden", type=int, default=5120)
@@ -175,6 +279,8 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=64)
     ap.add_argument("--kv-bits", type=int, choices=[4, 8, 16], default=8)
     ap.add_argument("--kv-group", type=int, default=0)
+    ap.add_argument("--adapters", type=int, default=3, help="low-rank adapters that the sequences have in turn; 0: none")
+    ap.add_argument("--rank", type=int, default=16, help="their rank, a multiple of 8")
     args = ap.parse_args(argv)
 
     import torch
@@ -186,13 +292,16 @@ def main(argv=None):
         print(f"decode: 1 to {MOST_ROWS} sequences, a prompt and steps", file=sys.stderr)
         return 2
     qkv, out = random_layer(args.hidden, args.heads, args.kv_heads, args.head_dim)
-    longest = args.prompt + args.steps + MOST_ROWS + 8
-
-    def layer():
-        return AttentionHalf(qkv, out, args.hidden, args.heads, args.kv_heads, args.head_dim, args.seqs, longest, kv_bits=args.kv_bits,
-                             kv_group=args.kv_group)
-
-    half = layer()
+    longest, page = args.prompt + args.steps + MOST_ROWS + 8, 64
+    norm = (1 + 0.1 * torch.randn(args.hidden, device="cuda")).half()
+    shapes = ((args.heads + 2 * args.kv_heads) * args.head_dim, args.hidden), (args.hidden, args.heads * args.head_dim)
+    adapters = [random_adapters(m, n, args.adapters, args.rank, seed=k) if args.adapters else None for k, (m, n) in enumerate(shapes)]
+    # (pages for every sequence's prompt and steps, and for one's drafted tree)
+    pages = args.seqs * -(-(args.prompt + args.steps) // page) + -(-MOST_ROWS // page)
+    half = AttentionHalf(qkv, out, args.hidden, args.heads, args.kv_heads, args.head_dim, args.seqs, longest, kv_bits=args.kv_bits, kv_group=args.kv_group,
+                         page=page, norm=norm, adapters=adapters, pages=pages)
+    if args.adapters:
+        half.adapter_of.copy_(torch.arange(args.seqs) % args.adapters)
     x = torch.randn(args.seqs, args.prompt, args.hidden, device="cuda").half()
     y = torch.empty_like(x)
     half.fill(x, y)
@@ -206,24 +315,23 @@ def main(argv=None):
     apart = ((alone - y[:, -1]).float().norm() / y[:, -1].float().norm()).item()
     print(f"{args.seqs} prompts of {args.prompt}: the last token by itself and in its chunk differ by {apart:.1e} of their norm")
 
-    # Decode: one step captured, lengths and positions advanced within it.
+    # Decode: one step captured; its tokens are placed, its pages taken and its lengths advanced within it.
     token, result = torch.randn(args.seqs, args.hidden, device="cuda").half(), torch.empty(args.seqs, args.hidden, dtype=torch.float16, device="cuda")
-    half.place([1] * args.seqs)
+    stream = torch.zeros(args.seqs, args.hidden, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):
-        half.run(token, result)
-        half.past.add_(1)
-        half.positions[:args.seqs].add_(1)
+        half.advance(token, result, stream)
+    half._set(half.past, half.lengths, np.int32)
     begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     begin.record()
     for _ in range(args.steps):
         graph.replay()
     end.record()
     torch.cuda.synchronize()
-    half.lengths = [n + args.steps for n in half.lengths]
-    print(f"{args.steps} decode steps of {args.seqs} tokens: {begin.elapsed_time(end) * 1e3 / args.steps:.1f} us a step")
+    half.advanced()
+    print(f"{args.steps} decode steps of {args.seqs} tokens: {begin.elapsed_time(end) * 1e3 / args.steps:.1f} us a step, {half.left} of {pages} pages left")
 
     # A drafted tree for the first sequence: two roots, the second with two children; the branch 1, 3 is accepted.
     depths, seen, branch = [0, 0, 1, 1], [0b0001, 0b0010, 0b0110, 0b1010], [1, 3]
