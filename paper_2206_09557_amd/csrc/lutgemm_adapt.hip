@@ -3,12 +3,14 @@
 //
 // Tokens with the same adapter are taken together, up to TILE of them, so that its A and B are read once for them: of up to 64 tokens
 // every wavefront finds the tiles by itself, from a ballot over the bits of their adapters; of more a kernel of one workgroup sorts them
-// first.  Then two products on the 16 x 16 x 32 matrix instructions, transposed (a lane owns a token):
-//     H^T (ranks x tokens) = A (ranks x n) X^T,      Y^T (m x tokens) = B (m x ranks) H^T
-// Both stream A and B, which is what bounds a decode step (2 r (n + m) bytes an adapter).  n is shared out among workgroups; their
-// sums meet where the second product reads them, in an order that the sizes decide.  H stays fp32 there, and meets B as two fp16 numbers
-// (22 bits) of a power of two that the token's largest decides: rounded to one, it would add as much error as the
-// result's own rounding to fp16, and more than that of fp32 results.
+// first.  Then two products on the 16 x 16 x 32 matrix instructions:
+//     H^T (ranks x tokens) = A (ranks x n) X^T,      Y (tokens x m) = H B^T (B m x ranks)
+// A decode step streams A and B (2 r (n + m) bytes an adapter), a prompt x, base and y; the time is that and two launches, each with a chain of
+// loads before it streams: adapters -> A and x -> sums, adapters -> sums of all parts -> H.  n is shared out among workgroups; their
+// sums are added up in an order that the sizes decide, by each workgroup of the second product or, of more than 64 tokens, once.  H stays fp32 until
+// then, and meets B as two fp16 numbers (22 bits) of a power of two that the token's largest decides: rounded to one, it would add as much
+// error as the result's own rounding to fp16, and more than that of fp32 results.  Measured: 32 adapters of rank 16 beside 36864 x 12288, one
+// token each, 56 MB: 6 + 12.3 us; three of up to 64 beside 12288 x 5120, 4096 tokens, 236 MB: sorting 7.5, products 19 and 52, joining 5.6.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -20,7 +22,6 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
-typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
 struct AdaptParams {
@@ -56,7 +57,7 @@ __device__ __forceinline__ int adapter_of(const AdaptParams& p, int token) {
 
 // A tile of up to `most` tokens: its adapter, how many tokens it has (0: there is no such tile, or nothing to do for it), which ones (of the workgroup, in LDS).
 struct Tile {
-  int adapter, tokens, rank;
+  int adapter, tokens, rank;   // (the rank as rank_of finds it, which is one more trip to memory)
 };
 __device__ __forceinline__ Tile tile_of(const AdaptParams& p, int number, int most, bool copies, int* token) {
   Tile t = {p.count, 0, 0};
@@ -89,9 +90,11 @@ __device__ __forceinline__ Tile tile_of(const AdaptParams& p, int number, int mo
     if ((int)threadIdx.x < t.tokens) token[threadIdx.x] = mine;
   }
   if (t.adapter >= p.count && !copies) t.tokens = 0;
-  if (t.adapter < p.count) t.rank = p.ranks ? min(max(p.ranks[t.adapter], 0), p.rank) : p.rank;
   __syncthreads();
   return t;
+}
+__device__ __forceinline__ int rank_of(const AdaptParams& p, const Tile& t) {
+  return t.adapter >= p.count ? 0 : (p.ranks ? min(max(p.ranks[t.adapter], 0), p.rank) : p.rank);
 }
 
 // Sorts the tokens by adapter, each adapter's in their order, and cuts them into tiles.  One workgroup; a wavefront has a stretch of the
@@ -221,7 +224,7 @@ __device__ __forceinline__ void split_h(int part, int each, int ranks, Value val
 
 // H of a tile, for a part of the columns and RANKS of its ranks.  Rows of x and A pass through LDS, CHUNK columns at
 // a time, so that a wavefront reads them a kilobyte (or two halves) at a time: as matrix operands, straight from memory, 16 neighbouring lanes
-// would touch 16 rows, which takes longer (4096 tokens of 5120 columns, rank 64: XX to XX us).  The next columns are on
+// would touch 16 rows, which takes longer (4096 tokens of 5120 columns, rank 64: 24 to 27 us so, 19 through LDS).  The next columns are on
 // their way meanwhile.  Every wavefront has some of a chunk's steps of 32 columns, for all tokens and RANKS; their sums meet in LDS.
 template <int NT, int RANKS, int CHUNK>
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParams p) {
@@ -232,9 +235,11 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParam
   __shared__ int token[TILE];
   __shared__ __attribute__((aligned(16))) char shared[OPERANDS > SUMS ? OPERANDS : SUMS];
   _Float16* rows = reinterpret_cast<_Float16*>(shared);
-  const Tile tile = tile_of(p, blockIdx.y, TILE, false, token);
+  Tile tile = tile_of(p, blockIdx.y, TILE, false, token);
+  if (tile.tokens == 0) return;
+  tile.rank = rank_of(p, tile);
   const int first_rank = blockIdx.z * RANKS, ranks = min(tile.rank - first_rank, RANKS);
-  if (tile.tokens <= 0 || ranks <= 0) return;
+  if (ranks <= 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, four = lane >> 4;
   const int64_t begin = (int64_t)blockIdx.x * p.part, end = min(begin + p.part, p.n);
   // Row i of LDS: token i, or rank i - TILE.  What there is none of is a row of zeros.
@@ -299,8 +304,8 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_down_kernel(AdaptParam
   }
 }
 
-// What the first product's parts have of a tile's tokens from `first` on, added up and scaled: h [token][rank] in LDS,
-// zeros beyond the adapter's rank.
+// What the first product's parts have of `tokens` of a tile (`from`: the first part's), added up and scaled: h [token][rank] in LDS, zeros
+// beyond the adapter's rank.
 __device__ __forceinline__ void add_parts(const AdaptParams& p, const Tile& tile, const float* from, int tokens, float* h) {
   __shared__ __attribute__((aligned(16))) float4v meet[kThreads];
   const int tid = threadIdx.x, items = tokens * p.rank / 4;
@@ -339,15 +344,17 @@ __device__ __forceinline__ void add_parts(const AdaptParams& p, const Tile& tile
   __syncthreads();
 }
 
-// Of more than a few tokens this is done once for all workgroups of the second product (which otherwise spend a third of their time
-// on it: 4096 tokens, 5120 -> 12288, rank 64, three parts 78 us, 54 so): 16 tokens of a tile, high and low numbers and powers to memory.
+// Of more than 64 tokens this is done once for all workgroups of the second product (which otherwise spend a third of their time
+// on it: 4096 tokens, 5120 -> 12288, rank 64, three parts: 78 us, 54 without): 16 tokens of a tile, high and low numbers and powers to memory.
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_join_kernel(AdaptParams p, int tile_tokens, int pad) {
   __shared__ float h[16 * kMostRank];
   __shared__ int token[64];
   const int first = 16 * blockIdx.x;
-  const Tile tile = tile_of(p, blockIdx.y, tile_tokens, false, token);
+  Tile tile = tile_of(p, blockIdx.y, tile_tokens, false, token);
   const int tokens = min(tile.tokens - first, 16);
-  if (tokens <= 0 || tile.rank == 0) return;
+  if (tokens <= 0) return;
+  tile.rank = rank_of(p, tile);
+  if (tile.rank == 0) return;
   add_parts(p, tile, p.sums + ((int64_t)blockIdx.y * tile_tokens + first) * p.rank, tokens, h);
   const int t = threadIdx.x / 16;
   auto value = [&](int r) { return t < tokens && r < tile.rank ? h[t * p.rank + r] : 0.0f; };
@@ -564,9 +571,19 @@ __global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= 32 && sizeof(Y) ==
   __shared__ __attribute__((aligned(16))) Target target[TILE];
   Joined<TILE, U::PAD> joined;
   joined.ask(p);
-  const Tile tile = tile_of(p, blockIdx.y, TILE, p.copies, token);
+  Tile tile = tile_of(p, blockIdx.y, TILE, p.copies, token);
   if (tile.tokens == 0) return;
   const int64_t first = (int64_t)blockIdx.x * p.rows, last = min(first + p.rows, p.m);
+  _Float16* high = reinterpret_cast<_Float16*>(shared);
+  _Float16* low = high + TILE * U::PITCH;
+  _Float16* stages = low + TILE * U::PITCH;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int eights = p.rank / 8;
+  U u{p, tile, high, low, p.up + (int64_t)min(tile.adapter, p.count - 1) * p.m * p.rank, stages + wave * U::ROWS * U::STAGE, target,
+      eights, (uint32_t)((((uint64_t)1 << 32) + eights - 1) / eights), lane, lane & 15, lane >> 4, {}};
+  const int64_t m0 = first + U::ROWS * wave;
+  if (U::AHEAD) u.fetch(min(m0, last - 1));
+  tile.rank = rank_of(p, tile);
   if (tile.rank == 0) {                          // nothing is added
     typedef typename U::Run Run;
     constexpr int kEach = WIDE ? 4 : 1, kTogether = 8;       // rows of m a thread, tokens on their way at a time
@@ -594,15 +611,6 @@ __global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= 32 && sizeof(Y) ==
     }
     return;
   }
-  _Float16* high = reinterpret_cast<_Float16*>(shared);
-  _Float16* low = high + TILE * U::PITCH;
-  _Float16* stages = low + TILE * U::PITCH;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int eights = p.rank / 8;
-  U u{p, tile, high, low, p.up + (int64_t)tile.adapter * p.m * p.rank, stages + wave * U::ROWS * U::STAGE, target,
-      eights, (uint32_t)((((uint64_t)1 << 32) + eights - 1) / eights), lane, lane & 15, lane >> 4, {}};
-  const int64_t m0 = first + U::ROWS * wave;
-  if (U::AHEAD) u.fetch(min(m0, last - 1));
   if (threadIdx.x < TILE) {
     const int64_t t = token[min((int)threadIdx.x, tile.tokens - 1)];
     target[threadIdx.x].base = t * p.base_stride;

@@ -164,6 +164,41 @@ def test_large_and_special_values(tokens):
     assert not np.isfinite(y[[1, 4]]).any() and not np.isfinite(y[of == 2]).any()
 
 
+@pytest.mark.parametrize("tokens,count,spread", [(8192, 3, "any"), (9000, 5, "any"), (9000, 1, "one"), (20000, 40, "each")])
+def test_many_tokens(tokens, count, spread):
+    """More than the sorting keeps in registers, and as many: small products, in numpy."""
+    rng = np.random.default_rng(tokens + count)
+    m, n, rank = 24, 16, 8
+    of = rng.integers(-1, count + 1, tokens) if spread == "any" else np.arange(tokens) % count if spread == "each" else np.zeros(tokens, int)
+    print("case many", tokens, count, spread, flush=True)
+    a = Set(rng, m, n, count, rank)
+    x, base = rng.standard_normal((tokens, n)).astype(np.float16), rng.standard_normal((tokens, m)).astype(np.float32)
+    y = _run(a, x, base, of, f32=True)
+    live = (of >= 0) & (of < count)
+    pick = np.where(live, of, 0)
+    h = np.einsum("trn,tn->tr", a.down.astype(np.float64)[pick], x.astype(np.float64))
+    c = np.where(live, a.scales.astype(np.float64)[pick], 0.0)[:, None]
+    ref = base + c * np.einsum("tmr,tr->tm", a.up.astype(np.float64)[pick], h)
+    reach = c * np.einsum("tmr,trn,tn->tm", np.abs(a.up.astype(np.float64))[pick], np.abs(a.down.astype(np.float64))[pick], np.abs(x.astype(np.float64)))
+    mass = c * np.abs(a.up.astype(np.float64))[pick].sum(2) * np.abs(h).max(1)[:, None]
+    _check(y, ref, reach, mass, True, n, rank)
+    np.testing.assert_array_equal(y[~live], base[~live])
+
+
+def test_an_infinite_weight_stays_in_its_row():
+    """One row of B: its own results are no numbers, those of the others what they are without it (also of ranks that share an instruction)."""
+    torch = torch_cuda()
+    for rank in (8, 16, 32, 64, 128):
+        rng = np.random.default_rng(rank)
+        a = Set(rng, 200, 64, 1, rank, scales=False)
+        x, base = rng.standard_normal((5, 64)).astype(np.float16), rng.standard_normal((5, 200)).astype(np.float32)
+        before = _run(a, x, base, [0] * 5, f32=True)
+        a.d[1][0, 70, 1] = float("inf")
+        y = _run(a, x, base, [0] * 5, f32=True)
+        assert not np.isfinite(y[:, 70]).any()
+        np.testing.assert_array_equal(np.delete(y, 70, 1), np.delete(before, 70, 1))
+
+
 def test_the_same_from_run_to_run_and_beside_others():
     """Bitwise: again, on another stream, and for a token whose neighbours have other values."""
     torch = torch_cuda()
