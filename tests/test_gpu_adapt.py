@@ -239,6 +239,91 @@ def test_a_captured_call_is_replayed_with_other_adapters(tokens):
         _check(got.cpu().numpy(), ref, reach, mass, False, n, rank)
 
 
+def test_offsets_beyond_32_bits():
+    """Rows of base and y 2^31 bytes apart; an adapter that begins 2^32 bytes and more into the store of B."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(2)
+    m, n, rank = 260, 64, 16
+    a = Set(rng, m, n, 2, rank)
+    x = rng.standard_normal((4, n)).astype(np.float16)
+    base = rng.standard_normal((4, m)).astype(np.float16)
+    stride = (1 << 30) + 8
+    d_base, d_y = (torch.empty(3 * stride + m, dtype=torch.float16, device="cuda") for _ in range(2))
+    for t in range(4):
+        d_base[t * stride:t * stride + m] = torch.from_numpy(base[t]).cuda()
+    of = torch.tensor([0, 1, -1, 1], dtype=torch.int32, device="cuda")
+    ws = make_workspace(L.lutgemm_adapt_workspace_bytes(a.handle, 4))
+    stream = torch.cuda.current_stream().cuda_stream
+    L.lutgemm_adapt(torch.from_numpy(x).cuda(), d_base, a.handle, of, None, d_y, 4, 0, n, stride, stride, 0, ws, ws.numel(), stream)
+    torch.cuda.synchronize()
+    y = np.stack([d_y[t * stride:t * stride + m].cpu().numpy() for t in range(4)])
+    _check(y, *S.adapt(x, base, a.down, a.up, None, a.scales, of.tolist()), False, n, rank)
+    del d_base, d_y
+    m, rank, count = 1 << 20, 256, 9               # 2^29 bytes an adapter
+    down = torch.zeros(count, rank, 8, dtype=torch.float16, device="cuda")
+    up = torch.empty(count, m, rank, dtype=torch.float16, device="cuda")
+    down[8] = torch.randn(rank, 8, device="cuda").half()
+    up[8] = torch.randn(m, rank, device="cuda", dtype=torch.float16)
+    handle = L.lutgemm_adapters(down, up, None, None, m, 8, count, rank)
+    x, zero, y = torch.randn(1, 8, device="cuda").half(), torch.zeros(1, m, device="cuda"), torch.empty(1, m, device="cuda")
+    ws = make_workspace(L.lutgemm_adapt_workspace_bytes(handle, 1))
+    L.lutgemm_adapt(x, zero, handle, torch.tensor([8], dtype=torch.int32, device="cuda"), None, y, 1, 0, 8, m, m, L.LUTGEMM_Y_F32, ws, ws.numel(), stream)
+    torch.cuda.synchronize()
+    some = np.r_[0:100, m // 2:m // 2 + 100, m - 100:m]
+    h_up = up[8][torch.from_numpy(some).cuda()].cpu().numpy()[None]
+    ref, reach, mass = S.adapt(x.cpu().numpy(), np.zeros((1, len(some)), np.float32), down[8:].cpu().numpy(), h_up, None, None, [0])
+    _check(y[:, torch.from_numpy(some).cuda()].cpu().numpy(), ref, reach, mass, True, 8, rank)
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured calls of different sizes and a product, in turn on one workspace, with the program's own calls between the replays."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(12)
+    m, n = 512, 640
+    a = Set(rng, m, n, 4, 16)
+    W = (rng.standard_normal((m, n)) * 0.05).astype(np.float16)
+    bits, alpha, _ = L.lutgemm_pack_bcq(W, 3, 128)
+    d_bits, d_alpha = torch.from_numpy(bits).cuda(), torch.from_numpy(alpha.view(np.int16)).cuda()
+    nbytes = max(L.lutgemm_adapt_workspace_bytes(a.handle, 130), L.lutgemm_workspace_bytes(m, n, 3, 128, 8, 6))
+    ws = make_workspace(nbytes)
+    sets = []
+    for tokens in (6, 130):
+        x = torch.from_numpy(rng.standard_normal((tokens, n)).astype(np.float16)).cuda()
+        of = torch.from_numpy((np.arange(tokens) % 5 - 1).astype(np.int32)).cuda()
+        sets.append((tokens, x, torch.zeros(tokens, m, dtype=torch.float16, device="cuda"), of))
+
+    def call(k):
+        tokens, x, y, of = sets[k]
+        s = torch.cuda.current_stream().cuda_stream
+        if k == 0:
+            L.lutgemm_gemm(x, d_bits, d_alpha, None, y, 3, 128, 8, m, n, tokens, 0, ws, nbytes, s)
+        else:
+            y.zero_()
+        L.lutgemm_adapt(x, y, a.handle, of, None, y, tokens, 0, n, m, m, 0, ws, nbytes, s)
+
+    want = []
+    for k in range(2):
+        call(k)
+        torch.cuda.synchronize()
+        want.append(sets[k][2].clone())
+    graphs = []
+    for k in range(2):
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            call(k)
+        graphs.append(graph)
+    for turn in range(6):
+        for k in (0, 1, 1, 0):
+            sets[k][2].fill_(float("nan"))
+            graphs[k].replay()
+            if turn % 2:
+                torch.cuda.synchronize()
+            assert torch.equal(sets[k][2], want[k])
+            call(1 - k)
+            assert torch.equal(sets[1 - k][2], want[1 - k])
+
+
 def test_no_tokens():
     torch = torch_cuda()
     a = Set(np.random.default_rng(0), 32, 64, 2, 8)

@@ -184,6 +184,55 @@ def test_values_at_the_ends():
     assert (scales[2] == 0).all() == bool((np.abs(ref[2]).reshape(-1, 32).max(1) < 2.0 ** -100).all())
 
 
+def test_many_rows_and_far_ones():
+    """More rows than a grid's second side has; rows 2^28 elements apart, 2^32 bytes and more in all; large outputs in place."""
+    torch = torch_cuda()
+    x = torch.randn(70001, 16, device="cuda").half()
+    y = torch.empty_like(x)
+    _call(x, None, None, None, y, None, 70001, 16, 0, 16, 0, 16, 0)
+    _check_y(y.cpu().numpy(), S.rms_norm(x.cpu().numpy(), None, None, EPS)[1])
+    rng = np.random.default_rng(3)
+    n, stride = 136, 1 << 28
+    rows = rng.standard_normal((9, n)).astype(np.float16)
+    far = torch.empty(8 * stride + n, dtype=torch.float16, device="cuda")
+    for t in range(9):
+        far[t * stride:t * stride + n] = torch.from_numpy(rows[t]).cuda()
+    _call(far, None, None, None, far, None, 9, n, 0, stride, 0, stride, 0)
+    got = np.stack([far[t * stride:t * stride + n].cpu().numpy() for t in range(9)])
+    _check_y(got, S.rms_norm(rows, None, None, EPS)[1])
+    del far
+    x = rng.standard_normal((3000, 5120)).astype(np.float16)
+    r = rng.standard_normal((3000, 5120)).astype(np.float32)
+    d_x, d_r = _up(x), _up(r)
+    _call(d_x, d_r, None, d_r, d_x, None, 3000, 5120, 0, 5120, 5120, 5120, L.LUTGEMM_NORM_STREAM_F32)
+    few = [0, 1, 1499, 2999]
+    s, ref = S.rms_norm(x[few], r[few], None, EPS)
+    _check_y(d_x.cpu().numpy().reshape(3000, 5120)[few], ref)
+    _check_sum(d_r.cpu().numpy().reshape(3000, 5120)[few], s, True)
+
+
+def test_a_captured_norm_is_replayed():
+    torch = torch_cuda()
+    n = 1000
+    x, r = torch.randn(5, n, device="cuda").half(), torch.zeros(5, n, device="cuda")
+    codes, scales = torch.empty(5, n, dtype=torch.int8, device="cuda"), torch.empty(5, 1, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        L.lutgemm_rms_norm(x, r, None, r, codes, scales, 5, n, 0, n, n, n, EPS, L.LUTGEMM_NORM_STREAM_F32, torch.cuda.current_stream().cuda_stream)
+    total = np.zeros((5, n))
+    for _ in range(4):
+        x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        s, ref = S.rms_norm(x.cpu().numpy(), total.astype(np.float32), None, EPS)
+        _check_sum(r.cpu().numpy(), s, True)
+        steps = scales.cpu().numpy().astype(np.float64)
+        assert (np.abs(codes.cpu().numpy() * steps - ref) <= steps * (0.5 + 127 * 8 * 2.0 ** -24)).all()
+        total = r.cpu().numpy().astype(np.float64)
+
+
 def test_nothing_to_do_and_another_stream():
     torch = torch_cuda()
     n = 640
