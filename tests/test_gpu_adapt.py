@@ -103,6 +103,18 @@ def test_against_oracle(tokens, m, n, count, rank, f32):
         _case(tokens, m, n, count, rank, of, f32=f32)
 
 
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 48, 64, 72, 128, 136, 256])
+@pytest.mark.parametrize("tokens,count", [(64, 1), (60, 2), (70, 1), (200, 2), (141, 3)])
+def test_tiles_of_every_size(tokens, count, rank):
+    """16, 32 and 64 tokens to a tile, full, of up to four and of up to sixteen; rows of four elements and of any; results over base and beside it."""
+    for m, f32, in_place in ((340, False, False), (340, True, True), (1028, True, False), (341, False, True)):
+        tile = L.lutgemm_plan_adapt(L.lutgemm_adapters(16, 16, None, None, m, 264, count, rank), tokens)[0]
+        assert tile == (16 if rank > 128 else 64 if tokens // count >= 48 else 32)
+        for of in (np.arange(tokens) % count, np.where(np.arange(tokens) < 3, 0, -1), np.where(np.arange(tokens) < tile + 9, count - 1, -1)):
+            print("case tiles", tokens, count, rank, m, f32, in_place, flush=True)
+            _case(tokens, m, 264, count, rank, of, f32=f32, in_place=in_place)
+
+
 @pytest.mark.parametrize("tokens,count,rank", [(7, 5, 16), (40, 6, 64), (200, 9, 80), (90, 4, 256)])
 def test_ranks_of_every_kind(tokens, count, rank):
     """What the stores hold beyond a rank is NaN; an adapter of rank 0 adds nothing."""

@@ -87,6 +87,36 @@ def test_against_oracle(tokens, n, x_f32, stream_f32, gaps, offset, parts):
     np.testing.assert_array_equal(again.cpu().numpy(), d_y.cpu().numpy())
 
 
+@pytest.mark.parametrize("x_f32,stream_f32", [(False, False), (True, False), (False, True), (True, True)])
+def test_every_width(x_f32, stream_f32):
+    """Rows of every number of runs and threads, whole 16 bytes and not, few and many of them, to fp16 and to 8 bits."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(6 + x_f32 + 2 * stream_f32)
+    flags = (L.LUTGEMM_Y_F32 if x_f32 else 0) | (L.LUTGEMM_NORM_STREAM_F32 if stream_f32 else 0)
+    for n in (504, 512, 520, 1024, 1056, 2048, 4096, 4104, 6144, 6176, 8192, 8224, 12320, 16384, 16416, 24576, 24608, 32768):
+        for tokens, gap in ((3, 0), (3, 1), (1030, 0)):
+            if tokens * n > 1 << 24:
+                continue
+            print("case width", n, tokens, gap, x_f32, stream_f32, flush=True)
+            stride = n + gap
+            x, r = _rows(rng, tokens, n, stride, x_f32), _rows(rng, tokens, n, stride, stream_f32, 3.0)
+            d_x, d_r, d_y = _up(x), _up(r), _up(np.full((tokens, stride), MARK, np.float16))
+            few = np.unique([0, tokens // 2, tokens - 1])
+            s, ref = S.rms_norm(x[few, :n], r[few, :n], None, EPS)
+            _call(d_x, d_r, None, d_r, d_y, None, tokens, n, 0, stride, stride, stride, flags)
+            y = _down(d_y, tokens, stride)
+            _check_y(y[few, :n], ref)
+            assert (y[:, n:] == MARK).all()
+            _check_sum(_down(d_r, tokens, stride)[few, :n], s, stream_f32)
+            if n % 32:
+                continue
+            codes, scales = _up(np.full((tokens, stride), MARK, np.int8)), torch.empty(tokens, n // 32, device="cuda")
+            _call(d_x, _up(r), None, None, codes, scales, tokens, n, 32, stride, stride, stride, flags)
+            steps = scales.cpu().numpy()[few].repeat(32, 1).astype(np.float64)
+            y = _down(codes, tokens, stride)
+            assert (np.abs(y[few, :n] * steps - ref) <= steps * (0.5 + 127 * 8 * 2.0 ** -24)).all() and (y[:, n:] == MARK).all()
+
+
 @pytest.mark.parametrize("tokens,n,group,x_f32,stream_f32,gap,offset", [
     (1, 32, 32, False, False, 0, 0), (3, 96, 32, False, False, 0, 0), (2, 1, 0, False, False, 0, 0), (5, 77, 0, True, True, 3, 1), (4, 2048, 64, False, True, 0, 0),
     (509, 1024, 128, False, True, 0, 0), (2, 8192, 128, False, True, 8, 0), (3, 5120, 0, False, False, 0, 0), (2, 12288, 96, True, False, 0, 0),
