@@ -73,6 +73,7 @@ class AttentionHalf:
             raise ValueError(f"{self.rot_dim} channels are turned by {self.rot_dim // 2} frequencies, not {len(turns)}")
         self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
         self.lengths, self.counts = [0] * seqs, None
+        self.placed, self.known = False, True       # a step that `keep` has not ended; whether the host knows the lengths
         self.past = torch.zeros(seqs, dtype=torch.int32, device="cuda")
         self.first = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
         self.positions = torch.zeros(MOST_ROWS, dtype=torch.int32, device="cuda")
@@ -112,12 +113,14 @@ class AttentionHalf:
             raise ValueError("a step has a depth for every token, by sequences")
         if mask is not None and len(mask) != sum(counts):
             raise ValueError("a step has a mask word for every token")
+        if not self.known:
+            raise ValueError("the lengths have advanced on the device: `advanced` tells them")
         needed = [0] * self.seqs
         if self.shared:
             needed = [max(0, -(-(n + c) // self.page) - t) if c else 0 for n, c, t in zip(self.lengths, counts, self.taken)]
             if sum(needed) > self.left:
                 raise ValueError(f"a step needs {sum(needed)} pages more, of {self.left} that are free")
-        self.counts = list(counts)
+        self.counts, self.placed = list(counts), True
         self._set(self.first, np.concatenate([[0], np.cumsum(counts)]), np.int32)
         self._set(self.past, self.lengths, np.int32)
         below = [np.arange(c) for c in counts] if depths is None else [np.asarray(d) for d in depths]
@@ -181,7 +184,7 @@ class AttentionHalf:
             raise ValueError("sequences that advance on the device share their pages")
         if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
             raise ValueError(f"up to {MOST_ROWS} sequences advance, up to a length of {self.longest}")
-        self.masked, self.counts = False, None
+        self.masked, self.counts, self.placed, self.known = False, None, False, False
         self.step = self._step(self.seqs, 1)
         self.fresh.fill_(1)
         L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, 1, self.first, self.positions, self.owner, None, self._stream())
@@ -192,7 +195,7 @@ class AttentionHalf:
         """What the device has made of the lengths since the last `place` or `advanced`; waits for it."""
         self.lengths = self.past.tolist()
         self.taken = self.owned.tolist()
-        self.left = int(self.free_count)
+        self.left, self.known = int(self.free_count), True
         if max(self.lengths) > self.longest:
             raise ValueError(f"a sequence has grown beyond {self.longest}")
         return self.lengths
@@ -218,6 +221,7 @@ class AttentionHalf:
                 keys, values = self.qkv[:, queries:], self.qkv[:, queries + self.kv_heads * self.dim:]
                 L.lutgemm_kv_write(keys, values, self.rows, self.cache, self._step(sum(kept), max(kept)), self.row, self.row, self._stream())
         self.lengths = [n + k for n, k in zip(self.lengths, kept)]
+        self.placed = False
         if self.shared:
             self._set(self.past, self.lengths, np.int32)
             self._trim(self.lengths)
@@ -229,7 +233,9 @@ class AttentionHalf:
         self.left += sum(back)
 
     def end(self, seq):
-        """Sequence `seq` is over: its pages are free, and the next tokens are a new one's first."""
+        """Sequence `seq` is over, between two steps: its pages are free, and the next tokens are a new one's first."""
+        if self.placed or not self.known:
+            raise ValueError("a sequence ends after `keep`, or after `advanced`")
         self.lengths[seq] = 0
         if self.shared:
             self._set(self.past, self.lengths, np.int32)

@@ -124,11 +124,16 @@ def test_pages_that_run_out():
     one = torch.empty(3, D.HIDDEN, dtype=torch.float16, device="cuda")
     token = D._tokens(torch, 3, D.HIDDEN, seed=6)
     half.advance(D._up(torch, token), one)
+    for call in (lambda: half.place([1, 0, 0]), lambda: half.end(0)):       # the host does not know the lengths yet
+        with pytest.raises(ValueError):
+            call()
     assert half.advanced() == [33, 32, 32] and half.left == 0
     D._close(one[:1].cpu().numpy(), sv.reference(0, np.concatenate([x[0], token[:1]]))[32:])
     half.end(1)
     assert half.left == 1 and half.lengths == [33, 0, 32] and int(half.free_count) == 1
     half.place([1, 0, 1])
+    with pytest.raises(ValueError):
+        half.end(2)                                # its new token is not kept yet
     last = torch.empty(2, D.HIDDEN, dtype=torch.float16, device="cuda")
     more = D._tokens(torch, 2, D.HIDDEN, seed=7)
     half.run(D._up(torch, more), last)
