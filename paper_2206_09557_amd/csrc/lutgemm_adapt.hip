@@ -1,13 +1,13 @@
 // Low-rank adapters of many requests beside a product whose weights they share: y[t] = base[t] + c_a B_a (A_a x[t]), a the adapter of
 // token t.  include/lutgemm.h has the layouts.
 //
-// Tokens with the same adapter are taken together, up to TILE of them, so that its A and B are read once for them: of up to 64 tokens
-// every wavefront finds the tiles by itself, from a ballot over the bits of their adapters; of more a kernel of one workgroup sorts them
+// Tokens with the same adapter are taken together, up to TILE of them, so that its A and B are read once for them: of up to 256 tokens
+// every wavefront finds the tiles by itself, from ballots over the bits of their adapters; of more a kernel of one workgroup sorts them
 // first.  Then two products on the 16 x 16 x 32 matrix instructions:
 //     H^T (ranks x tokens) = A (ranks x n) X^T,      Y (tokens x m) = H B^T (B m x ranks)
 // A decode step streams A and B (2 r (n + m) bytes an adapter), a prompt x, base and y; the time is that and two launches, each with a chain of
 // loads before it streams: adapters -> A and x -> sums, adapters -> sums of all parts -> H.  n is shared out among workgroups; their
-// sums are added up in an order that the sizes decide, by each workgroup of the second product or, of more than 64 tokens, once.  H stays fp32 until
+// sums are added up in an order that the sizes decide, by each workgroup of the second product or, of tiles of 64 tokens or many tokens, once.  H stays fp32 until
 // then, and meets B as two fp16 numbers (22 bits) of a power of two that the token's largest decides: rounded to one, it would add as much
 // error as the result's own rounding to fp16, and more than that of fp32 results.  Measured: 32 adapters of rank 16 beside 36864 x 12288, one
 // token each, 56 MB: 6 + 12.3 us; three of up to 64 beside 12288 x 5120, 4096 tokens, 236 MB: sorting 7.5, products 19 and 52, joining 5.6.
@@ -59,29 +59,63 @@ __device__ __forceinline__ int adapter_of(const AdaptParams& p, int token) {
 struct Tile {
   int adapter, tokens, rank;   // (the rank as rank_of finds it, which is one more trip to memory)
 };
+// Among up to 64 RUNS tokens, token 64 u + lane in a lane's u-th place: the tiles are numbered by their first tokens.  Against sorting
+// first, beside 8192 x 8192: 65 tokens of eight adapters of rank 16 12.1 us against 15.8, 256 16.7 against 20.3; 64 to a tile, 128 tokens
+// 21.5 against 22.3, 256 23.6 against 23.4 (5120 x 5120: 21.3, 20.6), where the ballots of every workgroup are as long as the launch.
+template <int RUNS>
+__device__ __forceinline__ void find_tile(const AdaptParams& p, int number, int most, int* token, Tile* t) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  int mine[RUNS], rank[RUNS];
+  uint64_t same[RUNS][RUNS];                     // the tokens of run v that have the adapter of this lane's u-th
+#pragma unroll
+  for (int u = 0; u < RUNS; ++u) mine[u] = 64 * u + lane < p.tokens ? adapter_of(p, 64 * u + lane) : -1;
+#pragma unroll
+  for (int v = 0; v < RUNS; ++v) {
+    const uint64_t live = __ballot(mine[v] >= 0);
+#pragma unroll
+    for (int u = 0; u < RUNS; ++u) same[u][v] = live;
+  }
+  for (int bit = 1; bit <= p.count; bit *= 2) {
+#pragma unroll
+    for (int v = 0; v < RUNS; ++v) {
+      const uint64_t set = __ballot((mine[v] & bit) != 0);
+#pragma unroll
+      for (int u = 0; u < RUNS; ++u) same[u][v] &= (mine[u] & bit) != 0 ? set : ~set;
+    }
+  }
+  int before = 0;                                // tiles that begin in earlier runs
+#pragma unroll
+  for (int u = 0; u < RUNS; ++u) {
+    rank[u] = __popcll(same[u][u] & below);
+#pragma unroll
+    for (int v = 0; v < u; ++v) rank[u] += __popcll(same[u][v]);
+    const bool head = mine[u] >= 0 && (rank[u] & (most - 1)) == 0;
+    const uint64_t heads = __ballot(head), chosen = __ballot(head && before + __popcll(heads & below) == number);
+    before += __popcll(heads);
+    if (chosen != 0) {
+      const int first = __builtin_ctzll(chosen), from = __builtin_amdgcn_readlane(rank[u], first);
+      t->adapter = __builtin_amdgcn_readlane(mine[u], first);
+      t->rank = from;                            // (of the first token, till the members are known)
+      t->tokens = 1;
+    }
+  }
+  if (t->tokens == 0) return;
+  const int from = t->rank;
+  t->tokens = t->rank = 0;
+#pragma unroll
+  for (int u = 0; u < RUNS; ++u) {
+    const bool member = mine[u] == t->adapter && rank[u] >= from && rank[u] < from + most;
+    t->tokens += __popcll(__ballot(member));
+    if (threadIdx.x < 64 && member) token[rank[u] - from] = 64 * u + lane;
+  }
+}
 __device__ __forceinline__ Tile tile_of(const AdaptParams& p, int number, int most, bool copies, int* token) {
   Tile t = {p.count, 0, 0};
-  if (p.tokens <= kFewTokens) {
-    const int lane = threadIdx.x & 63;
-    const bool live = lane < p.tokens;
-    const int mine = live ? adapter_of(p, lane) : -1;
-    uint64_t same = __ballot(live);
-    for (int bit = 1; bit <= p.count; bit *= 2) {
-      const uint64_t set = __ballot((mine & bit) != 0);
-      same &= (mine & bit) != 0 ? set : ~set;
-    }
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    const int rank = __popcll(same & below);
-    const uint64_t heads = __ballot(live && (rank & (most - 1)) == 0);
-    const uint64_t chosen = __ballot(live && (rank & (most - 1)) == 0 && __popcll(heads & below) == number);
-    if (chosen != 0) {
-      const int head = __builtin_ctzll(chosen);
-      t.adapter = __builtin_amdgcn_readlane(mine, head);
-      const int from = __builtin_amdgcn_readlane(rank, head);
-      const bool member = live && mine == t.adapter && rank >= from && rank < from + most;
-      t.tokens = __popcll(__ballot(member));
-      if (threadIdx.x < 64 && member) token[rank - from] = lane;
-    }
+  if (p.tokens <= 64) {
+    find_tile<1>(p, number, most, token, &t);
+  } else if (p.tokens <= kFewTokens) {
+    find_tile<kFewTokens / 64>(p, number, most, token, &t);
   } else if (number < p.table[0]) {
     const int32_t* entry = p.table + 4 + 4 * number;
     const int mine = p.table[4 + 4 * p.tiles + number * most + min((int)threadIdx.x, most - 1)];       // (of places without a token anything)
@@ -344,7 +378,7 @@ __device__ __forceinline__ void add_parts(const AdaptParams& p, const Tile& tile
   __syncthreads();
 }
 
-// Of more than 64 tokens this is done once for all workgroups of the second product (which otherwise spend a third of their time
+// Of many tokens, or 64 to a tile, this is done once for all workgroups of the second product (which otherwise spend a third of their time
 // on it: 4096 tokens, 5120 -> 12288, rank 64, three parts: 78 us, 54 without): 16 tokens of a tile, high and low numbers and powers to memory.
 __global__ __launch_bounds__(kThreads) void lutgemm_adapt_join_kernel(AdaptParams p, int tile_tokens, int pad) {
   __shared__ float h[16 * kMostRank];
@@ -691,7 +725,7 @@ extern "C" int lutgemm_adapt(const void* x, const void* base, const lutgemm_adap
   p.scales = a.scales;
   p.table = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kCounterBytes);
   p.sums = reinterpret_cast<float*>(p.table + ints);
-  p.joined = tokens > kFewTokens ? p.sums + plan.parts * part_floats : nullptr;
+  p.joined = adapt_joins(plan, tokens) ? p.sums + plan.parts * part_floats : nullptr;
   p.x_stride = x_stride;
   p.base_stride = base_stride;
   p.y_stride = y_stride;

@@ -16,7 +16,7 @@ constexpr int64_t kCacheBytes = 32 << 20;   // of the L2 caches
 constexpr int kMostAdapters = 1024;
 constexpr int kMostRank = 256;
 constexpr int kMostAdapted = 1 << 16;      // tokens of a call
-constexpr int kFewTokens = 64;             // as many as a wavefront groups by itself
+constexpr int kFewTokens = 256;            // as many as a wavefront groups by itself
 constexpr int kRankBlock = 64;             // ranks of a workgroup of the first product
 
 struct AdaptPlan {
@@ -30,13 +30,16 @@ AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens);
 int check_adapters(const lutgemm_adapters* a, int tokens);
 
 // The workspace behind the counters: tiles' table and their tokens (where there are more tokens than a wavefront groups), then
-// the first product's sums, [part][tile][token of the tile][rank], and for as many tokens [tile] high and low numbers [token][rank] and a power for each token.
+// the first product's sums, [part][tile][token of the tile][rank], and where these are joined [tile] high and low numbers [token][rank] and a power for each token.
 inline int64_t adapt_table_ints(const AdaptPlan& p, int tokens) { return tokens <= kFewTokens ? 0 : 4 + (4 + (int64_t)p.tile) * p.tiles; }
 inline int64_t adapt_part_floats(const AdaptPlan& p, int rank) { return (int64_t)p.tiles * p.tile * rank; }
+// Whether the first product's parts are added up once, by a kernel of its own.  Beside 8192 x 8192: 256 tokens of one adapter of rank 64,
+// 64 to a tile, 23.7 us against 33.4 when each workgroup adds them up; 65 tokens of eight of rank 16 15.5 against 12.1 (256: 21.3, 16.6).
+inline bool adapt_joins(const AdaptPlan& p, int tokens) { return tokens > kFewTokens || (tokens > 64 && p.tile == 64); }
 inline int64_t adapt_joined_floats(const AdaptPlan& p, int tokens, int rank) {
   int pad = 32;
   while (pad < rank) pad *= 2;
-  return tokens <= kFewTokens ? 0 : (int64_t)p.tiles * p.tile * (pad + 1);
+  return adapt_joins(p, tokens) ? (int64_t)p.tiles * p.tile * (pad + 1) : 0;
 }
 
 }  // namespace lutgemm_step_detail

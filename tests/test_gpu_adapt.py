@@ -93,7 +93,7 @@ def _case(tokens, m, n, count, rank, of, ranks=None, scales=True, f32=False, own
 @pytest.mark.parametrize("tokens,m,n,count,rank,f32", [
     (1, 1, 8, 1, 8, False), (1, 16, 32, 1, 16, True), (2, 17, 40, 2, 8, False), (3, 100, 264, 3, 24, True), (16, 64, 512, 1, 16, False), (17, 80, 520, 1, 32, False),
     (33, 255, 1032, 2, 40, True), (5, 257, 4104, 4, 64, False), (64, 130, 136, 5, 16, False), (65, 130, 136, 5, 16, False), (31, 300, 96, 40, 72, True),
-    (100, 70, 600, 7, 128, False), (9, 1000, 2048, 3, 256, True), (300, 333, 264, 3, 64, False), (1000, 90, 72, 1, 8, False), (130, 515, 1288, 100, 16, False),
+    (100, 70, 600, 7, 128, False), (128, 64, 72, 33, 16, True), (129, 68, 72, 3, 24, False), (256, 36, 40, 70, 8, True), (256, 36, 40, 256, 8, False), (257, 36, 40, 31, 8, True), (9, 1000, 2048, 3, 256, True), (300, 333, 264, 3, 64, False), (1000, 90, 72, 1, 8, False), (130, 515, 1288, 100, 16, False),
     (2100, 40, 64, 1024, 8, True), (1, 5120, 12288, 2, 16, False), (24, 900, 8192, 24, 16, False)])
 def test_against_oracle(tokens, m, n, count, rank, f32):
     rng = np.random.default_rng(tokens)

@@ -93,7 +93,7 @@ def test_adapt_refusals():
     assert need > 32768 and _refused(L.lutgemm_adapt, *{**good, "nbytes": need - 1}.values()) == W
 
 
-@pytest.mark.parametrize("tokens", [1, 3, 32, 64, 65, 300, 4096, 65536])
+@pytest.mark.parametrize("tokens", [1, 3, 32, 64, 65, 256, 257, 300, 4096, 65536])
 @pytest.mark.parametrize("count,rank,m,n", [(1, 8, 1, 8), (3, 16, 5000, 5120), (64, 64, 12288, 12288), (1024, 256, 49152, 1 << 20)])
 def test_a_plan_covers_everything(tokens, count, rank, m, n):
     a = _adapters(m=m, n=n, count=count, rank=rank)
@@ -104,8 +104,8 @@ def test_a_plan_covers_everything(tokens, count, rank, m, n):
     groups = min(count + 1, tokens)
     assert tiles == groups + (tokens - groups) // tile
     floats = parts * tiles * tile * rank
-    table = 0 if tokens <= 64 else 4 + (4 + tile) * tiles
+    table = 0 if tokens <= 256 else 4 + (4 + tile) * tiles
     pad = next(r for r in (32, 64, 128, 256) if r >= rank)
-    joined = 0 if tokens <= 64 else tiles * tile * (pad + 1)
+    joined = tiles * tile * (pad + 1) if tokens > 256 or (tokens > 64 and tile == 64) else 0
     assert L.lutgemm_adapt_workspace_bytes(a, tokens) == 32768 + 4 * (table + floats + joined)
     assert tiles <= 65535 and 32768 + 4 * floats < 1 << 40
