@@ -447,6 +447,24 @@ struct Target {
   float one, other;            // the power of two that its results are multiplied with, in two factors: one may leave 32 bits
 };
 
+// Four values of a row, which begins on as many bytes as they are together (WIDE) or as one of them is: the compiler knows which and
+// has an instruction of any alignment for the second.  Whole calls with values one by one, none of them ahead, took up to 2.2 times as
+// long: 1954 tokens, rank 16, 512 -> 28350: 172 us against 84; 2023, rank 128, 5808 -> 20791: 295 against 132.
+template <bool WIDE, typename Run, typename Y>
+__device__ __forceinline__ Run run_at(const Y* from) {
+  if (WIDE) return *reinterpret_cast<const Run*>(from);
+  Run v;
+  __builtin_memcpy(&v, from, sizeof v);
+  return v;
+}
+template <bool WIDE, typename Run, typename Y>
+__device__ __forceinline__ void run_to(Y* to, Run v) {
+  if (WIDE)
+    *reinterpret_cast<Run*>(to) = v;
+  else
+    __builtin_memcpy(to, &v, sizeof v);
+}
+
 // Y of a tile, for p.rows rows of m (tokens are the rows of the matrix instructions' results, m their columns).  A wavefront takes 64 rows
 // of B at a time (BLOCKS times that): they are contiguous in memory, and pass through LDS so that they are read that way and
 // are operands dealt out four by four: lane c of a result has rows 4 c .. 4 c + 3 of a token, the 16 lanes of a token
@@ -508,13 +526,18 @@ struct Up {
     const bool masked = tile.rank < RANKS;
     constexpr int DEPTH = sizeof(Y) == 4 && NT == 4 ? 2 : NT;        // (fp32 takes twice the registers)
     Run held[DEPTH][EACH][BLOCKS];               // of base, for the next results
+    const int64_t end = WIDE || p.m >= 4 ? p.m - 4 : 0;
     auto look = [&](int64_t at, int n) {
-      if constexpr (WIDE) {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-          const Y* base = static_cast<const Y*>(p.base) + target[min(16 * n + 4 * e + four, tile.tokens - 1)].base;
+      for (int e = 0; e < EACH; ++e) {
+        const Y* base = static_cast<const Y*>(p.base) + target[min(16 * n + 4 * e + four, tile.tokens - 1)].base;
 #pragma unroll
-          for (int b = 0; b < BLOCKS; ++b) held[n % DEPTH][e][b] = *reinterpret_cast<const Run*>(base + min(at + 64 * b + 4 * col, p.m - 4));
+        for (int b = 0; b < BLOCKS; ++b) {
+          Run& to = held[n % DEPTH][e][b];
+          if (WIDE || p.m >= 4)
+            to = run_at<WIDE, Run>(base + min(at + 64 * b + 4 * col, end));
+          else
+            to = (Run){base[0], base[min(1, (int)p.m - 1)], base[p.m - 1], base[p.m - 1]};
         }
       }
     };
@@ -562,17 +585,19 @@ struct Up {
             }
         }
         Run result[EACH][BLOCKS];
-        if constexpr (WIDE) {
 #pragma unroll
-          for (int e = 0; e < EACH; ++e) {
-            const float one = target[16 * n + 4 * e + four].one, other = target[16 * n + 4 * e + four].other;
+        for (int e = 0; e < EACH; ++e) {
+          const float one = target[16 * n + 4 * e + four].one, other = target[16 * n + 4 * e + four].other;
 #pragma unroll
-            for (int b = 0; b < BLOCKS; ++b)
+          for (int b = 0; b < BLOCKS; ++b) {
+            Run from = held[n % DEPTH][e][b];
+            if (!WIDE)                           // (a row's last one to three are behind others, which begin at `end`)
+              for (int64_t at = m0 + 64 * b + 4 * col; at > end && at < p.m; --at) from = (Run){from[1], from[2], from[3], from[3]};
 #pragma unroll
-              for (int i = 0; i < 4; ++i) result[e][b][i] = (Y)fmaf(acc[b][i][e] * one, other, (float)held[n % DEPTH][e][b][i]);
+            for (int i = 0; i < 4; ++i) result[e][b][i] = (Y)fmaf(acc[b][i][e] * one, other, (float)from[i]);
           }
-          look(n + DEPTH < NT ? m0 : after, (n + DEPTH) % NT);
         }
+        look(n + DEPTH < NT ? m0 : after, (n + DEPTH) % NT);
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
           const int t = 16 * n + 4 * e + four;
@@ -581,13 +606,12 @@ struct Up {
           for (int b = 0; b < BLOCKS; ++b) {
             const int64_t m = m0 + 64 * b + 4 * col;
             Y* y = static_cast<Y*>(p.y) + to.y + m;
-            if constexpr (WIDE) {
-              if (t < tile.tokens && m < p.m) *reinterpret_cast<Run*>(y) = result[e][b];
-            } else {
-              const Y* base = static_cast<const Y*>(p.base) + to.base + m;
+            if (t < tile.tokens && m + 4 <= p.m) {
+              run_to<WIDE>(y, result[e][b]);
+            } else if (!WIDE && t < tile.tokens && m < p.m) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (t < tile.tokens && m + i < p.m) y[i] = (Y)fmaf(acc[b][i][e] * to.one, to.other, (float)base[i]);
+              for (int i = 0; i < 3; ++i)
+                if (m + i < p.m) y[i] = result[e][b][i];
             }
           }
         }
@@ -597,7 +621,7 @@ struct Up {
 };
 
 template <int TILE, typename Y, bool WIDE, int RANKS>
-__global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= 32 && sizeof(Y) == 2 ? 3 : 2) void lutgemm_adapt_up_kernel(AdaptParams p) {
+__global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= (WIDE ? 32 : 0) && sizeof(Y) == 2 ? 3 : 2) void lutgemm_adapt_up_kernel(AdaptParams p) {
   typedef Up<TILE, Y, RANKS> U;
   extern __shared__ __attribute__((aligned(16))) char shared[];
   __shared__ int token[TILE];
@@ -620,26 +644,25 @@ __global__ __launch_bounds__(kThreads, TILE == 16 && RANKS <= 32 && sizeof(Y) ==
   tile.rank = rank_of(p, tile);
   if (tile.rank == 0) {                          // nothing is added
     typedef typename U::Run Run;
-    constexpr int kEach = WIDE ? 4 : 1, kTogether = 8;       // rows of m a thread, tokens on their way at a time
-    for (int64_t m = first + kEach * threadIdx.x; m < last; m += kEach * kThreads) {
+    constexpr int kTogether = 8;                 // tokens on their way at a time
+    const int end = (int)(last - first) & 3;     // values behind the last four
+    if (!WIDE)
+      for (int i = threadIdx.x; i < tile.tokens * end; i += kThreads) {
+        const int64_t t = token[i / end], m = last - end + i % end;
+        static_cast<Y*>(p.y)[t * p.y_stride + m] = static_cast<const Y*>(p.base)[t * p.base_stride + m];
+      }
+    for (int64_t m = first + 4 * threadIdx.x; m + 4 <= last; m += 4 * kThreads) {
       for (int t0 = 0; t0 < tile.tokens; t0 += kTogether) {
         Run v[kTogether];
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
           const Y* base = static_cast<const Y*>(p.base) + token[min(t0 + u, tile.tokens - 1)] * p.base_stride + m;
-          if (WIDE)
-            v[u] = *reinterpret_cast<const Run*>(base);
-          else
-            v[u][0] = *base;
+          v[u] = run_at<WIDE, Run>(base);
         }
 #pragma unroll
         for (int u = 0; u < kTogether; ++u) {
           Y* y = static_cast<Y*>(p.y) + token[min(t0 + u, tile.tokens - 1)] * p.y_stride + m;
-          if (t0 + u >= tile.tokens) continue;
-          if (WIDE)
-            *reinterpret_cast<Run*>(y) = v[u];
-          else
-            *y = v[u][0];
+          if (t0 + u < tile.tokens) run_to<WIDE>(y, v[u]);
         }
       }
     }

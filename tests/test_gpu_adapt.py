@@ -150,6 +150,17 @@ def test_strides_alignments_and_in_place(tokens, f32):
         _case(tokens, 129, 264, 3, 24, of, f32=f32, **more)
 
 
+@pytest.mark.parametrize("rank", [16, 40, 128])
+@pytest.mark.parametrize("tokens,count", [(2, 1), (30, 2), (70, 1), (96, 3), (300, 2)])
+def test_ends_of_rows(tokens, count, rank):
+    """Rows that end anywhere in a run of four, shorter ones too, that begin on any value's bytes; tokens without an adapter among them."""
+    for k, m in enumerate((1, 2, 3, 4, 5, 6, 7, 62, 63, 65, 127, 129, 130, 255, 513, 514, 515, 517)):
+        f32, in_place = k % 2 == 1, k % 3 == 0
+        print("case ends", tokens, count, rank, m, f32, in_place, flush=True)
+        for more in (dict(), dict(base_stride=m + 1 + k % 4, offset=k % 4)):
+            _case(tokens, m, 72, count, rank, np.arange(tokens) % (count + 1), f32=f32 != bool(more), in_place=in_place, **more)
+
+
 @pytest.mark.parametrize("tokens", [12, 80])
 def test_large_and_special_values(tokens):
     """A_a x beyond fp16's range, far below it, infinities and NaNs in one token and one adapter, which the others do not see."""
