@@ -3,7 +3,7 @@
 // A workgroup owns a row and holds it in registers between the two things that are done with it, so that every value
 // is read once: s = x + r, the sum of squares (in 64 bits: squares of fp32 values leave 32), then s * inv * w.  What bounds it is
 // HBM: 4096 rows of 12288 channels, 403 MB, 68.7 us, 5.9 TB/s (a copy past the caches: 6.3); of few rows the launch and one chain of
-// load, sum and store (3.4 us for one).  The next row on its way during a row's sum (512 workgroups that stay) was no faster: 75 to 79 us.
+// load, sum and store (3.4 us for one).  Rows that begin anywhere: 4096 of 12289 channels 92 us (280 value by value).  The next row on its way during a row's sum (512 workgroups that stay) was no faster: 75 to 79 us.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -43,15 +43,36 @@ using lutgemm_norm_parts::Params;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+typedef uint32_t Loose __attribute__((ext_vector_type(4), aligned(2)));      // 16 bytes that begin on any value's
+
 constexpr int kRun = 8;      // channels that a thread has next to each other
 
-// Eight values as they are in memory, 16 bytes at a time.
+// Eight values as they are in memory, 16 bytes at a time; those of a row that begins anywhere (not WIDE) too, with the compiler's
+// instructions for that; of a row of fewer as many as there are.
 template <typename T>
 struct Eight {
   u32x4 part[sizeof(T) * kRun / 16];
-  __device__ __forceinline__ void load(const T* p) {
+  template <bool WIDE>
+  __device__ __forceinline__ void load(const T* p, int n) {
+    if (WIDE) {
 #pragma unroll
-    for (unsigned i = 0; i < sizeof(part) / 16; ++i) part[i] = reinterpret_cast<const u32x4*>(p)[i];
+      for (unsigned i = 0; i < sizeof(part) / 16; ++i) part[i] = reinterpret_cast<const u32x4*>(p)[i];
+    } else {
+      if (n >= kRun) {
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(part) / 16; ++i) part[i] = reinterpret_cast<const Loose*>(p)[i];
+      } else {
+        constexpr int kEach = 16 / sizeof(T);
+        typedef T Values __attribute__((ext_vector_type(kEach)));
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(part) / 16; ++i) {
+          Values t;
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) t[e] = p[min((int)(kEach * i) + e, n - 1)];
+          part[i] = __builtin_bit_cast(u32x4, t);
+        }
+      }
+    }
   }
   __device__ __forceinline__ float value(int e) const { return (float)reinterpret_cast<const T*>(part)[e]; }
 };
@@ -68,59 +89,62 @@ __device__ __forceinline__ void store_wide(T* p, const float* v, bool past) {
       reinterpret_cast<u32x4*>(p)[i] = reinterpret_cast<const u32x4*>(t)[i];
   }
 }
+template <int COUNT = kRun, typename T>
+__device__ __forceinline__ void store_any(T* p, const float* v) {
+  T t[COUNT];
+#pragma unroll
+  for (int e = 0; e < COUNT; ++e) t[e] = (T)v[e];
+  __builtin_memcpy(p, t, sizeof t);
+}
 
-// WIDE: a thread's runs are eight channels next to each other, 16 bytes at a time; else rows begin anywhere and have any length: a
-// wavefront's lanes take channels next to each other.
+// A thread's runs are eight channels next to each other.  WIDE: rows begin on 16 bytes and are whole runs; else they begin anywhere and
+// have any length: the last run is read from the row's last eight channels, and those that the run before it has are left out.
 template <typename X, typename S, bool BYTES, bool WIDE, int THREADS, int RUNS>
 __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
   constexpr int kWaves = THREADS / 64;
   extern __shared__ uint32_t tops[];               // of every group: the largest |y|, as bits
   __shared__ double squares[kWaves];
   const int tid = threadIdx.x;
-  auto channel = [&](int run, int e) { return (uint32_t)(WIDE ? (run * THREADS + tid) * kRun + e : (run * kRun + e) * THREADS + tid); };
+  auto channel = [&](int run) { return (run * THREADS + tid) * kRun; };
   // (Loads have no branches: beyond the row's end they repeat its last eight channels.)
-  auto place = [&](int run) { return min(channel(run, 0), (uint32_t)(p.n - kRun)); };
+  auto place = [&](int run) { return WIDE ? min(channel(run), p.n - kRun) : max(min(channel(run), p.n - kRun), 0); };
+  auto has = [&](int run, int e) { return WIDE ? channel(run) < p.n : place(run) + e >= channel(run) && place(run) + e < p.n; };
+  auto keep = [&](int run, const float* v, auto* row, bool past) {
+    const int c = channel(run);
+    if (WIDE) {
+      if (c < p.n) store_wide(row + c, v, past);
+    } else if (c + kRun <= p.n) {
+      store_any(row + c, v);
+    } else if (c < p.n) {
+#pragma unroll
+      for (int e = 0; e < kRun; ++e)
+        if (has(run, e)) store_any<1>(row + place(run) + e, v + e);
+    }
+  };
 
   Eight<_Float16> w[RUNS];
-  if constexpr (WIDE) {
-    if (p.weight) {
+  if (p.weight) {
 #pragma unroll
-      for (int k = 0; k < RUNS; ++k) w[k].load(p.weight + place(k));
-    }
+    for (int k = 0; k < RUNS; ++k) w[k].template load<WIDE>(p.weight + place(k), p.n);
   }
   Eight<X> x[RUNS];
   Eight<S> r[RUNS];
   const int64_t row = blockIdx.x;
-  if (WIDE) {
 #pragma unroll
-    for (int k = 0; k < RUNS; ++k) x[k].load(static_cast<const X*>(p.x) + row * p.x_stride + place(k));
-    if (p.residual) {
+  for (int k = 0; k < RUNS; ++k) x[k].template load<WIDE>(static_cast<const X*>(p.x) + row * p.x_stride + place(k), p.n);
+  if (p.residual) {
 #pragma unroll
-      for (int k = 0; k < RUNS; ++k) r[k].load(static_cast<const S*>(p.residual) + row * p.stream_stride + place(k));
-    }
+    for (int k = 0; k < RUNS; ++k) r[k].template load<WIDE>(static_cast<const S*>(p.residual) + row * p.stream_stride + place(k), p.n);
   }
   float v[RUNS][kRun];
 #pragma unroll
-  for (int k = 0; k < RUNS; ++k) {
-    if constexpr (WIDE) {
-      const bool inside = channel(k, 0) < (uint32_t)p.n;
+  for (int k = 0; k < RUNS; ++k)
 #pragma unroll
-      for (int e = 0; e < kRun; ++e) {
-        v[k][e] = x[k].value(e);
-        if (p.residual) v[k][e] += r[k].value(e);
-        v[k][e] = inside ? v[k][e] : 0.0f;
-      }
-    } else {
-      const X* at = static_cast<const X*>(p.x) + row * p.x_stride;
-      const S* stream = static_cast<const S*>(p.residual) + row * p.stream_stride;
-#pragma unroll
-      for (int e = 0; e < kRun; ++e) {
-        const uint32_t c = channel(k, e);
-        v[k][e] = c < (uint32_t)p.n ? (float)at[c] : 0.0f;
-        if (p.residual && c < (uint32_t)p.n) v[k][e] += (float)stream[c];
-      }
+    for (int e = 0; e < kRun; ++e) {
+      v[k][e] = x[k].value(e);
+      if (p.residual) v[k][e] += r[k].value(e);
+      v[k][e] = has(k, e) ? v[k][e] : 0.0f;
     }
-  }
   if (BYTES) {
     for (int g = tid; g < p.groups; g += THREADS) tops[g] = 0;
   }
@@ -132,15 +156,7 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
   if (p.sum) {
     S* sum = static_cast<S*>(p.sum) + row * p.stream_stride;
 #pragma unroll
-    for (int k = 0; k < RUNS; ++k) {
-      if (WIDE) {
-        if (channel(k, 0) < (uint32_t)p.n) store_wide(sum + channel(k, 0), v[k], p.past);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < (uint32_t)p.n) sum[channel(k, e)] = (S)v[k][e];
-      }
-    }
+    for (int k = 0; k < RUNS; ++k) keep(k, v[k], sum, p.past);
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) square += __shfl_xor(square, d);
@@ -153,41 +169,23 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
 #pragma unroll
   for (int k = 0; k < RUNS; ++k) {
 #pragma unroll
-    for (int e = 0; e < kRun; ++e) {
-      float weight = 1.0f;
-      if (p.weight) weight = WIDE ? w[k].value(e) : (channel(k, e) < (uint32_t)p.n ? (float)p.weight[channel(k, e)] : 1.0f);
-      v[k][e] = v[k][e] * inv * weight;
-    }
+    for (int e = 0; e < kRun; ++e) v[k][e] = v[k][e] * inv * (p.weight ? w[k].value(e) : 1.0f);
   }
 
   if constexpr (!BYTES) {
     _Float16* y = static_cast<_Float16*>(p.y) + row * p.y_stride;
 #pragma unroll
-    for (int k = 0; k < RUNS; ++k) {
-      if (WIDE) {
-        if (channel(k, 0) < (uint32_t)p.n) store_wide(y + channel(k, 0), v[k], p.past);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < (uint32_t)p.n) y[channel(k, e)] = (_Float16)v[k][e];
-      }
-    }
+    for (int k = 0; k < RUNS; ++k) keep(k, v[k], y, p.past);
   } else {
     int8_t* y = static_cast<int8_t*>(p.y) + row * p.y_stride;
 #pragma unroll
     for (int k = 0; k < RUNS; ++k) {
-      if (WIDE) {
-        uint32_t top = 0;                          // (as bits: infinities and NaNs come out on top)
+      uint32_t top = 0;                            // (as bits: infinities and NaNs come out on top)
 #pragma unroll
-        for (int e = 0; e < kRun; ++e) top = max(top, __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2));       // of 32 channels, which are of one group
-        if ((tid & 3) == 0 && channel(k, 0) < (uint32_t)p.n) atomicMax(&tops[channel(k, 0) / (uint32_t)p.group], top);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < (uint32_t)p.n) atomicMax(&tops[channel(k, e) / (uint32_t)p.group], __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
-      }
+      for (int e = 0; e < kRun; ++e) top = has(k, e) ? max(top, __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu) : top;
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2));         // of 32 channels, which are of one group: a group has 32 channels' multiple, or all
+      if ((tid & 3) == 0 && channel(k) < p.n) atomicMax(&tops[(uint32_t)channel(k) / (uint32_t)p.group], top);
     }
     __syncthreads();
     for (int g = tid; g < p.groups; g += THREADS) {
@@ -202,19 +200,21 @@ __global__ __launch_bounds__(THREADS) void lutgemm_rms_norm_kernel(Params p) {
         return top < __builtin_inff() && !(top < 0x1p-100f) ? 127.0f / top : 0.0f;
       };
       auto code = [&](float value, float per) { return per == 0.0f ? 0 : (int)rintf(value * per); };
-      if (WIDE) {
-        const uint32_t c = channel(k, 0);
-        if (c < (uint32_t)p.n) {
-          const float steps = per(tops[c / (uint32_t)p.group]);
-          uint32_t word[2] = {0, 0};
+      const int c = channel(k);
+      if (c >= p.n) continue;
+      const float steps = per(tops[(uint32_t)c / (uint32_t)p.group]);
+      if (WIDE || c + kRun <= p.n) {
+        uint32_t word[2] = {0, 0};
 #pragma unroll
-          for (int e = 0; e < kRun; ++e) word[e / 4] |= ((uint32_t)code(v[k][e], steps) & 0xffu) << (8 * (e % 4));
+        for (int e = 0; e < kRun; ++e) word[e / 4] |= ((uint32_t)code(v[k][e], steps) & 0xffu) << (8 * (e % 4));
+        if (WIDE)
           *reinterpret_cast<u32x2*>(y + c) = (u32x2){word[0], word[1]};
-        }
+        else
+          __builtin_memcpy(y + c, word, sizeof word);
       } else {
 #pragma unroll
         for (int e = 0; e < kRun; ++e)
-          if (channel(k, e) < (uint32_t)p.n) y[channel(k, e)] = (int8_t)code(v[k][e], per(tops[channel(k, e) / (uint32_t)p.group]));
+          if (has(k, e)) y[place(k) + e] = (int8_t)code(v[k][e], steps);
       }
     }
   }
@@ -312,9 +312,9 @@ extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void*
                     (!sum || rows16(sum, stream_stride, ss)) && (uintptr_t)weight % 16 == 0 &&
                     (bytes ? ((uintptr_t)y | (uintptr_t)y_stride) % 8 == 0 : rows16(y, y_stride, 2));
   const int units = (n + 7) / 8;
-  // Threads enough for four runs each; more where there are few rows and much to do for a value, one by one or to 8 bits (77 rows of
-  // 5003 channels 5.6 us with 1024 threads, 9.7 with 256; 509 of 8192 to 8 bits 10.1 and 11.5).
-  const bool spread = tokens <= 1024 && (!wide || bytes);
+  // Threads enough for four runs each; more where there are few rows to 8 bits (509 of 8192 channels 10.1 us with 1024 threads, 11.5
+  // with 256; to fp16, rows that begin anywhere: 300 of 5003 6.6 and 5.3 with 256, 1000 12.4 and 9.3).
+  const bool spread = tokens <= 1024 && bytes;
   const int threads = spread ? (units <= 64 ? 64 : (units <= 256 ? 256 : 1024)) : (units <= 256 ? 64 : (units <= 1024 ? 256 : (units <= 2048 ? 512 : 1024)));
   int runs = (units + threads - 1) / threads;
   if (threads == 64 && runs == 3) runs = 4;

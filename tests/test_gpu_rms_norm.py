@@ -148,6 +148,33 @@ def test_eight_bits(tokens, n, group, x_f32, stream_f32, gap, offset):
         assert (scales[:, 0] == 0).all() and (y[:, :g] == 0).all()
 
 
+@pytest.mark.parametrize("x_f32,stream_f32", [(False, False), (True, False), (False, True), (True, True)])
+def test_ends_of_rows(x_f32, stream_f32):
+    """Rows that end anywhere in a run of eight, shorter ones too, that begin on any value's bytes: in place, and to 8 bits; what is behind a row stays."""
+    torch = torch_cuda()
+    rng = np.random.default_rng(60 + x_f32 + 2 * stream_f32)
+    flags = (L.LUTGEMM_Y_F32 if x_f32 else 0) | (L.LUTGEMM_NORM_STREAM_F32 if stream_f32 else 0)
+    for k, n in enumerate((1, 2, 5, 7, 8, 9, 11, 14, 15, 511, 513, 516, 519, 2047, 2050, 4101, 8191, 8193, 16387, 24577, 32761)):
+        tokens, stride = 1030 if 500 < n < 3000 else 3, n + k % 4
+        print("case ends", n, tokens, stride, x_f32, stream_f32, flush=True)
+        x, r = _rows(rng, tokens, n, stride, x_f32), _rows(rng, tokens, n, stride, stream_f32, 3.0)
+        w = (1 + 0.1 * rng.standard_normal(n)).astype(np.float16)
+        d_x, d_r, d_y = _up(x), _up(r), _up(np.full((tokens, stride), MARK, np.float16))
+        s, ref = S.rms_norm(x[:, :n], r[:, :n], w, EPS)
+        _call(d_x, d_r, _up(w), d_r, d_y, None, tokens, n, 0, stride, stride, stride, flags)
+        y = _down(d_y, tokens, stride)
+        _check_y(y[:, :n], ref)
+        assert (y[:, n:] == MARK).all()
+        after = _down(d_r, tokens, stride)
+        _check_sum(after[:, :n], s, stream_f32)
+        np.testing.assert_array_equal(after[:, n:], r[:, n:])
+        codes, scales = _up(np.full((tokens, stride), MARK, np.int8)), torch.empty(tokens, 1, device="cuda")
+        _call(d_x, _up(r), _up(w), None, codes, scales, tokens, n, 0, stride, stride, stride, flags)
+        steps = scales.cpu().numpy().astype(np.float64)
+        y = _down(codes, tokens, stride)
+        assert (np.abs(y[:, :n] * steps - ref) <= steps * (0.5 + 127 * 8 * 2.0 ** -24)).all() and (y[:, n:] == MARK).all()
+
+
 def test_in_place():
     """sum over residual, y over x; sum over x where y goes elsewhere; y over the residual; rows side by side in one buffer."""
     torch = torch_cuda()
