@@ -72,7 +72,7 @@ class AttentionHalf:
         if len(turns) * 2 != self.rot_dim:
             raise ValueError(f"{self.rot_dim} channels are turned by {self.rot_dim // 2} frequencies, not {len(turns)}")
         self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
-        self.lengths, self.counts = [0] * seqs, None
+        self.lengths = [0] * seqs
         self.placed, self.known = False, True       # a step that `keep` has not ended; whether the host knows the lengths
         self.past = torch.zeros(seqs, dtype=torch.int32, device="cuda")
         self.first = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
@@ -184,7 +184,7 @@ class AttentionHalf:
             raise ValueError("sequences that advance on the device share their pages")
         if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
             raise ValueError(f"up to {MOST_ROWS} sequences advance, up to a length of {self.longest}")
-        self.masked, self.counts, self.placed, self.known = False, None, False, False
+        self.masked, self.placed, self.known = False, False, False
         self.step = self._step(self.seqs, 1)
         self.fresh.fill_(1)
         L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, 1, self.first, self.positions, self.owner, None, self._stream())
@@ -202,8 +202,8 @@ class AttentionHalf:
 
     def keep(self, accepted=None):
         """The step's tokens become the past; accepted: of each sequence which of its tokens (ascending) do, next to each other."""
-        if self.counts is None:
-            raise ValueError("steps that `place` has placed are kept")
+        if not self.placed:
+            raise ValueError("a step that `place` has placed is kept, once")
         if accepted is None:
             kept = self.counts
         else:
