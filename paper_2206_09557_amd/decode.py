@@ -193,6 +193,8 @@ class AttentionHalf:
 
     def advanced(self):
         """What the device has made of the lengths since the last `place` or `advanced`; waits for it."""
+        if not self.shared:
+            raise ValueError("sequences that advance on the device share their pages")
         self.lengths = self.past.tolist()
         self.taken = self.owned.tolist()
         self.left, self.known = int(self.free_count), True

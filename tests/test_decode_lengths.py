@@ -64,3 +64,16 @@ def test_a_step_is_kept_once(device, pages):
     half.place([1, 1])
     half.keep([[0], []])
     assert half.lengths == [4, 0]
+
+
+def test_only_shared_pages_are_advanced(device):
+    """The device keeps no lengths of sequences with pages of their own; the host's stay."""
+    half = _half(512, 8, 2, 64, 2, 80, 16)
+    half.place([3, 2])
+    half.keep()
+    with pytest.raises(ValueError):
+        half.advanced()
+    assert half.lengths == [3, 2] and half.known
+    half.place([1, 1])
+    half.keep()
+    assert half.lengths == [4, 3]
