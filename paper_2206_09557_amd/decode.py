@@ -33,7 +33,8 @@ class AttentionHalf:
 
     `place` says where the next step's tokens stand, `run` launches the step (and may be captured), `keep` advances the
     lengths by all of the step's tokens, or by those of a drafted tree that were accepted.  `advance` is a step of one token of every
-    sequence with all of that on the device, for a graph to replay; `advanced` tells the host afterwards how many were."""
+    sequence with all of that on the device, for a graph to replay (not between a step's `place` and `keep`); `advanced` tells the host
+    afterwards what the lengths are, which `place`, `keep` and `end` have to know."""
 
     def __init__(self, qkv, out, hidden, heads, kv_heads, head_dim, seqs, longest, q=3, g=128, kv_bits=8, kv_group=0, page=64,
                  turns=None, rot_dim=0, neighbours=False, amplitude=1.0, norm=None, eps=1e-5, adapters=(None, None), pages=0):
@@ -73,7 +74,8 @@ class AttentionHalf:
             raise ValueError(f"{self.rot_dim} channels are turned by {self.rot_dim // 2} frequencies, not {len(turns)}")
         self.turns = torch.from_numpy(turns.view(np.int64)).cuda()
         self.lengths = [0] * seqs
-        self.placed, self.known = False, True       # a step that `keep` has not ended; whether the host knows the lengths
+        # a step that `keep` has not ended; whether the host knows the lengths; whether there may be a graph that advances them unseen
+        self.placed, self.known, self.captured = False, True, False
         self.past = torch.zeros(seqs, dtype=torch.int32, device="cuda")
         self.first = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
         self.positions = torch.zeros(MOST_ROWS, dtype=torch.int32, device="cuda")
@@ -113,8 +115,7 @@ class AttentionHalf:
             raise ValueError("a step has a depth for every token, by sequences")
         if mask is not None and len(mask) != sum(counts):
             raise ValueError("a step has a mask word for every token")
-        if not self.known:
-            raise ValueError("the lengths have advanced on the device: `advanced` tells them")
+        self._check_known()
         needed = [0] * self.seqs
         if self.shared:
             needed = [max(0, -(-(n + c) // self.page) - t) if c else 0 for n, c, t in zip(self.lengths, counts, self.taken)]
@@ -135,6 +136,11 @@ class AttentionHalf:
             L.lutgemm_kv_place(self.pages, self.past, self.fresh, sum(counts), max(counts), self.first, None, None, None, self._stream())
             self.taken = [t + n for t, n in zip(self.taken, needed)]
             self.left -= sum(needed)
+
+    def _check_known(self):
+        """Nothing of this class runs when a graph is replayed: once there may be one, the device's lengths are looked at, and waited for."""
+        if not self.known or self.captured and self.past.tolist() != self.lengths:
+            raise ValueError("the lengths have advanced on the device: `advanced` tells them")
 
     def _product(self, weights, x, y, m, n, batch):
         bits, alpha, z = weights
@@ -185,6 +191,7 @@ class AttentionHalf:
         if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
             raise ValueError(f"up to {MOST_ROWS} sequences advance, up to a length of {self.longest}")
         self.masked, self.placed, self.known = False, False, False
+        self.captured = self.captured or self.torch.cuda.is_current_stream_capturing()
         self.step = self._step(self.seqs, 1)
         self.fresh.fill_(1)
         L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, 1, self.first, self.positions, self.owner, None, self._stream())
@@ -195,7 +202,9 @@ class AttentionHalf:
         """What the device has made of the lengths since the last `place` or `advanced`; waits for it."""
         if not self.shared:
             raise ValueError("sequences that advance on the device share their pages")
-        self.lengths = self.past.tolist()
+        lengths = self.past.tolist()
+        if lengths != self.lengths:                 # (a step that was placed before is not what it was)
+            self.lengths, self.placed = lengths, False
         self.taken = self.owned.tolist()
         self.left, self.known = int(self.free_count), True
         if max(self.lengths) > self.longest:
@@ -206,6 +215,7 @@ class AttentionHalf:
         """The step's tokens become the past; accepted: of each sequence which of its tokens (ascending) do, next to each other."""
         if not self.placed:
             raise ValueError("a step that `place` has placed is kept, once")
+        self._check_known()
         if accepted is None:
             kept = self.counts
         else:
@@ -236,8 +246,9 @@ class AttentionHalf:
 
     def end(self, seq):
         """Sequence `seq` is over, between two steps: its pages are free, and the next tokens are a new one's first."""
-        if self.placed or not self.known:
+        if self.placed:
             raise ValueError("a sequence ends after `keep`, or after `advanced`")
+        self._check_known()
         self.lengths[seq] = 0
         if self.shared:
             self._set(self.past, self.lengths, np.int32)

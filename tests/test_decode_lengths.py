@@ -42,6 +42,8 @@ class Device:
 
 @pytest.fixture
 def device(on_host, monkeypatch):  # noqa: F811
+    import torch
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return Device(monkeypatch)
 
 
@@ -77,3 +79,62 @@ def test_only_shared_pages_are_advanced(device):
     half.place([1, 1])
     half.keep()
     assert half.lengths == [4, 3]
+
+
+class Decoding:
+    """A layer whose `advance` is captured and replayed, on the host: a replay does what it did to the tensors, and runs none of the class."""
+
+    def __init__(self, monkeypatch, *args, **more):
+        self.half = _half(*args, **more)
+        monkeypatch.setattr(self.half, "run", lambda *rows: None)
+
+    def capture(self, monkeypatch, device):
+        """Nothing is executed."""
+        import copy
+        import torch
+        kept = {name: t.clone() for name, t in vars(self.half).items() if torch.is_tensor(t)}
+        pages = copy.deepcopy(device.pages)
+        with monkeypatch.context() as m:
+            m.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+            self.half.advance(None, None)
+        for name, t in kept.items():
+            vars(self.half)[name].copy_(t)
+        device.pages = pages
+
+    def replay(self):
+        state = dict(vars(self.half))
+        self.half.advance(None, None)
+        vars(self.half).update(state)
+
+
+def test_replays_that_the_host_has_not_asked_about(device, monkeypatch):
+    """A graph is replayed again after `advanced`: no step is placed or kept, and no sequence ends, by lengths that are no longer so."""
+    d = Decoding(monkeypatch, 512, 8, 2, 64, 2, 80, 16, page=32, pages=6)
+    half = d.half
+    half.place([30, 1])
+    half.keep()
+    d.capture(monkeypatch, device)
+    assert half.advanced() == [30, 1]
+    for k in range(3):
+        d.replay()
+    assert half.past.tolist() == [33, 4] and half.owned.tolist() == [2, 1]
+    for call in (lambda: half.place([1, 1]), lambda: half.end(0), half.keep):
+        with pytest.raises(ValueError):
+            call()
+    assert half.past.tolist() == [33, 4] and half.lengths == [30, 1]
+    assert half.advanced() == [33, 4] and half.taken == [2, 1] and half.left == 3
+    half.place([1, 0])
+    half.keep()
+    half.end(1)
+    assert half.lengths == [34, 0] == half.past.tolist() and half.left == 4
+    # one between a step's place and its keep: the step is not what it was
+    half.place([2, 2])
+    d.replay()
+    with pytest.raises(ValueError):
+        half.keep()
+    assert half.advanced() == [35, 1]
+    with pytest.raises(ValueError):
+        half.keep()
+    half.place([2, 2])
+    half.keep([[0], [0, 1]])
+    assert half.lengths == [36, 3] == half.past.tolist()

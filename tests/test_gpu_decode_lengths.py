@@ -1,0 +1,54 @@
+"""GPU checks of decode.AttentionHalf where a captured step and steps placed by the host take turns."""
+import numpy as np
+import pytest
+
+from gpu_util import torch_cuda
+import test_gpu_decode as D
+from test_gpu_decode_serving import Serving
+
+pytestmark = pytest.mark.gpu
+
+
+def _captured(torch, half, x, y, *residual):
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        half.advance(x, y, *residual)
+    return graph
+
+
+def test_replays_and_placed_steps_in_turn():
+    """A graph is replayed again after `advanced`: the host's calls are refused till it has asked, and go on from there."""
+    torch = torch_cuda()
+    sv = Serving(2, 90, pages=6)
+    half = sv.half
+    x = D._tokens(torch, 2, 30, D.HIDDEN, seed=1)
+    half.fill(D._up(torch, x), torch.empty(2, 30, D.HIDDEN, dtype=torch.float16, device="cuda"))
+    token, y = torch.empty(2, D.HIDDEN, dtype=torch.float16, device="cuda"), torch.empty(2, D.HIDDEN, dtype=torch.float16, device="cuda")
+    graph = _captured(torch, half, token, y)
+    assert half.advanced() == [30, 30]
+    seen, results = [x[s] for s in range(2)], [[], []]
+    for turn in range(3):
+        for _ in range(2):
+            more = D._tokens(torch, 2, D.HIDDEN, seed=10 * turn + len(results[0]))
+            token.copy_(D._up(torch, more))
+            graph.replay()
+            torch.cuda.synchronize()
+            for s in range(2):
+                seen[s] = np.concatenate([seen[s], more[s:s + 1]])
+                results[s].append(y[s].cpu().numpy())
+        for call in (lambda: half.place([1, 1]), lambda: half.end(0), half.keep):
+            with pytest.raises(ValueError):
+                call()
+        assert half.advanced() == [len(t) for t in seen] == half.past.tolist()
+        more = D._tokens(torch, 2, D.HIDDEN, seed=90 + turn)
+        one = torch.empty(2, D.HIDDEN, dtype=torch.float16, device="cuda")
+        half.place([1, 1])
+        half.run(D._up(torch, more), one)
+        half.keep()
+        for s in range(2):
+            seen[s] = np.concatenate([seen[s], more[s:s + 1]])
+            results[s].append(one[s].cpu().numpy())
+    assert half.lengths == [39, 39] == half.past.tolist() and half.taken == [2, 2] == half.owned.tolist()
+    for s in range(2):
+        D._close(np.stack(results[s]), sv.reference(s, seen[s])[30:])
