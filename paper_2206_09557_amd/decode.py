@@ -42,7 +42,7 @@ class AttentionHalf:
         self.torch, self.weights, self.hidden, self.heads, self.kv_heads, self.dim = torch, (qkv, out), hidden, heads, kv_heads, head_dim
         self.q, self.g, self.seqs = q, g, seqs
         self.row = (heads + 2 * kv_heads) * head_dim
-        width = -(-(longest + MOST_ROWS) // page)
+        width = -(-(longest + MOST_ROWS + bool(pages)) // page)        # (one more: `advance`)
         held = pages or seqs * width
         self.pool = torch.empty(L.lutgemm_kv_pool_bytes(held, page, kv_heads, head_dim, kv_bits, kv_group), dtype=torch.uint8,
                                 device="cuda")
@@ -55,6 +55,10 @@ class AttentionHalf:
             L.lutgemm_kv_pages_init(self.pages, self._stream())
             self.taken, self.left = [0] * seqs, pages          # the host's count of them
             self.fresh = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+            # of `advance`: which sequences have as many positions as they may, and what the others and they ask for
+            self.full = torch.zeros(seqs, dtype=torch.bool, device="cuda")
+            self.asked = torch.zeros(2, seqs, dtype=torch.int32, device="cuda")
+            self.asked[0], self.asked[1] = 1, seqs + 1
         else:
             self.table = torch.arange(seqs * width, dtype=torch.int32, device="cuda").view(seqs, width)
         self.longest = longest
@@ -184,8 +188,8 @@ class AttentionHalf:
 
     def advance(self, x, y, residual=None):
         """One token of every sequence, x [seqs][hidden]: placed, run, and its lengths advanced, all on the device, so that a captured call can be
-        replayed, as long as no sequence grows beyond `longest`.  A sequence that finds no page (and those behind it) waits: its rows of y and
-        residual mean nothing, its length stays.  The host learns of it by `advanced`."""
+        replayed.  A sequence that finds no page, or is `longest` positions long, waits, and those behind it: their rows of y and
+        residual mean nothing, their lengths stay.  The host learns of it by `advanced`."""
         if not self.shared:
             raise ValueError("sequences that advance on the device share their pages")
         if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
@@ -193,8 +197,11 @@ class AttentionHalf:
         self.masked, self.placed, self.known = False, False, False
         self.captured = self.captured or self.torch.cuda.is_current_stream_capturing()
         self.step = self._step(self.seqs, 1)
-        self.fresh.fill_(1)
-        L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, 1, self.first, self.positions, self.owner, None, self._stream())
+        # One of `longest` positions asks for more rows than there are: it waits (a sequence whose table holds no more would be passed over, and
+        # those behind it would have one another's rows of x).
+        self.torch.ge(self.past, self.longest, out=self.full)
+        self.torch.where(self.full, self.asked[1], self.asked[0], out=self.fresh)
+        L.lutgemm_kv_place(self.pages, self.past, self.fresh, self.seqs, self.seqs + 1, self.first, self.positions, self.owner, None, self._stream())
         self.run(x, y, residual)
         self.past.add_(self.first[1:] - self.first[:-1])
 
@@ -207,8 +214,6 @@ class AttentionHalf:
             self.lengths, self.placed = lengths, False
         self.taken = self.owned.tolist()
         self.left, self.known = int(self.free_count), True
-        if max(self.lengths) > self.longest:
-            raise ValueError(f"a sequence has grown beyond {self.longest}")
         return self.lengths
 
     def keep(self, accepted=None):

@@ -138,3 +138,32 @@ def test_replays_that_the_host_has_not_asked_about(device, monkeypatch):
     half.place([2, 2])
     half.keep([[0], [0, 1]])
     assert half.lengths == [36, 3] == half.past.tolist()
+
+
+@pytest.mark.parametrize("seqs,page", [(3, 32), (32, 32)])
+def test_replays_beyond_the_longest(device, monkeypatch, seqs, page):
+    """A sequence of `longest` positions waits, and those behind it: nobody has another's row, and none is longer."""
+    longest = 64                                   # (with 32 tokens more the table's pages end there)
+    d = Decoding(monkeypatch, 512, 8, 2, 64, seqs, longest, 16, page=page, pages=200)
+    half = d.half
+    lengths = [5, longest - 2] + [9] * (seqs - 2)
+    for s, n in enumerate(lengths):
+        for at in range(0, n, 32):
+            half.place([min(32, n - at) if k == s else 0 for k in range(seqs)])
+            half.keep()
+    d.capture(monkeypatch, device)
+    assert half.advanced() == lengths
+    for k in range(5):
+        d.replay()
+        served = seqs if k < 2 else 1
+        assert half.first.tolist() == [min(s, served) for s in range(seqs + 1)]
+        assert half.owner[:seqs].tolist() == list(range(served)) + [-1] * (seqs - served)
+        assert half.positions[:served].tolist() == [5 + k, longest - 2 + k, *[9 + k] * (seqs - 2)][:served]
+    assert half.advanced() == [10, longest] + [11] * (seqs - 2)
+    with pytest.raises(ValueError):
+        half.place([0, 1] + [0] * (seqs - 2))
+    half.place([1, 0] + [1] * (seqs - 2))
+    half.keep()
+    assert half.lengths == [11, longest] + [12] * (seqs - 2) == half.past.tolist()
+    half.end(1)
+    assert half.owned.tolist() == half.taken == [1, 0] + [1] * (seqs - 2)

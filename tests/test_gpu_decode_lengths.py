@@ -52,3 +52,42 @@ def test_replays_and_placed_steps_in_turn():
     assert half.lengths == [39, 39] == half.past.tolist() and half.taken == [2, 2] == half.owned.tolist()
     for s in range(2):
         D._close(np.stack(results[s]), sv.reference(s, seen[s])[30:])
+
+
+def test_replays_beyond_the_longest():
+    """Sequences that may not grow wait, and those behind them; what they then get is what they would have had."""
+    torch = torch_cuda()
+    longest, begin = 40, (30, 38, 31)
+    sv = Serving(3, longest, pages=9)
+    half = sv.half
+    x = D._tokens(torch, 3, 38, D.HIDDEN, seed=2)
+    y, seen, results = torch.empty(38, D.HIDDEN, dtype=torch.float16, device="cuda"), [], [[], [], []]
+    for s, n in enumerate(begin):
+        for at, count in ((0, 30), (30, n - 30)):
+            if count:
+                half.place([count if k == s else 0 for k in range(3)])
+                half.run(D._up(torch, x[s, at:at + count]), y[:count])
+                half.keep()
+        seen.append(x[s, :n])
+    token, y = torch.empty(3, D.HIDDEN, dtype=torch.float16, device="cuda"), torch.empty(3, D.HIDDEN, dtype=torch.float16, device="cuda")
+    graph = _captured(torch, half, token, y)
+    half.advanced()
+    for k in range(13):
+        more = D._tokens(torch, 3, D.HIDDEN, seed=30 + k)
+        token.copy_(D._up(torch, more))
+        graph.replay()
+        torch.cuda.synchronize()
+        for s in range(3 if k < 2 else 1 if k < 10 else 0):
+            seen[s] = np.concatenate([seen[s], more[s:s + 1]])
+            results[s].append(y[s].cpu().numpy())
+    assert half.advanced() == [40, 40, 33] == [len(t) for t in seen] and half.left == 3
+    for s in (0, 1):
+        half.end(s)
+    more = D._tokens(torch, 1, D.HIDDEN, seed=60)
+    half.place([0, 0, 1])
+    half.run(D._up(torch, more), y[:1])
+    half.keep()
+    seen[2] = np.concatenate([seen[2], more])
+    results[2].append(y[0].cpu().numpy())
+    for s in range(3):
+        D._close(np.stack(results[s]), sv.reference(s, seen[s])[begin[s]:])
