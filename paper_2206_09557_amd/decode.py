@@ -55,10 +55,11 @@ class AttentionHalf:
             L.lutgemm_kv_pages_init(self.pages, self._stream())
             self.taken, self.left = [0] * seqs, pages          # the host's count of them
             self.fresh = torch.zeros(seqs, dtype=torch.int32, device="cuda")
-            # of `advance`: which sequences have as many positions as they may, and what the others and they ask for
+            # of `advance`: which sequences have as many positions as they may, and what the others and they ask for (nothing where they rest)
             self.full = torch.zeros(seqs, dtype=torch.bool, device="cuda")
             self.asked = torch.zeros(2, seqs, dtype=torch.int32, device="cuda")
-            self.asked[0], self.asked[1] = 1, seqs + 1
+            self.resting = [False] * seqs
+            self._ask()
         else:
             self.table = torch.arange(seqs * width, dtype=torch.int32, device="cuda").view(seqs, width)
         self.longest = longest
@@ -137,6 +138,9 @@ class AttentionHalf:
         self.step = self._step(sum(counts), max(counts))
         if self.shared:
             self._set(self.fresh, counts, np.int32)
+            if any(c and r for c, r in zip(counts, self.resting)):
+                self.resting = [r and not c for c, r in zip(counts, self.resting)]
+                self._ask()
             L.lutgemm_kv_place(self.pages, self.past, self.fresh, sum(counts), max(counts), self.first, None, None, None, self._stream())
             self.taken = [t + n for t, n in zip(self.taken, needed)]
             self.left -= sum(needed)
@@ -187,12 +191,13 @@ class AttentionHalf:
         self._adapt(self.adapters[1], self.mixed, y, tokens)
 
     def advance(self, x, y, residual=None):
-        """One token of every sequence, x [seqs][hidden]: placed, run, and its lengths advanced, all on the device, so that a captured call can be
-        replayed.  A sequence that finds no page, or is `longest` positions long, waits, and those behind it: their rows of y and
-        residual mean nothing, their lengths stay.  The host learns of it by `advanced`."""
+        """One token of every sequence that does not rest, x [seqs][hidden], their rows one after the other: placed, run, and their lengths
+        advanced, all on the device, so that a captured call can be replayed (`rest`, `end` and `place` say whose rows the next replay
+        takes).  A sequence that finds no page, or is `longest` positions long, waits, and those behind it (till it rests or ends): their
+        rows of y and residual mean nothing, their lengths stay.  The host learns of it by `advanced`."""
         if not self.shared:
             raise ValueError("sequences that advance on the device share their pages")
-        if self.seqs > MOST_ROWS or max(self.lengths) >= self.longest:
+        if self.seqs > MOST_ROWS or any(n >= self.longest and not r for n, r in zip(self.lengths, self.resting)):
             raise ValueError(f"up to {MOST_ROWS} sequences advance, up to a length of {self.longest}")
         self.masked, self.placed, self.known = False, False, False
         self.captured = self.captured or self.torch.cuda.is_current_stream_capturing()
@@ -250,7 +255,8 @@ class AttentionHalf:
         self.left += sum(back)
 
     def end(self, seq):
-        """Sequence `seq` is over, between two steps: its pages are free, and the next tokens are a new one's first."""
+        """Sequence `seq` is over, between two steps: its pages are free, and the next tokens that are placed are a new one's first, which rests
+        till then."""
         if self.placed:
             raise ValueError("a sequence ends after `keep`, or after `advanced`")
         self._check_known()
@@ -258,6 +264,17 @@ class AttentionHalf:
         if self.shared:
             self._set(self.past, self.lengths, np.int32)
             self._trim(self.lengths)
+            self.rest(seq)
+
+    def rest(self, seq, resting=True):
+        """Sequence `seq` has no part in `advance`, captured or not, until `place` brings tokens of it or `resting` is false."""
+        if not self.shared:
+            raise ValueError("sequences that advance on the device share their pages")
+        self.resting[seq] = bool(resting)
+        self._ask()
+
+    def _ask(self):
+        self.asked.copy_(self.torch.from_numpy(np.array([[0 if r else n for r in self.resting] for n in (1, self.seqs + 1)], dtype=np.int32)))
 
     def fill(self, x, y):
         """A prompt of every sequence, x [seqs][length][hidden], in chunks; y: their outputs."""

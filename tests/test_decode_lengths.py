@@ -167,3 +167,53 @@ def test_replays_beyond_the_longest(device, monkeypatch, seqs, page):
     assert half.lengths == [11, longest] + [12] * (seqs - 2) == half.past.tolist()
     half.end(1)
     assert half.owned.tolist() == half.taken == [1, 0] + [1] * (seqs - 2)
+
+
+def test_sequences_that_are_over_or_idle_sit_replays_out(device, monkeypatch):
+    """They get no token and no page; the others' rows follow one another."""
+    d = Decoding(monkeypatch, 512, 8, 2, 64, 3, 64, 16, page=32, pages=4)
+    half = d.half
+    half.place([10, 7, 15])
+    half.keep()
+    half.place([21, 0, 0])
+    half.keep()
+    half.end(1)
+    d.capture(monkeypatch, device)
+    assert half.advanced() == [31, 0, 15]
+    for k in range(2):
+        d.replay()
+        assert half.first.tolist() == [0, 1, 1, 2] and half.owner[:3].tolist() == [0, 2, -1] and half.positions[:3].tolist() == [31 + k, 15 + k, 0]
+    assert half.advanced() == [33, 0, 17] and half.taken == [2, 0, 1] and half.left == 1
+    half.rest(0)                                   # nobody else is told of a token of its
+    half.rest(1, False)
+    d.replay()
+    assert half.first.tolist() == [0, 0, 1, 2] and half.advanced() == [33, 1, 18] and half.left == 0
+    # tokens that are placed, or to be told otherwise, end it
+    half.end(2)
+    half.place([1, 0, 3])
+    half.keep()
+    half.rest(1)
+    d.replay()
+    assert half.first.tolist() == [0, 1, 1, 2] and half.advanced() == [35, 1, 4]
+    for s in range(3):
+        half.rest(s)
+    d.replay()
+    assert half.first.tolist() == [0, 0, 0, 0] and half.past.tolist() == [35, 1, 4]
+    half.rest(1, False)
+    half.place([29, 0, 0])
+    half.keep()
+    half.rest(0)
+    half.advance(None, None)                       # (one of 64 positions may rest)
+    assert half.advanced() == [64, 2, 4] and half.owner[:3].tolist() == [1, -1, -1]
+
+
+def test_sequences_with_pages_of_their_own_do_not_rest(device):
+    half = _half(512, 8, 2, 64, 2, 80, 16)
+    with pytest.raises(ValueError):
+        half.rest(0)
+    half.place([1, 1])
+    half.keep()
+    half.end(0)
+    half.place([1, 1])
+    half.keep()
+    assert half.lengths == [1, 2]

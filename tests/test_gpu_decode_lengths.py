@@ -91,3 +91,48 @@ def test_replays_beyond_the_longest():
     results[2].append(y[0].cpu().numpy())
     for s in range(3):
         D._close(np.stack(results[s]), sv.reference(s, seen[s])[begin[s]:])
+
+
+def test_sequences_that_are_over_sit_replays_out():
+    """The others' rows follow one another; a new sequence takes part from its first placed tokens on."""
+    torch = torch_cuda()
+    sv = Serving(4, 90, pages=6)
+    half = sv.half
+    x = D._tokens(torch, 4, 30, D.HIDDEN, seed=3)
+    half.fill(D._up(torch, x), torch.empty(4, 30, D.HIDDEN, dtype=torch.float16, device="cuda"))
+    token, y = torch.empty(4, D.HIDDEN, dtype=torch.float16, device="cuda"), torch.empty(4, D.HIDDEN, dtype=torch.float16, device="cuda")
+    stream = torch.empty(4, D.HIDDEN, device="cuda")
+    graph = _captured(torch, half, token, y, stream)
+    half.advanced()
+    seen, results, at = [x[s] for s in range(4)], [[] for _ in range(4)], [30] * 4
+
+    def replay(takers):
+        more = D._tokens(torch, 4, D.HIDDEN, seed=100 + sum(map(len, results)))
+        token.copy_(D._up(torch, more))
+        stream.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert half.owner[:4].tolist() == takers + [-1] * (4 - len(takers))
+        for row, s in enumerate(takers):
+            seen[s] = np.concatenate([seen[s], more[row:row + 1]])
+            results[s].append(y[row].cpu().numpy())
+
+    replay([0, 1, 2, 3])
+    half.advanced()
+    half.end(1)
+    half.rest(2)
+    for _ in range(3):
+        replay([0, 3])
+    assert half.advanced() == [34, 0, 31, 34] and half.left == 1 and half.taken == [2, 0, 1, 2]
+    first = results[1]
+    D._close(np.stack(first), sv.reference(1, seen[1])[30:])
+    seen[1], results[1], at[1] = D._tokens(torch, 5, D.HIDDEN, seed=4), [], 5
+    half.place([0, 5, 0, 0])
+    half.run(D._up(torch, seen[1]), torch.empty(5, D.HIDDEN, dtype=torch.float16, device="cuda"))
+    half.keep()
+    replay([0, 1, 3])
+    half.rest(2, False)
+    replay([0, 1, 2, 3])
+    assert half.advanced() == [36, 7, 32, 36] == [len(t) for t in seen] and half.left == 0
+    for s in range(4):
+        D._close(np.stack(results[s]), sv.reference(s, seen[s])[at[s]:])
