@@ -127,14 +127,16 @@ class AttentionHalf:
             if sum(needed) > self.left:
                 raise ValueError(f"a step needs {sum(needed)} pages more, of {self.left} that are free")
         self.counts, self.placed = list(counts), True
-        self._set(self.first, np.concatenate([[0], np.cumsum(counts)]), np.int32)
+        if not self.shared:                         # (else the device writes it)
+            self._set(self.first, np.concatenate([[0], np.cumsum(counts)]), np.int32)
         self._set(self.past, self.lengths, np.int32)
         below = [np.arange(c) for c in counts] if depths is None else [np.asarray(d) for d in depths]
         self._set(self.positions, np.concatenate([n + b for n, b in zip(self.lengths, below)]), np.int32)
         self.masked = mask is not None
         if self.masked:
             self._set(self.mask, np.array(mask, dtype=np.uint64).view(np.int64), np.int64)
-        self._set(self.owner, np.repeat(np.arange(self.seqs), counts), np.int32)
+        if self.adapters != (None, None):
+            self._set(self.owner, np.repeat(np.arange(self.seqs), counts), np.int32)
         self.step = self._step(sum(counts), max(counts))
         if self.shared:
             self._set(self.fresh, counts, np.int32)

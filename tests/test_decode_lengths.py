@@ -217,3 +217,24 @@ def test_sequences_with_pages_of_their_own_do_not_rest(device):
     half.place([1, 1])
     half.keep()
     assert half.lengths == [1, 2]
+
+
+@pytest.mark.parametrize("pages,adapters", [(0, False), (0, True), (9, False), (9, True)])
+def test_what_a_step_copies(device, monkeypatch, pages, adapters):
+    """Whose the tokens are matters to adapters alone; with shared pages the device writes where the sequences' rows begin."""
+    half = _half(512, 8, 2, 64, 2, 80, 16, page=32, pages=pages)
+    if adapters:
+        half.adapters = (None, L.lutgemm_adapters(16, 16, None, None, 512, 512, 1, 8))
+    copied, put = [], half._set
+    names = {id(t): name for name, t in vars(half).items()}
+
+    def spy(tensor, values, kind):
+        copied.append(names[id(tensor)])
+        put(tensor, values, kind)
+
+    monkeypatch.setattr(half, "_set", spy)
+    half.place([3, 2])
+    assert sorted(copied) == sorted(["past", "positions"] + ["owner"] * adapters + (["fresh"] if pages else ["first"]))
+    assert half.first.tolist() == [0, 3, 5] and half.positions[:5].tolist() == [0, 1, 2, 0, 1]
+    if adapters:
+        assert half.owner[:5].tolist() == [0, 0, 0, 1, 1]
