@@ -573,7 +573,8 @@ typedef struct lutgemm_adapters {
                   0..seqs-1 is none: y[t] = base[t]
      x            fp16 rows of x_stride: the product's input; 16-byte aligned, stride a multiple of 8
      base, y      fp16 or fp32 (LUTGEMM_Y_F16 / LUTGEMM_Y_F32) rows of base_stride and y_stride: the product's output.  y may be base
-                  (with the same stride), else must not overlap it, nor x in either case.  Any alignment that the type has; rows that begin on
+                  (with the same stride); else no byte of y's rows is one of base's or x's rows (LUTGEMM_EINVAL; parts of the same rows side by
+                  side are apart).  Strides up to 2^40.  Any alignment that the type has; rows that begin on
                   multiples of four elements, and m one, are faster
      workspace    lutgemm_adapt_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any other and shared with
                   products on the same stream if large enough

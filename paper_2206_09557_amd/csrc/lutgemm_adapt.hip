@@ -732,10 +732,13 @@ extern "C" int lutgemm_adapt(const void* x, const void* base, const lutgemm_adap
   if ((((uintptr_t)x | (uintptr_t)a.down | (uintptr_t)a.up | (uintptr_t)workspace) & 15) != 0) return LUTGEMM_EINVAL;
   if ((((uintptr_t)of | (uintptr_t)owner | (uintptr_t)a.ranks | (uintptr_t)a.scales) & 3) != 0 || ((uintptr_t)base | (uintptr_t)y) % size != 0) return LUTGEMM_EINVAL;
   if (x_stride < a.n || x_stride % 8 != 0 || base_stride < a.m || y_stride < a.m || (base == y && base_stride != y_stride)) return LUTGEMM_EINVAL;
+  if (x_stride > kMostAdaptStride || base_stride > kMostAdaptStride || y_stride > kMostAdaptStride) return LUTGEMM_EUNSUPPORTED;
   const AdaptPlan plan = plan_adapt(adapters, tokens);
   const int64_t ints = adapt_table_ints(plan, tokens), part_floats = adapt_part_floats(plan, a.rank);
   if (workspace_bytes < (size_t)(kCounterBytes + 4 * (ints + plan.parts * part_floats + adapt_joined_floats(plan, tokens, a.rank)))) return LUTGEMM_EWORKSPACE;
   if (tokens == 0) return LUTGEMM_OK;
+  const Rows x_rows = rows_of(x, tokens, x_stride, a.n, 2), base_rows = rows_of(base, tokens, base_stride, a.m, (int64_t)size), y_rows = rows_of(y, tokens, y_stride, a.m, (int64_t)size);
+  if (!apart(x_rows, y_rows) || (base != y && !apart(base_rows, y_rows))) return LUTGEMM_EINVAL;
   AdaptParams p = {};
   p.x = static_cast<const _Float16*>(x);
   p.base = base;

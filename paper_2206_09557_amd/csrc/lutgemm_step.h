@@ -12,10 +12,23 @@ namespace lutgemm_step_detail {
 constexpr int64_t kCounterBytes = 32768;   // of a workspace, which products keep their arrival counters in
 constexpr int64_t kCacheBytes = 32 << 20;   // of the L2 caches
 
+// ---- where outputs may stand ----
+// Rows of a matrix in memory, in bytes.  At least one; `pitch` is at least `bytes` and of more rows than one.
+struct Rows {
+  uintptr_t at;
+  int64_t rows, pitch, bytes;
+};
+inline Rows rows_of(const void* p, int64_t rows, int64_t stride, int64_t n, int64_t size) { return {(uintptr_t)p, rows, stride * size, n * size}; }
+// A kernel that reads a row of one before it writes that row of the other may be given both.
+inline bool same_rows(const Rows& a, const Rows& b) { return a.at == b.at && a.rows == b.rows && a.bytes == b.bytes && (a.pitch == b.pitch || a.rows == 1); }
+// Whether no byte is in both (parts of the same rows next to each other are apart).
+bool apart(const Rows& a, const Rows& b);
+
 // ---- low-rank adapters ----
 constexpr int kMostAdapters = 1024;
 constexpr int kMostRank = 256;
 constexpr int kMostAdapted = 1 << 16;      // tokens of a call
+constexpr int64_t kMostAdaptStride = (int64_t)1 << 40;     // (so that offsets in bytes stay within 64 bits)
 constexpr int kFewTokens = 256;            // as many as a wavefront groups by itself
 constexpr int kRankBlock = 64;             // ranks of a workgroup of the first product
 

@@ -1,9 +1,27 @@
-// Host side of what surrounds products and attention: how low-rank adapters split their work.  Nothing here touches the GPU.
+// Host side of what surrounds products and attention: how low-rank adapters split their work, where outputs may stand.  Nothing here touches the GPU.
 #include "lutgemm_step.h"
 
 #include <algorithm>
 
 namespace lutgemm_step_detail {
+
+bool apart(const Rows& a, const Rows& b) {
+  const uintptr_t a_end = a.at + (uintptr_t)((a.rows - 1) * a.pitch + a.bytes), b_end = b.at + (uintptr_t)((b.rows - 1) * b.pitch + b.bytes);
+  if (a_end <= b.at || b_end <= a.at) return true;
+  if (a.rows > 1 && b.rows > 1 && a.pitch == b.pitch) {        // where a row of b begins, from the beginning of the row of a before it
+    const int64_t behind = a.at < b.at ? (int64_t)(b.at - a.at) % a.pitch : (a.pitch - (int64_t)(a.at - b.at) % a.pitch) % a.pitch;
+    return behind >= a.bytes && behind + b.bytes <= a.pitch;
+  }
+  // Both in the order of their addresses, from the first row that may meet the other's first one.  (All rows of both in the worst case:
+  // matrices of different strides within one another, which hardly anybody has.)
+  auto first = [](const Rows& of, uintptr_t at) { return at > of.at && of.rows > 1 ? std::min((int64_t)(at - of.at) / of.pitch, of.rows - 1) : (int64_t)0; };
+  for (int64_t i = first(a, b.at), j = first(b, a.at); i < a.rows && j < b.rows;) {
+    const uintptr_t p = a.at + (uintptr_t)(i * a.pitch), q = b.at + (uintptr_t)(j * b.pitch);
+    if (p < q + (uintptr_t)b.bytes && q < p + (uintptr_t)a.bytes) return false;
+    p < q ? ++i : ++j;
+  }
+  return true;
+}
 
 int check_adapters(const lutgemm_adapters* a, int tokens) {
   if (!a || a->m < 1 || a->n < 8 || a->n % 8 != 0 || a->count < 1 || a->rank < 8 || a->rank % 8 != 0 || tokens < 0) return LUTGEMM_EINVAL;
