@@ -249,28 +249,6 @@ const void* family3(int threads, int runs, bool wide, bool bytes) { return pick<
 }  // namespace lutgemm_norm_parts
 
 #if LUT_PART == 0
-namespace {
-// The bytes from the first row's first value to the last row's last.
-struct Range {
-  uintptr_t from, to;
-};
-Range range_of(const void* p, int64_t rows, int64_t stride, int64_t n, int64_t size) {
-  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * stride + n) * size)};
-}
-// Whether a kernel that reads a row of `in` before it writes that row of `out` may be given both: the same rows of the same type, or
-// no byte in common (parts of one matrix's rows next to each other among them).
-bool apart(const void* in, int64_t in_stride, int64_t in_size, const void* out, int64_t out_stride, int64_t out_size, int64_t rows, int64_t n) {
-  const Range a = range_of(in, rows, in_stride, n, in_size), b = range_of(out, rows, out_stride, n, out_size);
-  if (a.to <= b.from || b.to <= a.from) return true;
-  if (in_stride * in_size != out_stride * out_size) return rows == 1 && in == out && in_size == out_size;
-  if (in == out) return in_size == out_size;
-  // Rows of one pitch: where a row of one begins within a row of the other.
-  const uintptr_t pitch = (uintptr_t)(in_stride * in_size);
-  const uintptr_t behind = a.from < b.from ? (b.from - a.from) % pitch : (pitch - (a.from - b.from) % pitch) % pitch;
-  return behind >= (uintptr_t)(n * in_size) && behind + (uintptr_t)(n * out_size) <= pitch;
-}
-}  // namespace
-
 extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales, int tokens, int n,
                                 int group, int64_t x_stride, int64_t stream_stride, int64_t y_stride, float eps, unsigned flags, void* hip_stream) {
   using namespace lutgemm_norm_parts;
@@ -288,10 +266,19 @@ extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void*
   if (tokens == 0) return LUTGEMM_OK;
   const int64_t most_stride = (int64_t)1 << 28;          // (so that offsets in bytes stay within 64 bits)
   if (x_stride > most_stride || y_stride > most_stride || ((residual || sum) && stream_stride > most_stride)) return LUTGEMM_EUNSUPPORTED;
-  if (!apart(x, x_stride, xs, y, y_stride, ys, tokens, n) || (residual && !apart(residual, stream_stride, ss, y, y_stride, ys, tokens, n)) ||
-      (sum && (!apart(x, x_stride, xs, sum, stream_stride, ss, tokens, n) || sum == y || !apart(sum, stream_stride, ss, y, y_stride, ys, tokens, n))) ||
-      (sum && residual && !apart(residual, stream_stride, ss, sum, stream_stride, ss, tokens, n)))
+  const Rows x_rows = rows_of(x, tokens, x_stride, n, xs), y_rows = rows_of(y, tokens, y_stride, n, ys), weight_rows = rows_of(weight, 1, n, n, 2);
+  const Rows residual_rows = rows_of(residual, tokens, stream_stride, n, ss), sum_rows = rows_of(sum, tokens, stream_stride, n, ss);
+  auto clash = [](const Rows& in, const Rows& out) { return !apart(in, out) && !same_rows(in, out); };
+  if (clash(x_rows, y_rows) || (residual && clash(residual_rows, y_rows)) || (weight && !apart(weight_rows, y_rows))) return LUTGEMM_EINVAL;
+  if (sum && (clash(x_rows, sum_rows) || (residual && clash(residual_rows, sum_rows)) || (weight && !apart(weight_rows, sum_rows)) || !apart(sum_rows, y_rows)))
     return LUTGEMM_EINVAL;
+  if (scales) {
+    const int64_t all = (int64_t)tokens * (group == 0 ? 1 : n / group);
+    const Rows scale_rows = rows_of(scales, 1, all, all, 4);
+    if (!apart(x_rows, scale_rows) || (residual && !apart(residual_rows, scale_rows)) || (weight && !apart(weight_rows, scale_rows)) ||
+        (sum && !apart(sum_rows, scale_rows)) || !apart(y_rows, scale_rows))
+      return LUTGEMM_EINVAL;
+  }
   Params p = {};
   p.x = x;
   p.residual = residual;

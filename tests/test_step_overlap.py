@@ -34,3 +34,18 @@ def test_adapters_results_over_inputs(change):
 @pytest.mark.parametrize("change", [dict(xs=1 << 41), dict(bs=(1 << 40) + 1, ys=(1 << 40) + 1), dict(ys=1 << 62, y=2 * FAR), dict(bs=(1 << 63) - 1, y=2 * FAR)], ids=str)
 def test_strides_beyond_what_offsets_hold(change):
     assert _adapt(**change) == U
+
+
+def _norm(**change):
+    """Three rows of 64 values in 128 bytes, and in 64 with two scales each."""
+    g = dict(x=A, residual=2 * A, weight=3 * A, sum=4 * A, y=5 * A, scales=6 * A, tokens=3, n=64, group=32, xs=64, ss=64, ys=64, eps=1e-5, flags=0)
+    return _refused(L.lutgemm_rms_norm, *{**g, **change}.values())
+
+
+@pytest.mark.parametrize("change", [
+    dict(scales=A), dict(scales=A + 3 * 128 - 4), dict(scales=A - 20), dict(scales=2 * A + 256), dict(scales=3 * A), dict(scales=3 * A + 124),
+    dict(scales=4 * A + 380), dict(scales=5 * A), dict(scales=5 * A + 188), dict(scales=5 * A - 20), dict(scales=5 * A + 60, ys=1 << 20), dict(scales=5 * A + 64, ys=80),
+    dict(scales=2 * A + 128, ss=74), dict(weight=5 * A), dict(weight=5 * A + 190), dict(weight=5 * A - 126), dict(weight=4 * A), dict(weight=4 * A + 200),
+    dict(weight=4 * A + 128, ss=100), dict(weight=5 * A + 382, scales=None, group=0), dict(weight=4 * A + 764, flags=L.LUTGEMM_NORM_STREAM_F32)], ids=str)
+def test_norms_outputs_over_scales_and_weights(change):
+    assert _norm(**change) == E
