@@ -577,7 +577,8 @@ typedef struct lutgemm_adapters {
                   side are apart).  Strides up to 2^40.  Any alignment that the type has; rows that begin on
                   multiples of four elements, and m one, are faster
      workspace    lutgemm_adapt_workspace_bytes(...) bytes, prepared by lutgemm_workspace_init like any other and shared with
-                  products on the same stream if large enough
+                  products on the same stream if large enough.  It does not grow with the tokens throughout (fewer of them can be split into more
+                  parts): ask for every number of tokens that will be used
    Sums are fp32, and A_a x[t] is kept to 22 bits of its largest element.  An adapter's weights are read once for up to 16 of its tokens (32 or 64 where the
    tokens are many).  Tokens with adapters of their own do not see those of others, nor one another's infinities and NaNs (which may
    be NaN where the exact result is an infinity).  Up to 65536 tokens.  Bitwise reproducible.  */

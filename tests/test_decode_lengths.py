@@ -238,3 +238,21 @@ def test_what_a_step_copies(device, monkeypatch, pages, adapters):
     assert half.first.tolist() == [0, 3, 5] and half.positions[:5].tolist() == [0, 1, 2, 0, 1]
     if adapters:
         assert half.owner[:5].tolist() == [0, 0, 0, 1, 1]
+
+
+@pytest.mark.parametrize("count,rank", [(3, 16), (24, 256), (40, 128), (64, 64)])
+def test_a_layer_has_workspace_for_adapters_of_any_step(on_host, count, rank):  # noqa: F811
+    """Fewer tokens may need more than more of them do: a call that has too little is refused."""
+    hidden, heads, dim = 5120, 40, 128
+    shapes = (3 * heads * dim, hidden), (hidden, heads * dim)
+    adapters = [L.lutgemm_adapters(16, 16, None, None, m, n, count, rank) for m, n in shapes]
+    half = _half(hidden, heads, heads, dim, 4, 100, 16, adapters=adapters)
+    for a, (m, n) in zip(adapters, shapes):
+        need = [L.lutgemm_adapt_workspace_bytes(a, t) for t in range(1, decode.MOST_ROWS + 1)]
+        assert max(need) <= half.ws_bytes
+        fewer = [t for t in range(1, decode.MOST_ROWS) if need[t - 1] > need[t]]
+        assert bool(fewer) == (count > 3)
+        for t in fewer:
+            with pytest.raises(L.LutGemmError) as e:
+                L.lutgemm_adapt(16, 16, a, 16, None, 16, t, 0, n, m, m, 0, 16, need[t])
+            assert e.value.code == L.LUTGEMM_EWORKSPACE
