@@ -543,7 +543,7 @@ enum { LUTGEMM_NORM_STREAM_F32 = 8 /* residual and sum are fp32, else fp16 */ };
      s = x[t][c] + residual[t][c],   sum[t][c] = s,   y[t][c] = s * weight[c] / sqrt(mean over c of s^2 + eps)
    in fp32 from the sum before its rounding (squares are added in 64 bits), one rounding to fp16.  With scales not NULL y is 8 bits,
    by the rule of the cache's but with an fp32 scale: for every `group` channels (a multiple of 32 that divides n; 0: the whole row, whatever n)
-     scales[t][g] = max|y| / 127,    y = rint(y / scale) in -127..127 (int8; the quotient within 2^-23 of itself)
+     scales[t][g] = max|y| / 127,    y = rint(y / scale) in -127..127 (int8; the quotient within 3 * 2^-24 of itself)
    A group with an infinity or a NaN has a NaN for its scale, one whose values are all below 2^-100 zero; codes are 0 in both.
      residual   NULL: nothing is added                sum      NULL: not kept
      weight     fp16 [n], NULL: ones                  scales   fp32 [tokens][n / group], without gaps
