@@ -402,26 +402,23 @@ __global__ __launch_bounds__(kThreads) void lutgemm_adapt_join_kernel(AdaptParam
 template <int TILE, int PAD>
 struct Joined {
   static constexpr int LOADS = TILE * PAD / 8 / kThreads > 0 ? TILE * PAD / 8 / kThreads : 1;
-  static constexpr bool HELD = LOADS <= 4;       // (in registers meanwhile)
-  u32x4 high[HELD ? LOADS : 1], low[HELD ? LOADS : 1];
+  static_assert(LOADS <= 4, "in registers meanwhile");
+  u32x4 high[LOADS], low[LOADS];
   int drop;
-  const u32x4* from;
   __device__ __forceinline__ static int at(int u) { return min(u * kThreads + (int)threadIdx.x, TILE * PAD / 8 - 1); }
   __device__ __forceinline__ void ask(const AdaptParams& p) {
-    from = reinterpret_cast<const u32x4*>(p.joined + (int64_t)blockIdx.y * TILE * (PAD + 1));
     if (!p.joined) return;
-    if constexpr (HELD) {
+    const u32x4* from = reinterpret_cast<const u32x4*>(p.joined + (int64_t)blockIdx.y * TILE * (PAD + 1));
 #pragma unroll
-      for (int u = 0; u < LOADS; ++u) high[u] = from[at(u)], low[u] = from[TILE * PAD / 8 + at(u)];
-    }
+    for (int u = 0; u < LOADS; ++u) high[u] = from[at(u)], low[u] = from[TILE * PAD / 8 + at(u)];
     drop = reinterpret_cast<const int*>(from + TILE * PAD / 4)[min((int)threadIdx.x, TILE - 1)];
   }
   __device__ __forceinline__ void put(_Float16* to_high, _Float16* to_low, int pitch, int* to_drop) const {
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int place = at(u) / (PAD / 8) * pitch + at(u) % (PAD / 8) * 8;
-      *reinterpret_cast<u32x4*>(to_high + place) = HELD ? high[HELD ? u : 0] : from[at(u)];
-      *reinterpret_cast<u32x4*>(to_low + place) = HELD ? low[HELD ? u : 0] : from[TILE * PAD / 8 + at(u)];
+      *reinterpret_cast<u32x4*>(to_high + place) = high[u];
+      *reinterpret_cast<u32x4*>(to_low + place) = low[u];
     }
     if (threadIdx.x < TILE) to_drop[threadIdx.x] = drop;
   }
