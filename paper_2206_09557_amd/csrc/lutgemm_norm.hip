@@ -224,7 +224,10 @@ template <typename X, typename S, bool BYTES, bool WIDE>
 const void* pick(int threads, int runs) {
 #define CASE(t, r) \
   if (threads == t && runs == r) return reinterpret_cast<const void*>(lutgemm_rms_norm_kernel<X, S, BYTES, WIDE, t, r>);
-  CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 1) CASE(256, 2) CASE(256, 3) CASE(256, 4) CASE(512, 3) CASE(512, 4) CASE(1024, 1) CASE(1024, 2) CASE(1024, 3) CASE(1024, 4)
+  CASE(64, 1) CASE(64, 2) CASE(64, 4) CASE(256, 2) CASE(256, 3) CASE(256, 4) CASE(512, 3) CASE(512, 4) CASE(1024, 3) CASE(1024, 4)
+  if constexpr (BYTES) {                           // few rows, over more threads
+    CASE(256, 1) CASE(1024, 1) CASE(1024, 2)
+  }
 #undef CASE
   return nullptr;
 }
