@@ -10,7 +10,7 @@
 // sums are added up in an order that the sizes decide, by each workgroup of the second product or, of tiles of 64 tokens or many tokens, once.  H stays fp32 until
 // then, and meets B as two fp16 numbers (22 bits) of a power of two that the token's largest decides: rounded to one, it would add as much
 // error as the result's own rounding to fp16, and more than that of fp32 results.  Measured: 32 adapters of rank 16 beside 36864 x 12288, one
-// token each, 56 MB: 6 + 12.3 us; three of up to 64 beside 12288 x 5120, 4096 tokens, 236 MB: sorting 7.5, products 19 and 52, joining 5.6.
+// token each, 56 MB: 6 + 12.8 us; three of up to 64 beside 12288 x 5120, 4096 tokens, 236 MB: sorting 7.6, products 19 and 50, joining 5.5.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 

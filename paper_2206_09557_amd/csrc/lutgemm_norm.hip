@@ -2,8 +2,8 @@
 //
 // A workgroup owns a row and holds it in registers between the two things that are done with it, so that every value
 // is read once: s = x + r, the sum of squares (in 64 bits: squares of fp32 values leave 32), then s * inv * w.  What bounds it is
-// HBM: 4096 rows of 12288 channels, 403 MB, 68.7 us, 5.9 TB/s (a copy past the caches: 6.3); of few rows the launch and one chain of
-// load, sum and store (3.4 us for one).  Rows that begin anywhere: 4096 of 12289 channels 92 us (280 value by value).  The next row on its way during a row's sum (512 workgroups that stay) was no faster: 75 to 79 us.
+// HBM: 4096 rows of 12288 channels, 403 MB, 68.4 us, 5.9 TB/s (a copy past the caches: 6.3); of few rows the launch and one chain of
+// load, sum and store (3.4 us for one).  Rows that begin anywhere: 4096 of 12289 channels 91 us (280 value by value).  The next row on its way during a row's sum (512 workgroups that stay) was no faster: 75 to 79 us.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -302,8 +302,10 @@ extern "C" int lutgemm_rms_norm(const void* x, const void* residual, const void*
                     (!sum || rows16(sum, stream_stride, ss)) && (uintptr_t)weight % 16 == 0 &&
                     (bytes ? ((uintptr_t)y | (uintptr_t)y_stride) % 8 == 0 : rows16(y, y_stride, 2));
   const int units = (n + 7) / 8;
-  // Threads enough for four runs each; more where there are few rows to 8 bits (509 of 8192 channels 10.1 us with 1024 threads, 11.5
-  // with 256; to fp16, rows that begin anywhere: 300 of 5003 6.6 and 5.3 with 256, 1000 12.4 and 9.3).
+  // Threads enough for four runs each; more where there are few rows to 8 bits.  Groups of 128, an fp32 stream, us with a run a thread
+  // and with four: 64 rows of 8192 channels 5.2 and 5.8, 509 10.7 and 12.8, 1024 19.9 and 21.0, 4096 64.2 and 66.4; of 2048 channels 3.6 and 4.9,
+  // 5.0 and 6.3, 7.0 and 8.6, 19.0 and 20.6: less and less, but nowhere the other way round.  (To fp16, rows that begin anywhere: 300 of 5003
+  // 6.6 with more threads and 5.3 with 256, 1000 12.4 and 9.3.)
   const bool spread = tokens <= 1024 && bytes;
   const int threads = spread ? (units <= 64 ? 64 : (units <= 256 ? 256 : 1024)) : (units <= 256 ? 64 : (units <= 1024 ? 256 : (units <= 2048 ? 512 : 1024)));
   int runs = (units + threads - 1) / threads;

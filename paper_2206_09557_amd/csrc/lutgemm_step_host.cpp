@@ -40,14 +40,15 @@ AdaptPlan plan_adapt(const lutgemm_adapters* a, int tokens) {
   p.tiles = (int)(groups + (t - groups) / p.tile);
   const int64_t rank_blocks = (a->rank + kRankBlock - 1) / kRankBlock;
   // Of the first product as many workgroups as leave none waiting (1024 of them fit the device where a tile and a chunk of the ranks are small,
-  // else 512, but a third fewer is as fast, and leaves fewer parts to add up: 4096 tokens, 5120 columns, rank 64: 18.4 us in five parts, 23.2 in seven).
+  // else 512, but a third fewer is about as fast, and leaves fewer parts to add up: 4096 tokens, rank 64: 5120 columns 18.7 us in five parts and
+  // 18.5 in seven, 12288 columns 37.0 and 34.4 (39.5 in four); 1000 tokens, 5120 columns 9.2 in ten, 11.1 in seven, 8.9 in twenty).
   const int64_t chunk = p.tile == 16 && a->rank <= 32 ? 512 : 256, units = p.tiles * rank_blocks;
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(a->n + chunk - 1) / chunk, (chunk == 512 ? 1024 : 352) / units, 32}));
   p.part = (int)(((a->n + parts - 1) / parts + chunk - 1) / chunk * chunk);
   p.parts = (int)((a->n + p.part - 1) / p.part);
   // Of the second one, which has 768 or 512 at work, about as many as that: a round more for a few would be as long as the first, and
-  // each begins with 4 us in which it streams nothing (32 adapters of rank 16, 36864 rows: 12.4 us in 768 workgroups, 14.6 in 1152;
-  // 12288 rows of 4096 tokens, rank 64: 48.8 in 469, 54.5 in 804).
+  // each begins with 4 us in which it streams nothing (32 adapters of rank 16, 36864 rows: 12.9 us in 768 workgroups, 17.2 in 1152;
+  // 12288 rows of 4096 tokens, rank 64: 50.5 in 469, 52.7 in 804).
   const int64_t step = p.tile == 16 && a->rank <= 16 ? 512 : 256, pieces = std::max<int64_t>(1, (p.tile == 16 && a->rank <= 32 ? 768 : 512) / p.tiles);
   p.rows = (int)(std::max<int64_t>(1, ((a->m + pieces - 1) / pieces + step / 2) / step) * step);
   return p;
