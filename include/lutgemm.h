@@ -549,8 +549,8 @@ enum { LUTGEMM_NORM_STREAM_F32 = 8 /* residual and sum are fp32, else fp16 */ };
      weight     fp16 [n], NULL: ones                  scales   fp32 [tokens][n / group], without gaps
    Row t of x begins at t * x_stride, of residual and sum at t * stream_stride, of y at t * y_stride; strides are at least n, up to 2^28.
    sum may be residual, or x where the types agree; y may be x or residual where types and strides do.  Else outputs, scales among
-   them, overlap neither inputs, weight among them, nor one another (LUTGEMM_EINVAL; parts of the same rows side by side are apart).  n up to 32768, tokens up to 2^21, eps > 0.
-   Any alignment that the types have; rows of 16-byte multiples are faster.  A row with an infinity or a NaN is none of the others'
+   them, overlap neither inputs, weight among them, nor one another (LUTGEMM_EINVAL; parts of the same rows side by side are apart).
+   n up to 32768, tokens up to 2^21, eps > 0.  Any alignment that the types have; rows of 16-byte multiples are faster.  A row with an infinity or a NaN is none of the others'
    business.  Bitwise reproducible.                                                       */
 int lutgemm_rms_norm(const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales, int tokens, int n,
                      int group, int64_t x_stride, int64_t stream_stride, int64_t y_stride, float eps, unsigned flags,
